@@ -559,6 +559,157 @@ beagle_status beagle_xattn_draft_step_prepared(const beagle_xattn_desc* desc,
     const uint32_t* tree_mask, int32_t mask_words, void* y, float* lse,
     void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * The paged cache: key/value rows of many sequences of different lengths in
+ * pages of one pool, for programs that draft for many users at once (section
+ * 4.1, KV-cache paragraph, per sequence).
+ *
+ * A sequence lives in a slot.  Row j of slot s stands in page
+ * page_table[s][j / page_rows] at j % page_rows of k_pages / v_pages; a row is
+ * the row [G,d] of the contiguous cache, so such a cache of n * page_rows rows
+ * is a pool of n pages.  lens[s] is the number of rows that slot s holds (0: it
+ * is empty).  refs[p] is the number of slots whose held part of the table names
+ * page p; a page with refs[p] == 0 is free.  A new pool is lens and refs zeroed.
+ * All five arrays are DEVICE memory of the caller (k_pages, v_pages 16-byte
+ * aligned, the others 4-byte), and change in the order of the stream only, so
+ * a whole drafting loop can be captured in a graph.
+ *
+ * What the device arrays of a call hold cannot be checked on the host: a slot
+ * outside [0, n_slots) is an empty sequence (nothing is written for it), lengths
+ * are clamped to what a slot can hold, and a page number outside [0, n_pages) is a page
+ * whose rows nobody sees.  No content leads to an access outside the buffers.
+ *
+ * Supported: page_rows a power of two from 4 to 4096, n_slots <= 8192,
+ * slot_pages * page_rows <= 2^28, n_pages <= 2^28 (the pool itself may be of
+ * any size: offsets are 64 bits); BEAGLE_F32 any d <= 128 with d % 4 == 0,
+ * BEAGLE_BF16 d == 128.  Of desc the calls read batch (B <= 8192 entries),
+ * seq_q (M rows of each entry, B * M <= 2^28), n_q_heads, n_kv_heads, head_dim,
+ * io_dtype, softmax_scale, flags (BEAGLE_FLAG_ROPE only), rope_base,
+ * rope_positions [B*M] and, where they say so, seq_kv and hidden.
+ * Workspaces are 256-byte aligned (beagle_xattn_paged_workspace_bytes for the same
+ * desc and cache); their content before a call does not matter.
+ */
+typedef struct {
+  int32_t struct_size;          /* sizeof(beagle_paged_cache); checked           */
+  int32_t n_pages;              /* P                                             */
+  int32_t page_rows;            /* rows of a page                                */
+  int32_t n_slots;              /* N                                             */
+  int32_t slot_pages;           /* width of the table: pages a slot can hold     */
+  int32_t reserved;             /* 0                                             */
+  void *k_pages, *v_pages;      /* [P, page_rows, G, d] in io_dtype              */
+  int32_t *page_table;          /* [N, slot_pages]                               */
+  int32_t *lens;                /* [N]                                           */
+  int32_t *refs;                /* [P]                                           */
+} beagle_paged_cache;
+
+enum { BEAGLE_WS_PAGED_ATTEND = 0, BEAGLE_WS_PAGED_APPEND = 1, BEAGLE_WS_PAGED_FORK = 2, BEAGLE_WS_PAGED_COMPACT = 3,
+       BEAGLE_WS_PAGED_DRAFT = 4, BEAGLE_WS_PAGED_KV_APPEND = 5 };
+
+/* Workspace bytes of a paged call (`which` is BEAGLE_WS_PAGED_*); 0 for an
+ * invalid descriptor or cache. */
+size_t beagle_xattn_paged_workspace_bytes(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, int which);
+
+/*
+ * Attention of M queries of each of B entries over their sequences' rows.
+ * Entry b reads slot slots[b] (NULL: slot b; entries may share a slot).  With
+ * n = lens of that slot, at most desc->seq_kv (the longest sequence that the
+ * call is asked to serve: rows behind it are not seen), and nt = n_true[b]
+ * clamped to [0, n] (n_true NULL: nt = n), query m sees
+ *   true row j < nt      iff window == 0, or j < sinks, or j >= nt - window
+ *   drafted row nt <= j < n  iff bit (j - nt) % 32 of tree_mask[b][m][(j - nt) / 32]
+ *                        is set (words from mask_words on count as zero)
+ * that is, beagle_xattn_draft_step_tree's mask, and optionally a sliding window
+ * over the true rows of which the first `sinks` rows stay visible; rows that
+ * the window hides are not fetched.  n_true NULL: tree_mask is not read.
+ *   lse = log sum_j exp(scale <q, k_j>),   o = sum_j exp(scale <q, k_j> - lse) v_j
+ * over the rows that the query sees; with none of them, or with every
+ * score -infinity, o = 0 and lse = -infinity.  What stands in rows that a query
+ * does not see (stale, infinite, not a number) does not reach its result.
+ *   in : q [B,M,H,d] (rotated by the caller if its model rotates), slots,
+ *        n_true [B] or NULL, tree_mask uint32 [B,M,mask_words] or NULL
+ *   out: o [B,M,H,d], lse [B,H,M] float
+ * The work is split by the lengths as they stand on the device: a batch of any
+ * mix of lengths takes the time of its rows in all.
+ * Workspace: BEAGLE_WS_PAGED_ATTEND.
+ */
+beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words, int32_t window, int32_t sinks,
+    void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows into the cache.  Entry b keeps the first pos[b] rows of its slot (pos
+ * NULL, or more than the slot holds: all of them), gives up the pages behind
+ * them, takes the pages it lacks and stores its n = n_new[b] (NULL: M; clamped to
+ * [0, M]) rows at pos[b] .. pos[b] + n - 1: resetting a sequence to its true rows
+ * and appending the next ones is one call, n = 0 alone drops rows.  A page that
+ * the slot keeps a part of and shares with others is copied first, so other
+ * slots never see the change.  With BEAGLE_FLAG_ROPE the K rows are rotated, at
+ * desc->rope_positions[b * M + i] or, if that is NULL, at their row numbers.
+ * Pages are taken lowest number first, in the order of the entries; pages
+ * given up in the call can be taken in it.  If the pool runs out, the entries
+ * that the pages reached before it did not get any keep their first pos[b] rows and
+ * store none, as does an entry whose rows exceed what a slot can hold; short_pages
+ * (DEVICE, one int32, or NULL) takes the number of pages missing in all, 0 if
+ * everything was stored.  Of two entries with one slot the first counts.
+ *   in    : k_new, v_new [B,M,G,d]; slots, pos, n_new [B] or NULL
+ *   in/out: cache
+ * Rows of k_new / v_new from n on are not read.
+ * Workspace: BEAGLE_WS_PAGED_APPEND.
+ */
+beagle_status beagle_xattn_paged_append(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const int32_t* slots,
+    const int32_t* pos, const int32_t* n_new, const void* k_new, const void* v_new, int32_t* short_pages,
+    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Slot dst[b] becomes the first rows[b] rows (rows NULL, or more than there
+ * are: all) of slot src[b] as it was before the call, sharing its pages; what
+ * dst[b] held is given up.  That forks a sequence (dst another slot), reorders
+ * a beam (dst and src any lists over the same slots), shortens a sequence (dst ==
+ * src) and frees it (src outside [0, n_slots), or rows 0).  No row moves: a page
+ * that ends up shared in part is copied when one of its slots appends.  Table
+ * entries behind the held pages become -1.  Of two entries with one dst the
+ * first counts.  in: dst, src, rows [B] (rows may be NULL).
+ * Workspace: BEAGLE_WS_PAGED_FORK.
+ */
+beagle_status beagle_xattn_paged_fork(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const int32_t* dst,
+    const int32_t* src, const int32_t* rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Moves the cache into another pool, larger or smaller: the live pages, in the order of
+ * their numbers, become pages 0, 1, 2, .. of `into` (same page_rows and n_slots;
+ * n_pages and slot_pages its own; no memory in common with `cache`); its table,
+ * lens and refs are written whole, entries behind the held pages -1, and pages
+ * that nothing moved to keep their content.  If `into` has fewer pages than
+ * are live (or a slot holds more than its slot_pages), the sequences end before their first row
+ * that has no page there; short_pages (DEVICE, one int32, or NULL) takes the
+ * number of live pages that did not fit its n_pages.  desc: batch is not read.
+ *   in : cache    out: into
+ * Workspace: BEAGLE_WS_PAGED_COMPACT.
+ */
+beagle_status beagle_xattn_paged_compact(const beagle_xattn_desc* desc, const beagle_paged_cache* cache,
+    const beagle_paged_cache* into, int32_t* short_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The draft step and the cache append of many sequences at once, from states:
+ *   beagle_xattn_draft_step_paged: q = x Wq, beagle_xattn_paged_attend, y = o Wo.
+ *     With BEAGLE_FLAG_ROPE q is rotated at desc->rope_positions[b * M + m], or,
+ *     if that is NULL, at the number of rows that the slot holds.  q and o are
+ *     stored in io_dtype between the steps.
+ *       in : x_draft [B,M,D], wq [D,H*d], wo [H*d,D]    out: y [B,M,D], lse [B,H,M]
+ *     Workspace: BEAGLE_WS_PAGED_DRAFT.
+ *   beagle_xattn_kv_append_paged: K = x Wk, V = x Wv, beagle_xattn_paged_append.
+ *       in : x_new [B,M,D], wk, wv [D,G*d]
+ *     Workspace: BEAGLE_WS_PAGED_KV_APPEND.
+ * desc->hidden is read; shapes and operand sizes as for beagle_xattn_draft_step
+ * with B * M queries.
+ */
+beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words,
+    int32_t window, int32_t sinks, void* y, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+beagle_status beagle_xattn_kv_append_paged(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_new,
+    const void* wk, const void* wv, const int32_t* slots, const int32_t* pos, const int32_t* n_new, int32_t* short_pages,
+    void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ---- mask / index inspection (HOST memory, integers only, no GPU needed) --
  * These run the same index code that the kernels use, so that it can be
  * compared bit for bit with a mask built independently from the paper. */

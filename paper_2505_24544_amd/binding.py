@@ -23,6 +23,8 @@ BEAGLE_F32, BEAGLE_BF16 = 0, 1
 BEAGLE_FLAG_NEED_DXKV, BEAGLE_FLAG_WGRAD_F32, BEAGLE_FLAG_ROPE, BEAGLE_FLAG_STATES_F16 = 1, 2, 4, 8
 BEAGLE_WS_FWD, BEAGLE_WS_BWD, BEAGLE_WS_DRAFT, BEAGLE_WS_APPEND, BEAGLE_WS_BWD_SIM, BEAGLE_WS_BLOCK_APPEND = 0, 1, 2, 3, 4, 5
 BEAGLE_WS_BLOCK_FWD, BEAGLE_WS_BLOCK_BWD, BEAGLE_WS_BLOCK_DRAFT, BEAGLE_WS_BLOCK_BWD_SIM = 0, 1, 2, 3
+(BEAGLE_WS_PAGED_ATTEND, BEAGLE_WS_PAGED_APPEND, BEAGLE_WS_PAGED_FORK, BEAGLE_WS_PAGED_COMPACT, BEAGLE_WS_PAGED_DRAFT,
+ BEAGLE_WS_PAGED_KV_APPEND) = range(6)
 STATUS_NAMES = {0: "BEAGLE_OK", 1: "BEAGLE_ERR_NULL", 2: "BEAGLE_ERR_SHAPE", 3: "BEAGLE_ERR_UNSUPPORTED",
                 4: "BEAGLE_ERR_WORKSPACE", 5: "BEAGLE_ERR_ALIGN", 6: "BEAGLE_ERR_HIP"}
 
@@ -35,6 +37,8 @@ EXPORTS = (
     "beagle_xattn_block_draft_step", "beagle_xattn_block_draft_step_prepared", "beagle_xattn_block_prepare_weights",
     "beagle_xattn_block_fwd_sim", "beagle_xattn_block_bwd_sim",
     "beagle_xattn_block_kv_append",
+    "beagle_xattn_paged_workspace_bytes", "beagle_xattn_paged_attend", "beagle_xattn_paged_append", "beagle_xattn_paged_fork",
+    "beagle_xattn_paged_compact", "beagle_xattn_draft_step_paged", "beagle_xattn_kv_append_paged",
     "beagle_xattn_mask_row_limit", "beagle_xattn_mask_dense", "beagle_xattn_tile_map",
     "beagle_xattn_profile_begin", "beagle_xattn_profile_end", "beagle_xattn_profile_get",
     "beagle_xattn_probe_read", "beagle_xattn_probe_clock", "beagle_xattn_status_string", "beagle_xattn_version",
@@ -91,6 +95,11 @@ class beagle_block_grads(C.Structure):
                                    "dg_q", "dg_kv", "dg_mlp", "dxpred")]
 
 
+class beagle_paged_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("struct_size", "n_pages", "page_rows", "n_slots", "slot_pages", "reserved")] + \
+               [(n, _VP) for n in ("k_pages", "v_pages", "page_table", "lens", "refs")]
+
+
 def _fill(struct, tensors: dict):
     """Pointer struct from a dict name -> tensor / address / None; keeps nothing alive (the caller does)."""
     names = [f[0] for f in struct._fields_ if f[1] is _VP]
@@ -121,6 +130,23 @@ def make_block_saved(**tensors) -> beagle_block_saved:
 
 def make_block_grads(**tensors) -> beagle_block_grads:
     return _fill(beagle_block_grads, tensors)
+
+
+def make_paged_cache(k_pages, v_pages, page_table, lens, refs) -> beagle_paged_cache:
+    """k_pages, v_pages [P, page_rows, G, d]; page_table [N, slot_pages], lens [N], refs [P] int32, all on one device.  Keeps
+    nothing alive (the caller does)."""
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
+        raise ValueError("k_pages and v_pages are [P, page_rows, G, d] of one type")
+    if page_table.dim() != 2 or tuple(lens.shape) != tuple(page_table.shape[:1]) or tuple(refs.shape) != tuple(k_pages.shape[:1]):
+        raise ValueError("page_table is [N, slot_pages], lens [N], refs [P]")
+    _device(k_pages, v_pages, page_table, lens, refs)
+    for t in (page_table, lens, refs):
+        _ints(t)
+    c = beagle_paged_cache(C.sizeof(beagle_paged_cache), k_pages.shape[0], k_pages.shape[1], page_table.shape[0],
+                           page_table.shape[1], 0, *(_ptr(t) for t in (k_pages, v_pages, page_table, lens, refs)))
+    c.rows = tuple(k_pages.shape[2:])       # [G, d] of a row, its element type and its device: checked against a call's tensors
+    c.dtype, c.device = k_pages.dtype, k_pages.device
+    return c
 
 
 _lib = None
@@ -189,6 +215,22 @@ def lib() -> C.CDLL:
                                                         vp, vp, vp, C.c_int32, vp]
     L.beagle_xattn_kv_append.restype = C.c_int
     L.beagle_xattn_kv_append.argtypes = [dp] + [vp] * 5 + [C.c_int32, vp, C.c_size_t, vp]
+    cp = C.POINTER(beagle_paged_cache)
+    L.beagle_xattn_paged_workspace_bytes.restype = C.c_size_t
+    L.beagle_xattn_paged_workspace_bytes.argtypes = [dp, cp, C.c_int]
+    view = [vp, vp, vp, C.c_int32, C.c_int32, C.c_int32]
+    L.beagle_xattn_paged_attend.restype = C.c_int
+    L.beagle_xattn_paged_attend.argtypes = [dp, cp, vp] + view + [vp, vp] + [vp, C.c_size_t, vp]
+    L.beagle_xattn_paged_append.restype = C.c_int
+    L.beagle_xattn_paged_append.argtypes = [dp, cp] + [vp] * 6 + [vp, C.c_size_t, vp]
+    L.beagle_xattn_paged_fork.restype = C.c_int
+    L.beagle_xattn_paged_fork.argtypes = [dp, cp] + [vp] * 3 + [vp, C.c_size_t, vp]
+    L.beagle_xattn_paged_compact.restype = C.c_int
+    L.beagle_xattn_paged_compact.argtypes = [dp, cp, cp, vp] + [vp, C.c_size_t, vp]
+    L.beagle_xattn_draft_step_paged.restype = C.c_int
+    L.beagle_xattn_draft_step_paged.argtypes = [dp, cp, vp, vp, vp] + view + [vp, vp] + [vp, C.c_size_t, vp]
+    L.beagle_xattn_kv_append_paged.restype = C.c_int
+    L.beagle_xattn_kv_append_paged.argtypes = [dp, cp] + [vp] * 7 + [vp, C.c_size_t, vp]
     L.beagle_xattn_mask_row_limit.restype = C.c_int
     L.beagle_xattn_mask_row_limit.argtypes = [dp, vp]
     L.beagle_xattn_mask_dense.restype = C.c_int
@@ -229,6 +271,24 @@ def _stream(stream):
         import torch
         return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _device(*tensors):
+    """The one device that the tensors among the arguments are on, or None."""
+    seen = {t.device for t in tensors if t is not None and not isinstance(t, int)}
+    if len(seen) > 1:
+        raise ValueError("tensor arguments are on different devices: %s" % ", ".join(sorted(str(d) for d in seen)))
+    return seen.pop() if seen else None
+
+
+def _ints(t, count=None):
+    """Address of a tensor of 32-bit whole numbers (of `count` of them), or of None or an address as it is."""
+    if t is not None and not isinstance(t, int):
+        if str(t.dtype) not in ("torch.int32", "torch.uint32"):
+            raise ValueError("an index argument is a tensor of 32-bit whole numbers, not of %s" % t.dtype)
+        if count is not None and t.numel() != count:
+            raise ValueError("an index argument has %d values, %d are needed" % (t.numel(), count))
+    return _ptr(t)
 
 
 def _nbytes(ws):
@@ -384,6 +444,104 @@ def beagle_xattn_kv_append(desc, x_new, wk, wv, k_cache, v_cache, pos, workspace
         C.byref(desc), *(_ptr(t) for t in (x_new, wk, wv, k_cache, v_cache)), int(pos),
         _ptr(workspace), _nbytes(workspace) if workspace_bytes is None else workspace_bytes, _stream(stream))
     return _check(st, "beagle_xattn_kv_append", check)
+
+
+def _paged_rows(desc, t, heads):
+    """Address of a tensor of desc.batch * desc.seq_q rows of `heads` heads (0: of width desc.hidden) in desc's type."""
+    if t is not None and not isinstance(t, int):
+        want = "torch.bfloat16" if desc.io_dtype == BEAGLE_BF16 else "torch.float32"
+        if str(t.dtype) != want:
+            raise ValueError("a tensor of %s is needed, not of %s" % (want, t.dtype))
+        if t.numel() != desc.batch * desc.seq_q * (heads * desc.head_dim if heads else desc.hidden):
+            raise ValueError("a tensor of shape %s does not hold batch * seq_q rows" % (tuple(t.shape),))
+    return _ptr(t)
+
+
+def _paged_lse(desc, t):
+    if t is not None and not isinstance(t, int) and (str(t.dtype) != "torch.float32" or t.numel() != desc.batch * desc.n_q_heads * desc.seq_q):
+        raise ValueError("lse is a torch.float32 tensor [batch, heads, seq_q]")
+    return _ptr(t)
+
+
+def _paged_call(name, desc, cache, tensors, args, workspace, workspace_bytes, stream, check):
+    """One paged entry point: everything on the cache's device, and by default on that device's current stream."""
+    where = getattr(cache, "device", None)
+    dev = _device(workspace, *tensors)
+    if where is not None and dev is not None and dev != where:
+        raise ValueError("tensor arguments are on %s, the cache is on %s" % (dev, where))
+    dev = where if dev is None else dev
+    if dev is not None and dev.type != "cuda":
+        raise ValueError("tensor arguments are on %s, not on a GPU" % dev)
+    if cache is not None and where is not None and desc is not None:
+        if cache.rows != (desc.n_kv_heads, desc.head_dim) or \
+                str(cache.dtype) != ("torch.bfloat16" if desc.io_dtype == BEAGLE_BF16 else "torch.float32"):
+            raise ValueError("the cache holds rows %s of %s, not what the descriptor says" % (cache.rows, cache.dtype))
+
+    def call():
+        return getattr(lib(), name)(C.byref(desc) if desc is not None else None, C.byref(cache) if cache is not None else None, *args,
+                                    _ptr(workspace), _nbytes(workspace) if workspace_bytes is None else workspace_bytes,
+                                    _stream(stream))
+    if dev is not None:
+        import torch
+        if dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):
+                return _check(call(), name, check)
+    return _check(call(), name, check)
+
+
+def _view(desc, slots, n_true, tree_mask, mask_words, window, sinks):
+    B, M = desc.batch, desc.seq_q
+    return (_ints(slots, B), _ints(n_true, B), _ints(tree_mask, B * M * int(mask_words)), int(mask_words), int(window), int(sinks))
+
+
+def beagle_xattn_paged_workspace_bytes(desc, cache, which) -> int:
+    return int(lib().beagle_xattn_paged_workspace_bytes(C.byref(desc), C.byref(cache), int(which)))
+
+
+def beagle_xattn_paged_attend(desc, cache, q, slots, n_true, tree_mask, mask_words, window, sinks, o, lse, workspace, stream=None,
+                              *, workspace_bytes=None, check=True) -> int:
+    args = (_paged_rows(desc, q, desc.n_q_heads), *_view(desc, slots, n_true, tree_mask, mask_words, window, sinks),
+            _paged_rows(desc, o, desc.n_q_heads), _paged_lse(desc, lse))
+    return _paged_call("beagle_xattn_paged_attend", desc, cache, (q, slots, n_true, tree_mask, o, lse), args, workspace,
+                       workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_append(desc, cache, slots, pos, n_new, k_new, v_new, short_pages, workspace, stream=None, *,
+                              workspace_bytes=None, check=True) -> int:
+    B = desc.batch
+    args = (_ints(slots, B), _ints(pos, B), _ints(n_new, B), _paged_rows(desc, k_new, desc.n_kv_heads),
+            _paged_rows(desc, v_new, desc.n_kv_heads), _ints(short_pages, 1))
+    return _paged_call("beagle_xattn_paged_append", desc, cache, (slots, pos, n_new, k_new, v_new, short_pages), args, workspace,
+                       workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_fork(desc, cache, dst, src, rows, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    args = tuple(_ints(t, desc.batch) for t in (dst, src, rows))
+    return _paged_call("beagle_xattn_paged_fork", desc, cache, (dst, src, rows), args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_compact(desc, cache, into, short_pages, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    a, b = getattr(cache, "device", None), getattr(into, "device", None)
+    if a is not None and b is not None and (a != b or cache.rows != into.rows or cache.dtype != into.dtype):
+        raise ValueError("the two pools hold different rows, or are on different devices")
+    args = (C.byref(into) if into is not None else None, _ints(short_pages, 1))
+    return _paged_call("beagle_xattn_paged_compact", desc, cache, (short_pages,), args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_draft_step_paged(desc, cache, x_draft, wq, wo, slots, n_true, tree_mask, mask_words, window, sinks, y, lse,
+                                  workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    args = (_paged_rows(desc, x_draft, 0), _ptr(wq), _ptr(wo), *_view(desc, slots, n_true, tree_mask, mask_words, window, sinks),
+            _paged_rows(desc, y, 0), _paged_lse(desc, lse))
+    return _paged_call("beagle_xattn_draft_step_paged", desc, cache, (x_draft, wq, wo, slots, n_true, tree_mask, y, lse), args,
+                       workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_kv_append_paged(desc, cache, x_new, wk, wv, slots, pos, n_new, short_pages, workspace, stream=None, *,
+                                 workspace_bytes=None, check=True) -> int:
+    B = desc.batch
+    args = (_paged_rows(desc, x_new, 0), _ptr(wk), _ptr(wv), _ints(slots, B), _ints(pos, B), _ints(n_new, B), _ints(short_pages, 1))
+    return _paged_call("beagle_xattn_kv_append_paged", desc, cache, (x_new, wk, wv, slots, pos, n_new, short_pages), args, workspace,
+                       workspace_bytes, stream, check)
 
 
 def beagle_xattn_workspace_bytes(desc, which) -> int:

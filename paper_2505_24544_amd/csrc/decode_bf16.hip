@@ -1917,6 +1917,17 @@ void launch_kv_append_bf16(const void* x, const void* wk, const void* wv, void* 
   }
 }
 
+void launch_proj_rows_bf16(const void* x, const void* w, void* y, int32_t n, int32_t N, int32_t K, void* ws, const char* name, hipStream_t s) {
+  using namespace dec;
+  const int KS = (K + SG_K - 1) / SG_K;
+  const int64_t MN = (int64_t)n * N;
+  ProfScope ps(name, s);
+  hipLaunchKernelGGL(skinny_gemm_kernel<false>, dim3(N / SG_N, KS), dim3(256), 0, s, (const bf16_t*)x, (const bf16_t*)w, (float*)ws, n, N,
+                     K, CombineArgs{}, (const bf16_t*)nullptr, (float*)nullptr, 0, RopeRows{});
+  hipLaunchKernelGGL(sum_slices_kernel, dim3((unsigned)((MN / 4 + 255) / 256)), dim3(256), 0, s, (const float*)ws, (bf16_t*)y, MN, KS,
+                     (const float*)nullptr, (bf16_t*)nullptr, (const bf16_t*)nullptr);
+}
+
 
 // ---- feed-forward layer of the draft block for a handful of rows (decode time): HBM-bound on the three weight
 // matrices, so the same split-k streaming projection: [z W_gate, z W_up] in one launch (z = 0 / 1), the gate fused

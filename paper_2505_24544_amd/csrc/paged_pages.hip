@@ -1,0 +1,391 @@
+// What changes a paged cache: appending rows, forking sequences, moving the live pages into another pool.
+//
+// Everything is whole numbers and copies; a page is free where no slot's table names it (refs[p] == 0), and free pages are taken lowest
+// first in the order of the call's entries, so the outcome is a function of the cache's state and the arguments alone.
+// Reference counts change by integer atomics, whose order does not show.  Bound: the rows that are copied (HBM), and for
+// a few rows the chain of dependent trips to memory in the planning workgroup.
+#include "paged.h"
+
+namespace beagle {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+constexpr int PLAN = 1024;                 // threads of a planning workgroup
+constexpr int PLAN_WAVES = PLAN / 64;
+
+// counts that other waves of the launch have changed: past the vector cache
+__device__ __forceinline__ int load_count(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void add_count(int32_t* p, int v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool is_page(const PagedCache& c, int p) { return (unsigned)p < (unsigned)c.P; }
+// every thread's earlier stores and atomics are seen by the workgroup's later loads
+__device__ __forceinline__ void settle() { __threadfence(); __syncthreads(); }
+
+// Inclusive sum over the workgroup's threads in order; `all` gets the sum of everything.
+__device__ __forceinline__ int block_scan(int v, int* wave_sums, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int x = __shfl_up(v, m);
+    if (lane >= m) v += x;
+  }
+  __syncthreads();                         // (the sums of the call before have been read)
+  if (lane == 63) wave_sums[wave] = v;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+  for (int w = 0; w < PLAN_WAVES; ++w) {
+    const int x = wave_sums[w];
+    before += w < wave ? x : 0;
+    all += x;
+  }
+  return v + before;
+}
+
+// ------------------------------------------------------------------ append
+// What the plan tells the copying launch about an entry: rows pos .. pos + n - 1 of slot are new; page `from`, if any, held the
+// first pos % page_rows rows of the page that row pos stands in now.
+struct Entry { int32_t slot, pos, n, from; };
+struct AppendWs { Entry* entry; int32_t *upto, *taken; };       // [B], [B] pages wanted by the entries up to this one, [P]
+
+// pages that an entry keeps, and holds when all its rows are there
+struct Want { int slot, len, pos, n, keep, pages; bool room; };
+__device__ __forceinline__ Want want_of(const PagedAppendArgs& a, const int* owner, int b) {
+  Want w;
+  w.slot = paged_slot(a.c, a.slots, b);
+  if (w.slot >= 0 && owner[w.slot] != b) w.slot = -1;           // the slot's first entry counts
+  w.len = paged_len(a.c, w.slot);
+  w.pos = a.pos ? min(max(a.pos[b], 0), w.len) : w.len;
+  w.n = w.slot < 0 ? 0 : a.n_new ? min(max(a.n_new[b], 0), a.M) : a.M;
+  w.room = (int64_t)w.pos + w.n <= (int64_t)a.c.W << a.c.shift;
+  w.keep = paged_pages(w.pos, a.c.shift);
+  w.pages = w.room ? paged_pages(w.pos + w.n, a.c.shift) : w.keep;
+  return w;
+}
+
+// One workgroup: releases, then the pages that every entry wants, then the lowest free ones, handed out in order.
+__global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs a, AppendWs ws) {
+  __shared__ int owner[PAGED_MAX_BATCH];
+  __shared__ int wave_sums[PLAN_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, in_page = (1 << a.c.shift) - 1;
+  for (int s = tid; s < a.c.N; s += PLAN) owner[s] = INT32_MAX;
+  __syncthreads();
+  for (int b = tid; b < a.B; b += PLAN) {
+    const int s = paged_slot(a.c, a.slots, b);
+    if (s >= 0) atomicMin(&owner[s], b);
+  }
+  __syncthreads();
+  // pages behind the kept rows
+  for (int b = wave; b < a.B; b += PLAN_WAVES) {
+    const Want w = want_of(a, owner, b);
+    for (int i = w.keep + lane; i < paged_pages(w.len, a.c.shift); i += 64) {
+      const int p = a.c.table[(int64_t)w.slot * a.c.W + i];
+      if (is_page(a.c, p)) add_count(a.c.refs + p, -1);
+    }
+  }
+  settle();
+  // pages wanted; a page that is kept in part and shared is copied into one of its own
+  int wanted = 0, lacking = 0;
+  for (int b0 = 0; b0 < a.B; b0 += PLAN) {
+    const int b = b0 + tid;
+    int need = 0, over = 0;
+    if (b < a.B) {
+      const Want w = want_of(a, owner, b);
+      int from = -1;
+      if (w.n > 0 && w.room && (w.pos & in_page)) {
+        const int p = a.c.table[(int64_t)w.slot * a.c.W + w.keep - 1];
+        if (!is_page(a.c, p)) from = -2;                        // (a page that is none: the rows go into a fresh one)
+        else if (load_count(a.c.refs + p) > 1) from = p;
+      }
+      need = w.pages - w.keep + (from != -1);
+      over = w.room ? 0 : (int)(((int64_t)w.pos + w.n - ((int64_t)a.c.W << a.c.shift) + in_page) >> a.c.shift);
+      ws.entry[b] = Entry{w.slot, w.pos, w.room ? w.n : 0, from};
+    }
+    int all, none;
+    const int upto = wanted + block_scan(need, wave_sums, all);
+    if (b < a.B) ws.upto[b] = upto;
+    wanted += all;
+    block_scan(over, wave_sums, none);
+    lacking += none;
+  }
+  // the lowest free pages
+  int found = 0;
+  for (int64_t p0 = 0; p0 < a.c.P && found < wanted; p0 += 4 * PLAN) {
+    const int64_t p = p0 + 4 * tid;
+    int n = 0, is_free[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      is_free[i] = p + i < a.c.P && load_count(a.c.refs + p + i) <= 0;
+      n += is_free[i];
+    }
+    int all, at = block_scan(n, wave_sums, all) - n + found;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (is_free[i]) ws.taken[at++] = (int32_t)(p + i);
+    found += all;
+  }
+  settle();
+  if (tid == 0 && a.short_pages) a.short_pages[0] = max(wanted - found, 0) + lacking;
+  for (int b = wave; b < a.B; b += PLAN_WAVES) {
+    const Entry e = ws.entry[b];
+    if (e.slot < 0) continue;
+    const int upto = ws.upto[b], keep = paged_pages(e.pos, a.c.shift), pages = paged_pages(e.pos + e.n, a.c.shift);
+    const int own = e.from != -1, need = pages - keep + own;
+    int32_t* row = a.c.table + (int64_t)e.slot * a.c.W;
+    if (need && upto > found) {                                 // not enough pages: the entry keeps its first rows
+      if (lane == 0) { ws.entry[b].n = 0; ws.entry[b].from = -1; a.c.lens[e.slot] = e.pos; }
+      continue;
+    }
+    for (int i = lane; i < need; i += 64) {
+      const int p = ws.taken[upto - need + i];
+      row[keep - own + i] = p;
+      __hip_atomic_store(a.c.refs + p, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (lane == 0) {
+      if (e.from >= 0) add_count(a.c.refs + e.from, -1);
+      a.c.lens[e.slot] = e.pos + e.n;
+    }
+  }
+}
+
+constexpr int STORE_ROWS = 4;              // rows of a workgroup of the copying launch
+
+// New rows (blockIdx.x < new_blocks) and the kept rows of copied pages.  K rows are rotated on the way: the angles of a workgroup's rows
+// are evaluated once, in LDS, and serve all heads.
+template <bool BF16>
+__global__ __launch_bounds__(256) void paged_append_store_kernel(PagedAppendArgs a, AppendWs ws, int new_blocks) {
+  constexpr int E = BF16 ? 2 : 4, PIECE = BF16 ? 8 : 2;        // bytes and values of a thread's access
+  __shared__ float2 cs[STORE_ROWS][64];
+  const int b = blockIdx.y, tid = threadIdx.x, in_page = (1 << a.c.shift) - 1;
+  const Entry e = ws.entry[b];
+  const bool fresh = (int)blockIdx.x < new_blocks;
+  const int r0 = (fresh ? blockIdx.x : blockIdx.x - new_blocks) * STORE_ROWS;
+  const int rows = fresh ? e.n : e.from >= 0 ? e.pos & in_page : 0;
+  if (r0 >= rows) return;
+  const int here = min(STORE_ROWS, rows - r0);
+  const int64_t row_bytes = (int64_t)a.G * a.d * E;
+  const int32_t* table = a.c.table + (int64_t)e.slot * a.c.W;
+  if (!fresh) {
+    const int64_t to = (((int64_t)table[e.pos >> a.c.shift] << a.c.shift) + r0) * row_bytes;
+    const int64_t from = (((int64_t)e.from << a.c.shift) + r0) * row_bytes;
+    for (int64_t i = (int64_t)tid * 16; i < here * row_bytes; i += 256 * 16) {
+      *(u32x4*)((char*)a.c.k + to + i) = *(const u32x4*)((const char*)a.c.k + from + i);
+      *(u32x4*)((char*)a.c.v + to + i) = *(const u32x4*)((const char*)a.c.v + from + i);
+    }
+    return;
+  }
+  const int half = a.d >> 1;
+  if (a.rope) {
+    for (int i = tid; i < here * 64; i += 256) {
+      const int r = i >> 6, c = i & 63;
+      if (c < half) cs[r][c] = rope_cos_sin(a.rope_pos ? a.rope_pos[(int64_t)b * a.M + r0 + r] : e.pos + r0 + r, c, a.d, a.l2base);
+    }
+    __syncthreads();
+  }
+  typedef unsigned int piece_t __attribute__((ext_vector_type(PIECE * E / 4)));
+  const int per_head = half / PIECE, per_row = a.G * per_head;   // (d is a multiple of 4; bf16: 128)
+  for (int i = tid; i < here * per_row; i += 256) {
+    const int r = i / per_row, head = i % per_row / per_head, c = i % per_head * PIECE;
+    const int row = e.pos + r0 + r;
+    const int64_t src = ((int64_t)b * a.M + r0 + r) * row_bytes + ((int64_t)head * a.d + c) * E;
+    const int64_t dst = (((int64_t)table[row >> a.c.shift] << a.c.shift) + (row & in_page)) * row_bytes + ((int64_t)head * a.d + c) * E;
+    piece_t x = *(const piece_t*)((const char*)a.k_new + src), y = *(const piece_t*)((const char*)a.k_new + src + half * E);
+    const piece_t v0 = *(const piece_t*)((const char*)a.v_new + src), v1 = *(const piece_t*)((const char*)a.v_new + src + half * E);
+    if (a.rope) {
+      if constexpr (BF16) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 t = cs[r][c + 2 * j], u = cs[r][c + 2 * j + 1];
+          const float x0 = __uint_as_float(x[j] << 16), x1 = __uint_as_float(x[j] & 0xffff0000u);
+          const float y0 = __uint_as_float(y[j] << 16), y1 = __uint_as_float(y[j] & 0xffff0000u);
+          x[j] = pack_bf16x2(x0 * t.x - y0 * t.y, x1 * u.x - y1 * u.y);
+          y[j] = pack_bf16x2(y0 * t.x + x0 * t.y, y1 * u.x + x1 * u.y);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 t = cs[r][c + j];
+          const float x0 = __uint_as_float(x[j]), y0 = __uint_as_float(y[j]);
+          x[j] = __float_as_uint(x0 * t.x - y0 * t.y);
+          y[j] = __float_as_uint(y0 * t.x + x0 * t.y);
+        }
+      }
+    }
+    *(piece_t*)((char*)a.c.k + dst) = x;
+    *(piece_t*)((char*)a.c.k + dst + half * E) = y;
+    *(piece_t*)((char*)a.c.v + dst) = v0;
+    *(piece_t*)((char*)a.c.v + dst + half * E) = v1;
+  }
+}
+
+// ------------------------------------------------------------------ fork
+// Sources are read in one launch and targets changed in the next: a slot may be both.
+struct ForkWs { int32_t *rows, *pages; };  // [B] rows that the target takes (-1: the entry does not count), [B, W] their pages
+
+__global__ __launch_bounds__(256) void paged_fork_read_kernel(PagedCache c, const int32_t* dst, const int32_t* src, const int32_t* rows, ForkWs ws) {
+  __shared__ int again;
+  const int b = blockIdx.x, tid = threadIdx.x, to = dst[b], from = src[b];
+  if (tid == 0) again = 0;
+  __syncthreads();
+  if ((unsigned)to < (unsigned)c.N)
+    for (int i = tid; i < b; i += 256)
+      if (dst[i] == to) again = 1;         // the target's first entry counts
+  __syncthreads();
+  const bool counts = (unsigned)to < (unsigned)c.N && !again;
+  const int slot = (unsigned)from < (unsigned)c.N ? from : -1, len = paged_len(c, slot);
+  const int n = rows ? min(max(rows[b], 0), len) : len;
+  if (tid == 0) ws.rows[b] = counts ? n : -1;
+  if (!counts) return;
+  for (int i = tid; i < paged_pages(n, c.shift); i += 256) ws.pages[(int64_t)b * c.W + i] = c.table[(int64_t)slot * c.W + i];
+}
+
+__global__ __launch_bounds__(256) void paged_fork_write_kernel(PagedCache c, const int32_t* dst, ForkWs ws) {
+  const int b = blockIdx.x, tid = threadIdx.x, n = ws.rows[b];
+  if (n < 0) return;
+  const int to = dst[b], had = paged_pages(paged_len(c, to), c.shift), has = paged_pages(n, c.shift);
+  int32_t* row = c.table + (int64_t)to * c.W;
+  for (int i = tid; i < c.W; i += 256) {
+    const int old = i < had ? row[i] : -1, now = i < has ? ws.pages[(int64_t)b * c.W + i] : -1;
+    row[i] = now;
+    if (old == now) continue;
+    if (is_page(c, old)) add_count(c.refs + old, -1);
+    if (is_page(c, now)) add_count(c.refs + now, 1);
+  }
+  __syncthreads();                         // (everyone has read the old length)
+  if (tid == 0) c.lens[to] = n;
+}
+
+// ------------------------------------------------------------------ compact
+struct CompactWs { int32_t *number, *live, *count; };   // [P] new number of a live page, [P] live pages in order, [1] how many move
+
+// Workgroup 0 numbers the live pages; the others clear the target's counts.
+__global__ __launch_bounds__(PLAN) void paged_number_kernel(PagedCache from, PagedCache into, int32_t* short_pages, CompactWs ws) {
+  __shared__ int wave_sums[PLAN_WAVES];
+  const int tid = threadIdx.x;
+  if (blockIdx.x) {
+    for (int64_t p = (int64_t)(blockIdx.x - 1) * PLAN + tid; p < into.P; p += (int64_t)(gridDim.x - 1) * PLAN) into.refs[p] = 0;
+    return;
+  }
+  int found = 0;
+  for (int64_t p0 = 0; p0 < from.P; p0 += 4 * PLAN) {
+    const int64_t p = p0 + 4 * tid;
+    int n = 0, held[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      held[i] = p + i < from.P && from.refs[p + i] > 0;
+      n += held[i];
+    }
+    int all, at = block_scan(n, wave_sums, all) - n + found;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < from.P) {
+        ws.number[p + i] = held[i] ? at : -1;
+        if (held[i]) ws.live[at++] = (int32_t)(p + i);
+      }
+    found += all;
+  }
+  if (tid == 0) {
+    ws.count[0] = min(found, into.P);
+    if (short_pages) short_pages[0] = max(found - into.P, 0);
+  }
+}
+
+// Workgroups 0 .. N - 1 rewrite a slot's table (its rows end before the first page that did not move); the others copy pages.
+__global__ __launch_bounds__(256) void paged_move_kernel(PagedCache from, PagedCache into, int64_t page_bytes, CompactWs ws) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < from.N) {
+    __shared__ int stop;
+    const int s = blockIdx.x, len = paged_len(from, s), pages = paged_pages(len, from.shift);
+    if (tid == 0) stop = min(pages, into.W);
+    __syncthreads();
+    auto number = [&](int i) {
+      const int p = from.table[(int64_t)s * from.W + i], q = is_page(from, p) ? ws.number[p] : -1;
+      return (unsigned)q < (unsigned)into.P ? q : -1;
+    };
+    for (int i = tid; i < pages; i += 256)
+      if (number(i) < 0) atomicMin(&stop, i);
+    __syncthreads();
+    for (int i = tid; i < into.W; i += 256) {
+      const int q = i < stop ? number(i) : -1;
+      into.table[(int64_t)s * into.W + i] = q;
+      if (q >= 0) add_count(into.refs + q, 1);
+    }
+    if (tid == 0) into.lens[s] = min((int64_t)len, (int64_t)stop << from.shift);
+    return;
+  }
+  const int64_t pieces = page_bytes / 16, all = 2 * pieces * ws.count[0], step = (int64_t)(gridDim.x - from.N) * 256;
+  for (int64_t i = (int64_t)(blockIdx.x - from.N) * 256 + tid; i < all; i += step) {
+    const int64_t unit = i / pieces, piece = i - unit * pieces, to = unit >> 1;
+    const int64_t src = (int64_t)ws.live[to] * pieces + piece, dst = to * pieces + piece;
+    if (unit & 1) ((u32x4*)into.v)[dst] = ((const u32x4*)from.v)[src];
+    else ((u32x4*)into.k)[dst] = ((const u32x4*)from.k)[src];
+  }
+}
+
+// where the queries of a draft step stand when the caller does not say: behind the rows that their sequence holds
+__global__ __launch_bounds__(256) void paged_positions_kernel(PagedCache c, const int32_t* slots, int B, int M, int32_t* pos) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < B * M) pos[i] = paged_len(c, paged_slot(c, slots, i / M));
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t paged_append_ws_bytes(const PagedCache& c, int32_t B) {
+  return up256((size_t)B * sizeof(Entry)) + up256((size_t)B * 4) + up256((size_t)c.P * 4);
+}
+void launch_paged_append(bool bf16, const PagedAppendArgs& a, void* ws, hipStream_t s) {
+  AppendWs w;
+  char* base = (char*)ws;
+  w.entry = (Entry*)base; base += up256((size_t)a.B * sizeof(Entry));
+  w.upto = (int32_t*)base; base += up256((size_t)a.B * 4);
+  w.taken = (int32_t*)base;
+  {
+    ProfScope ps("paged_append_plan", s);
+    hipLaunchKernelGGL(paged_append_plan_kernel, dim3(1), dim3(PLAN), 0, s, a, w);
+  }
+  const int new_blocks = (a.M + STORE_ROWS - 1) / STORE_ROWS;
+  const int copy_blocks = ((1 << a.c.shift) - 1 + STORE_ROWS - 1) / STORE_ROWS;
+  ProfScope ps("paged_append_store", s);
+  const dim3 grid((unsigned)(new_blocks + copy_blocks), (unsigned)a.B);
+  if (bf16) hipLaunchKernelGGL(paged_append_store_kernel<true>, grid, dim3(256), 0, s, a, w, new_blocks);
+  else hipLaunchKernelGGL(paged_append_store_kernel<false>, grid, dim3(256), 0, s, a, w, new_blocks);
+}
+
+void launch_paged_positions(const PagedCache& c, const int32_t* slots, int32_t B, int32_t M, int32_t* pos, hipStream_t s) {
+  ProfScope ps("paged_positions", s);
+  hipLaunchKernelGGL(paged_positions_kernel, dim3((unsigned)((B * M + 255) / 256)), dim3(256), 0, s, c, slots, B, M, pos);
+}
+
+size_t paged_fork_ws_bytes(const PagedCache& c, int32_t B) { return up256((size_t)B * 4) + up256((size_t)B * c.W * 4); }
+void launch_paged_fork(const PagedCache& c, const int32_t* dst, const int32_t* src, const int32_t* rows, int32_t B, void* ws,
+                       hipStream_t s) {
+  ForkWs w;
+  w.rows = (int32_t*)ws;
+  w.pages = (int32_t*)((char*)ws + up256((size_t)B * 4));
+  {
+    ProfScope ps("paged_fork_read", s);
+    hipLaunchKernelGGL(paged_fork_read_kernel, dim3((unsigned)B), dim3(256), 0, s, c, dst, src, rows, w);
+  }
+  ProfScope ps("paged_fork_write", s);
+  hipLaunchKernelGGL(paged_fork_write_kernel, dim3((unsigned)B), dim3(256), 0, s, c, dst, w);
+}
+
+size_t paged_compact_ws_bytes(const PagedCache& c) { return 2 * up256((size_t)c.P * 4) + 256; }
+void launch_paged_compact(const PagedCache& from, const PagedCache& into, int64_t page_bytes, int32_t* short_pages, void* ws,
+                          hipStream_t s) {
+  CompactWs w;
+  w.number = (int32_t*)ws;
+  w.live = (int32_t*)((char*)ws + up256((size_t)from.P * 4));
+  w.count = (int32_t*)((char*)ws + 2 * up256((size_t)from.P * 4));
+  {
+    ProfScope ps("paged_number", s);
+    hipLaunchKernelGGL(paged_number_kernel, dim3(1 + 64), dim3(PLAN), 0, s, from, into, short_pages, w);
+  }
+  ProfScope ps("paged_move", s);
+  const int64_t most = 2 * (page_bytes / 16) * (from.P < into.P ? from.P : into.P);
+  const int64_t blocks = (most + 255) / 256 < 2048 ? (most + 255) / 256 : 2048;
+  hipLaunchKernelGGL(paged_move_kernel, dim3((unsigned)(from.N + blocks)), dim3(256), 0, s, from, into, page_bytes, w);
+}
+
+}  // namespace beagle

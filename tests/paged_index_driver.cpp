@@ -1,0 +1,49 @@
+// Host build of the paged cache's index code, under sanitizers.  Reads lines of whole numbers, prints what the code says:
+//   rows n nt window sinks   -> number of blocks, then for every row 0 .. n + 40: counted blocks that hold it * 4 + seen * 2 + (its block of 32 is all seen)
+//   units target least len.. -> chunk, then the units of every entry
+//   page n_pages shift row seen entry.. -> the page
+//   slot s n_slots len slot_pages shift -> slot, clamped length, its pages
+#include <cstdio>
+#include <iostream>
+#include <sstream>
+#include <string>
+#include <vector>
+#include "../paper_2505_24544_amd/csrc/paged_index.h"
+using namespace beagle;
+
+int main() {
+  std::string line;
+  while (std::getline(std::cin, line)) {
+    std::istringstream in(line);
+    std::string what;
+    in >> what;
+    std::vector<long long> x;
+    for (long long v; in >> v;) x.push_back(v);
+    if (what == "rows") {
+      const PagedRows r = paged_rows((int)x[0], (int)x[1], (int)x[2], (int)x[3]);
+      std::printf("%d", r.blocks);
+      if (x[0] <= 4096) {
+        std::vector<int> hold(x[0] + 96, 0);
+        for (int i = 0; i < r.blocks; ++i)
+          for (int j = 0; j < PAGED_BLOCK; ++j) hold.at(paged_block(r, i) * PAGED_BLOCK + j) += 1;
+        for (int row = 0; row < x[0] + 40; ++row)
+          std::printf(" %d", hold.at(row) * 4 + paged_seen(r, row) * 2 + paged_all_seen(r, row / 32 * 32, 32));
+      }
+      std::printf("\n");
+    } else if (what == "units") {
+      long long all = 0;
+      for (size_t i = 2; i < x.size(); ++i) all += (x[i] + PAGED_BLOCK - 1) / PAGED_BLOCK;
+      const int chunk = paged_chunk(all, (int)x[0], (int)x[1]);
+      std::printf("%d", chunk);
+      for (size_t i = 2; i < x.size(); ++i) std::printf(" %d", paged_units((int)((x[i] + PAGED_BLOCK - 1) / PAGED_BLOCK), chunk));
+      std::printf("\n");
+    } else if (what == "page") {
+      std::vector<int32_t> table(x.begin() + 4, x.end());
+      std::printf("%d\n", paged_page(table.data(), (int)x[2], x[3] != 0, (int)x[1], (int)x[0]));
+    } else {
+      const int s = paged_slot_of((int)x[0], (int)x[1]), len = paged_clamped((int)x[2], (int)x[3], (int)x[4]);
+      std::printf("%d %d %d\n", s, len, paged_pages(len, (int)x[4]));
+    }
+  }
+  return 0;
+}
