@@ -47,7 +47,7 @@ __device__ Unit find_unit(const PagedAttnArgs& a, int which, bool want_entry) {
     int blocks = b < a.B ? rows_of(a, paged_slot(a.c, a.slots, b), b).blocks : 0;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) blocks += __shfl_xor(blocks, m);       // (64 entries of 2^23 blocks: fits)
-    total += blocks;
+    total += __builtin_amdgcn_readfirstlane(blocks);
   }
   Unit u;
   u.chunk = paged_chunk(total, a.target, a.least);
@@ -67,21 +67,25 @@ __device__ Unit find_unit(const PagedAttnArgs& a, int which, bool want_entry) {
     const unsigned long long at = __ballot(hit);
     if (at) {
       const int l = __ffsll((long long)at) - 1;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       u.b = b0 + l;
-      u.units = __shfl(mine, l);
-      u.i = want_entry ? 0 : which - base - (__shfl(upto, l) - u.units);
-      u.first = parts + __shfl(pupto, l) - (u.units > 1 ? u.units : 0);
+      u.units = of(mine);
+      u.i = want_entry ? 0 : which - base - (of(upto) - u.units);
+      u.first = parts + of(pupto) - of(kept);
       return u;
     }
-    base += __shfl(upto, 63);
-    parts += __shfl(pupto, 63);
+    base += __builtin_amdgcn_readlane(upto, 63);
+    parts += __builtin_amdgcn_readlane(pupto, 63);
   }
   return u;
 }
 
+// over the four lanes that hold a column's keys
 __device__ __forceinline__ float max_over_keys(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
@@ -105,15 +109,17 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
   constexpr int E = BF16 ? 2 : 4, HDP = BF16 ? 128 : 64 * NH;       // bytes of a value; padded head width
   __shared__ float part_o[WAVES][16][HDP + 4];
   __shared__ float part_m[WAVES][RT * 16], part_l[WAVES][RT * 16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
   // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
   const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
   if (ug >= heads8) return;
   const int head = ug % a.G;
   const Unit u = find_unit(a, ug / a.G, false);
   if (u.b < 0) return;
-  const int slot = paged_slot(a.c, a.slots, u.b);
-  const PagedRows rows = rows_of(a, slot, u.b);
+  const int slot = __builtin_amdgcn_readfirstlane(paged_slot(a.c, a.slots, u.b));
+  PagedRows rows = rows_of(a, slot, u.b);
+  rows.n = __builtin_amdgcn_readfirstlane(rows.n); rows.nt = __builtin_amdgcn_readfirstlane(rows.nt);
+  rows = paged_rows(rows.n, rows.nt, a.window, a.sinks);               // (the wave's, not a lane's)
   const int rep = a.H / a.G, R = a.M * rep;
   const int first = u.i * u.chunk, last = min(first + u.chunk, rows.blocks);
   const int64_t row_bytes = (int64_t)a.G * a.d * E;
@@ -144,161 +150,236 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
     for (int c = 0; c < S::NA; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float c2 = a.scale * LOG2E;
+  const float c2 = fmaxf(a.scale * LOG2E, 1.1754944e-38f);           // (0 * -infinity is no number)
 
-  auto page_of = [&](int row) { return paged_page(table, row, paged_seen(rows, row), a.c.shift, a.c.P); };
-  for (int vb = first + wave; vb < last; vb += WAVES) {
-    const int block = paged_block(rows, vb);
+  // ---- the steps of this wave: KROWS rows each, of every WAVES-th block of the unit
+  constexpr int SUB = PAGED_BLOCK / S::KROWS;
+  const int steps = last > first + wave ? (last - first - wave + WAVES - 1) / WAVES * SUB : 0;
+  const int shift = a.c.shift;
+  const bool wide = shift >= 4;            // 16 rows of a score tile stand on one page: its number is the wave's, not a lane's
+  auto base_of = [&](int s) { return paged_block(rows, first + wave + s / SUB * WAVES) * PAGED_BLOCK + s % SUB * S::KROWS; };
+  auto page_of = [&](int row) { return paged_page(table, row, paged_seen(rows, row), shift, a.c.P); };
+  // page numbers of a step, a step ahead of the rows: of the tiles, if they stand on one page each
+  struct Ahead { int base, whole; int page[S::KT]; };
+  auto look = [&](int s) BEAGLE_INLINE_LAMBDA {
+    Ahead h;
+    h.base = __builtin_amdgcn_readfirstlane(s < steps ? base_of(s) : rows.n);
+    h.whole = wide && paged_all_seen(rows, h.base, S::KROWS);
 #pragma unroll
-    for (int sub = 0; sub < PAGED_BLOCK / S::KROWS; ++sub) {
-      const int base = block * PAGED_BLOCK + sub * S::KROWS;
-      if (base >= rows.n) break;
-      // ---- K rows, one in each lane's l16; V rows, four neighbours (one page: its rows are a multiple of four)
-      u32x4 k[S::KT][S::NJ], v[S::NV][NH];
+    for (int t = 0; t < S::KT; ++t) h.page[t] = h.whole ? table[(h.base + 16 * t) >> shift] : 0;
+    return h;
+  };
+  // (an unreadable page number: the step goes row by row)
+  auto settle = [&](Ahead& h) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
-      for (int t = 0; t < S::KT; ++t) {
-        const int row = base + 16 * t + l16, p = page_of(row);
-        const char* src = p >= 0 ? kbase + (((int64_t)p << a.c.shift) + (row & in_page)) * row_bytes : (const char*)zero_row;
+    for (int t = 0; t < S::KT; ++t) {
+      h.page[t] = __builtin_amdgcn_readfirstlane(h.page[t]);
+      if ((unsigned)h.page[t] >= (unsigned)a.c.P) h.whole = 0;
+    }
+  };
+  uint32_t koff[S::NJ], voff[4][NH];       // of a lane's pieces, from the first row of a tile
+#pragma unroll
+  for (int j = 0; j < S::NJ; ++j) koff[j] = (uint32_t)(l16 * row_bytes) + (4 * j + g4) * 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < NH; ++h) voff[i][h] = (uint32_t)((4 * g4 + i) * row_bytes) + (16 * h + l16) * 16;
+  u32x4 k[S::KT][S::NJ], v[S::NV][NH];
+  // K rows, one in each lane's l16
+  auto request_k = [&](const Ahead& h) BEAGLE_INLINE_LAMBDA {
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) {
+      if (h.whole) {
+        const char* src = kbase + (((int64_t)h.page[t] << shift) + ((h.base + 16 * t) & in_page)) * row_bytes;
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j)
+          k[t][j] = BF16 || (4 * j + g4) * 16 < a.d * E ? *(const u32x4*)(src + koff[j]) : u32x4{0, 0, 0, 0};
+      } else {
+        const int row = h.base + 16 * t + l16, p = page_of(row);
+        const char* src = p >= 0 ? kbase + (((int64_t)p << shift) + (row & in_page)) * row_bytes : (const char*)zero_row;
 #pragma unroll
         for (int j = 0; j < S::NJ; ++j) {
           const int piece = (4 * j + g4) * 16;
           k[t][j] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
         }
       }
-      bool seen[S::KT][4];
+    }
+  };
+  // V rows, four neighbours in each lane's g4 (one page: its rows are a multiple of four)
+  auto request_v = [&](const Ahead& h) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
-      for (int t = 0; t < S::KT; ++t) {
-        const int r0 = base + 16 * t + 4 * g4;
-        // (a page number that is not one hides its rows)
-        const int p = paged_page(table, r0, r0 < rows.n, a.c.shift, a.c.P);
+    for (int t = 0; t < S::KT; ++t) {
+      if (h.whole) {
+        const char* src = vbase + (((int64_t)h.page[t] << shift) + ((h.base + 16 * t) & in_page)) * row_bytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int n = 0; n < NH; ++n)
+            v[4 * t + i][n] = BF16 || (16 * n + l16) * 16 < a.d * E ? *(const u32x4*)(src + voff[i][n]) : u32x4{0, 0, 0, 0};
+      } else {
+        const int r0 = h.base + 16 * t + 4 * g4, p = paged_page(table, r0, r0 < rows.n, shift, a.c.P);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          seen[t][i] = p >= 0 && paged_seen(rows, r0 + i);
-          const char* src = seen[t][i] ? vbase + (((int64_t)p << a.c.shift) + ((r0 + i) & in_page)) * row_bytes : (const char*)zero_row;
+          const bool seen = p >= 0 && paged_seen(rows, r0 + i);
+          const char* src = seen ? vbase + (((int64_t)p << shift) + ((r0 + i) & in_page)) * row_bytes : (const char*)zero_row;
 #pragma unroll
-          for (int h = 0; h < NH; ++h) {
-            const int piece = (16 * h + l16) * 16;
-            v[4 * t + i][h] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
+          for (int n = 0; n < NH; ++n) {
+            const int piece = (16 * n + l16) * 16;
+            v[4 * t + i][n] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
           }
         }
       }
-      // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
-      // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
-      [[maybe_unused]] bool odd = false;
-      if constexpr (TREE)
-        if (base + S::KROWS > rows.nt) {
-          unsigned top = 0;
+    }
+  };
+  Ahead now = look(0), next = look(1);
+  settle(now);
+  if (steps > 0) { request_k(now); request_v(now); }
+  for (int s = 0; s < steps; ++s) {
+    // ---- scores
+    f32x4 sc[RT][S::KT];
 #pragma unroll
-          for (int i = 0; i < S::NV; ++i)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int h = 0; h < NH; ++h)
+      for (int kt = 0; kt < S::KT; ++kt) {
+        sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const unsigned x = v[i][h][e];
-                top = max(top, x & 0x7f800000u);
-                if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
-              }
-          odd = __ballot(top == 0x7f800000u) != 0;
+        for (int j = 0; j < S::NJ; ++j) {
+          if constexpr (BF16) sc[t][kt] = mfma_bf16(k[kt][j], q[t][j], sc[t][kt]);
+          else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[t][kt] = mfma_f32(__uint_as_float(k[kt][j][e]), __uint_as_float(q[t][j][e]), sc[t][kt]);
         }
+      }
+    // the registers of K are free: the next step's rows travel while this one's probabilities are computed
+    settle(next);
+    if (s + 1 < steps) request_k(next);
+    const Ahead after = look(s + 2);
+    bool seen[S::KT][4];
+    if (!now.whole) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        // ---- scores
-        f32x4 s[S::KT];
+      for (int kt = 0; kt < S::KT; ++kt) {
+        const int r0 = now.base + 16 * kt + 4 * g4;
+        const bool there = paged_page(table, r0, r0 < rows.n, shift, a.c.P) >= 0;      // (a page number that is none hides its rows)
 #pragma unroll
-        for (int kt = 0; kt < S::KT; ++kt) {
-          s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) seen[kt][i] = there && paged_seen(rows, r0 + i);
+      }
+    }
+    // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
+    // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
+    [[maybe_unused]] bool odd = false;
+    if constexpr (TREE)
+      if (now.base + S::KROWS > rows.nt) {
+        unsigned top = 0;
 #pragma unroll
-          for (int j = 0; j < S::NJ; ++j) {
-            if constexpr (BF16) s[kt] = mfma_bf16(k[kt][j], q[t][j], s[kt]);
-            else
+        for (int i = 0; i < S::NV; ++i)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s[kt] = mfma_f32(__uint_as_float(k[kt][j][e]), __uint_as_float(q[t][j][e]), s[kt]);
-          }
-        }
-        float top = -INFINITY;
-        [[maybe_unused]] bool saw[S::KT][4];
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned x = v[i][h][e];
+              top = max(top, x & 0x7f800000u);
+              if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
+            }
+        odd = __ballot(top == 0x7f800000u) != 0;
+      }
+    // ---- running maximum and sum, probabilities
+    float p[RT][S::KT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (!now.whole) {
 #pragma unroll
         for (int kt = 0; kt < S::KT; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             bool see = seen[kt][i];
             if constexpr (TREE) {
-              const int bit = base + 16 * kt + 4 * g4 + i - rows.nt;
+              const int bit = now.base + 16 * kt + 4 * g4 + i - rows.nt;
               if (see && bit >= 0)
                 see = qm[t] < a.M && (bit >> 5) < a.words &&
                       (a.tree[((int64_t)u.b * a.M + qm[t]) * a.words + (bit >> 5)] >> (bit & 31) & 1u);
             }
-            s[kt][i] = see ? s[kt][i] * c2 : -INFINITY;
-            if constexpr (TREE) saw[kt][i] = see;
-            top = fmaxf(top, s[kt][i]);
+            if (!see) sc[t][kt][i] = -INFINITY;
           }
-        // ---- running maximum and sum
-        const float now = fmaxf(mx[t], max_over_keys(top)), safe = now == -INFINITY ? 0.f : now;
+      }
+      float top = sc[t][0][0];
+#pragma unroll
+      for (int e = 1; e < 4 * S::KT; ++e) top = fmaxf(top, sc[t][e / 4][e % 4]);
+      const float most = fmaxf(mx[t], max_over_keys(top) * c2), safe = most == -INFINITY ? 0.f : most;
+      if (__any(most > mx[t])) {
         const float shrink = exp2_fast(mx[t] - safe);
-        mx[t] = now;
-        float p[S::KT][4], add = 0.f;
+        sum[t] *= shrink;
+#pragma unroll
+        for (int c = 0; c < S::NA; ++c) acc[t][c] *= shrink;
+        mx[t] = most;
+      }
+#pragma unroll
+      for (int kt = 0; kt < S::KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p[t][kt][i] = exp2_fast(fmaf(sc[t][kt][i], c2, -safe)); sum[t] += p[t][kt][i]; }
+    }
+    // ---- O^T += V^T P^T
+    if (TREE && odd) {
+      float* mine = part_o[wave][l16];       // (free until the end)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
 #pragma unroll
         for (int kt = 0; kt < S::KT; ++kt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { p[kt][i] = exp2_fast(s[kt][i] - safe); add += p[kt][i]; }
-        sum[t] = sum[t] * shrink + add;
+          for (int i = 0; i < 4; ++i) mine[16 * kt + 4 * g4 + i] = sc[t][kt][i] == -INFINITY ? -1.f : p[t][kt][i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int j = 0; j < S::KROWS; ++j) {
+          const float w = mine[j];
+          const int row = now.base + j, pg = page_of(row);
+          if (w == -1.f || pg < 0) continue;
+          const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
 #pragma unroll
-        for (int c = 0; c < S::NA; ++c) acc[t][c] *= shrink;
-        // ---- O^T += V^T P^T
-        if constexpr (TREE) if (odd) {
-          float* mine = part_o[wave][l16];       // (free until the end)
+          for (int c = 0; c < S::NA; ++c)
 #pragma unroll
-          for (int kt = 0; kt < S::KT; ++kt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[16 * kt + 4 * g4 + i] = saw[kt][i] ? p[kt][i] : -1.f;
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          for (int j = 0; j < S::KROWS; ++j) {
-            const float w = mine[j];
-            const int row = base + j, pg = page_of(row);
-            if (w == -1.f || pg < 0) continue;
-            const char* src = vbase + (((int64_t)pg << a.c.shift) + (row & in_page)) * row_bytes;
-#pragma unroll
-            for (int c = 0; c < S::NA; ++c)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
-                if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
-                else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
-              }
-          }
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          continue;
+            for (int i = 0; i < 4; ++i) {
+              const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
+              if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
+              else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
+            }
         }
-        if constexpr (BF16) {
-          // a probability as two bf16 numbers, 16 bits in all: the matrix pipe has the time, and the rounding of one
-          // would cost the output as much again as its own (2^-9)
-          u32x4 hi, lo;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+    } else if constexpr (BF16) {
+      // a probability as two bf16 numbers, 16 bits in all: the matrix pipe has the time, and the rounding of one
+      // would cost the output as much again as its own (2^-9)
+      u32x4 hi[RT], lo[RT];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = p[i >> 1][2 * (i & 1)], y = p[i >> 1][2 * (i & 1) + 1];
-            hi[i] = pack_bf16x2(x, y);
-            lo[i] = pack_bf16x2(x - __uint_as_float(hi[i] << 16), y - __uint_as_float(hi[i] & 0xffff0000u));
-          }
+      for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {       // channels 8 l16 + c
-            u32x4 w;
+        for (int i = 0; i < 4; ++i) {
+          const float x = p[t][i >> 1][2 * (i & 1)], y = p[t][i >> 1][2 * (i & 1) + 1];
+          hi[t][i] = pack_bf16x2(x, y);
+          lo[t][i] = pack_bf16x2(x - __uint_as_float(hi[t][i] << 16), y - __uint_as_float(hi[t][i] & 0xffff0000u));
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = __builtin_amdgcn_perm(v[2 * i + 1][0][c >> 1], v[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-            acc[t][c] = mfma_bf16(w, hi, acc[t][c]);
-            acc[t][c] = mfma_bf16(w, lo, acc[t][c]);
-          }
-        } else {
+      for (int c = 0; c < 8; ++c) {       // channels 8 l16 + c
+        u32x4 w;
 #pragma unroll
-          for (int h = 0; h < NH; ++h)
+        for (int i = 0; i < 4; ++i)
+          w[i] = __builtin_amdgcn_perm(v[2 * i + 1][0][c >> 1], v[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)       // channels 64 h + 4 l16 + c
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                acc[t][4 * h + c] = mfma_f32(__uint_as_float(v[i][h][c]), p[0][i], acc[t][4 * h + c]);
+        for (int t = 0; t < RT; ++t) {
+          acc[t][c] = mfma_bf16(w, hi[t], acc[t][c]);
+          acc[t][c] = mfma_bf16(w, lo[t], acc[t][c]);
         }
       }
+    } else {
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)       // channels 64 h + 4 l16 + c
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc[t][4 * h + c] = mfma_f32(__uint_as_float(v[i][h][c]), p[t][0][i], acc[t][4 * h + c]);
     }
+    if (s + 1 < steps) request_v(next);
+    now = next;
+    next = after;
   }
 
   // ---- the waves' shares, then the unit's result
@@ -398,10 +479,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
 }
 
 constexpr int AIM = 1024;                  // workgroups
-int row_tiles(int R) { return R <= 16 ? 1 : 2; }
+constexpr int MAX_TILES = 4;               // of 16 query rows that a workgroup takes
+struct Tiles { int each, blocks; };        // tiles of a workgroup, workgroups that the rows of a kv head take
+Tiles tiles_of(int R) {
+  const int all = (R + 15) / 16, blocks = (all + MAX_TILES - 1) / MAX_TILES;
+  return {(all + blocks - 1) / blocks, blocks};
+}
 int units_aimed(int R, int G) {
-  const int per = G * ((R + 16 * row_tiles(R) - 1) / (16 * row_tiles(R)));
-  return per < AIM ? AIM / per : 1;
+  const int64_t per = (int64_t)G * tiles_of(R).blocks;
+  return per < AIM ? (int)(AIM / per) : 1;
 }
 
 }  // namespace
@@ -413,28 +499,33 @@ size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G) {
 }
 
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
-  const int R = a.M * (a.H / a.G), RT = row_tiles(R), rowblocks = (R + 16 * RT - 1) / (16 * RT);
+  const int R = a.M * (a.H / a.G);
+  const Tiles tiles = tiles_of(R);
   a.target = units_aimed(R, a.G);
   a.least = WAVES;
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
   const int heads8 = (a.target + a.B) * a.G;
-  const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * rowblocks)), wg(64 * WAVES);
+  const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(64 * WAVES);
   const bool tree = a.n_true != nullptr, narrow = !bf16 && a.d <= 64;
   {
     ProfScope ps("paged_attn", s);
-    auto go = [&](auto bf_, auto nh_) {
+    auto go = [&](auto bf_, auto nh_, auto rt_) {
       constexpr bool BF = decltype(bf_)::value != 0;
-      constexpr int NH = decltype(nh_)::value;
-      if (RT == 1 && !tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, 1, false>), grid, wg, 0, s, a, heads8, rowblocks);
-      else if (RT == 1) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, 1, true>), grid, wg, 0, s, a, heads8, rowblocks);
-      else if (!tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, 2, false>), grid, wg, 0, s, a, heads8, rowblocks);
-      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, 2, true>), grid, wg, 0, s, a, heads8, rowblocks);
+      constexpr int NH = decltype(nh_)::value, RT = decltype(rt_)::value;
+      if (tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, true>), grid, wg, 0, s, a, heads8, tiles.blocks);
+      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, false>), grid, wg, 0, s, a, heads8, tiles.blocks);
     };
-    if (bf16) go(int_c<1>{}, int_c<1>{});
-    else if (narrow) go(int_c<0>{}, int_c<1>{});
-    else go(int_c<0>{}, int_c<2>{});
+    auto with = [&](auto bf_, auto nh_) {
+      if (tiles.each == 1) go(bf_, nh_, int_c<1>{});
+      else if (tiles.each == 2) go(bf_, nh_, int_c<2>{});
+      else if (tiles.each == 3) go(bf_, nh_, int_c<3>{});
+      else go(bf_, nh_, int_c<4>{});
+    };
+    if (bf16) with(int_c<1>{}, int_c<1>{});
+    else if (narrow) with(int_c<0>{}, int_c<1>{});
+    else with(int_c<0>{}, int_c<2>{});
   }
   // no entry can have two units: nothing to join
   if ((a.bound + PAGED_BLOCK - 1) / PAGED_BLOCK <= a.least) return;
