@@ -53,9 +53,9 @@ beagle_status check_paged(const beagle_xattn_desc* desc, const beagle_paged_cach
   if (st != BEAGLE_OK) return st;
   Dims& d = out->d;
   d.B = desc->batch; d.S = desc->seq_q; d.L = desc->seq_kv; d.Tq = d.B * d.S;
-  // grids: 16 rows a workgroup at least, units of every entry and kv head
+  // grids: 16 rows a workgroup at least
   const int64_t rows = d.S * (d.H / d.G);
-  if (rows > (1 << 24) || (d.B + 1024) * d.G * ((rows + 15) / 16) > (1 << 28) || d.H * d.S > (1 << 28)) return BEAGLE_ERR_UNSUPPORTED;
+  if (rows > (1 << 24) || d.G * ((rows + 15) / 16) > (1 << 24) || d.H * d.S > (1 << 28)) return BEAGLE_ERR_UNSUPPORTED;
   st = check_cache(cache, &out->c);
   if (st != BEAGLE_OK) return st;
   out->page_bytes = ((int64_t)1 << out->c.shift) * d.GD * (int64_t)d.esz;

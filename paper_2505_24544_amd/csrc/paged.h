@@ -26,8 +26,8 @@ struct PagedAttnArgs {
   const int32_t* n_true;                   // [B] or null: every row is a true one
   const uint32_t* tree; int32_t words;     // [B, M, words]
   int32_t window, sinks;                   // window 0: none
-  float* part; float* ml;                  // partial sums of the units, see paged_attn.hip
-  int32_t target, least;                   // units of a kv head to aim at, blocks that a unit has at least
+  float* part; float* ml;                  // sums of the parts of entries that several workers share
+  int32_t target, least;                   // see paged_workers
 };
 size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G);
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s);

@@ -25,59 +25,38 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4;
+// workgroups that fit on a compute unit at a time (registers)
+constexpr int RESIDENT(int RT, int NH) { return RT == 1 && NH == 1 ? 3 : RT <= 2 ? 2 : 1; }
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // what rows that nobody sees are read from: their V must be a number (0 * NaN is NaN)
 __device__ __align__(16) const unsigned char zero_row[1024] = {};
 
-__device__ __forceinline__ PagedRows rows_of(const PagedAttnArgs& a, int slot, int b) {
-  const int n = min(paged_len(a.c, slot), a.bound);
-  return paged_rows(n, a.n_true ? a.n_true[b] : n, a.window, a.sinks);
+// Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks of the row of all blocks that it
+// and the lanes before it have.
+struct Entry { int slot, blocks, upto; PagedRows rows; };
+__device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
+  Entry e;
+  e.slot = -1; e.blocks = 0;
+  e.rows = PagedRows{};
+  if (b < a.B) {
+    const int nt = a.n_true ? a.n_true[b] : INT32_MAX;
+    e.slot = paged_slot(a.c, a.slots, b);
+    e.rows = paged_rows(min(paged_len(a.c, e.slot), a.bound), nt, a.window, a.sinks);
+    e.blocks = e.rows.blocks;
+  }
+  e.upto = e.blocks;                       // (64 entries of 2^23 blocks: fits)
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int x = __shfl_up(e.upto, m);
+    if ((int)(threadIdx.x & 63) >= m) e.upto += x;
+  }
+  return e;
 }
-
-// Where a unit lives: entry, its blocks, and where its partial sums go (first unit of the entry; units that the entry has).
-struct Unit { int b, i, units, first, chunk; };
-// Every wave walks the entries by itself, 64 at a time.  want_entry: the unit 0 of entry `which`; else unit number `which`
-// (b = -1: there are fewer).
-__device__ Unit find_unit(const PagedAttnArgs& a, int which, bool want_entry) {
-  const int lane = threadIdx.x & 63;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    int blocks = b < a.B ? rows_of(a, paged_slot(a.c, a.slots, b), b).blocks : 0;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) blocks += __shfl_xor(blocks, m);       // (64 entries of 2^23 blocks: fits)
-    total += __builtin_amdgcn_readfirstlane(blocks);
-  }
-  Unit u;
-  u.chunk = paged_chunk(total, a.target, a.least);
-  u.b = -1;
-  int base = 0, parts = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    const int mine = b < a.B ? paged_units(rows_of(a, paged_slot(a.c, a.slots, b), b).blocks, u.chunk) : 0;
-    const int kept = mine > 1 ? mine : 0;
-    int upto = mine, pupto = kept;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int x = __shfl_up(upto, m), y = __shfl_up(pupto, m);
-      if (lane >= m) { upto += x; pupto += y; }
-    }
-    const bool hit = want_entry ? b == which : b < a.B && which >= base + upto - mine && which < base + upto;
-    const unsigned long long at = __ballot(hit);
-    if (at) {
-      const int l = __ffsll((long long)at) - 1;
-      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      u.b = b0 + l;
-      u.units = of(mine);
-      u.i = want_entry ? 0 : which - base - (of(upto) - u.units);
-      u.first = parts + of(pupto) - of(kept);
-      return u;
-    }
-    base += __builtin_amdgcn_readlane(upto, 63);
-    parts += __builtin_amdgcn_readlane(pupto, 63);
-  }
-  return u;
+__device__ __forceinline__ int64_t all_blocks(const PagedAttnArgs& a, const Entry& first) {
+  int64_t all = __builtin_amdgcn_readlane(first.upto, 63);
+  for (int b0 = 64; b0 < a.B; b0 += 64) all += __builtin_amdgcn_readlane(entry_of(a, b0 + (threadIdx.x & 63)).upto, 63);
+  return all;
 }
 
 // over the four lanes that hold a column's keys
@@ -94,6 +73,7 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 template <bool BF16, int NH> struct Shape {
+  static constexpr int HDP = BF16 ? 128 : 64 * NH;      // head width, padded
   static constexpr int KROWS = BF16 ? 32 : 16;          // rows of a step
   static constexpr int KT = KROWS / 16;                 // score tiles of a step
   static constexpr int NJ = BF16 ? 4 : 4 * NH;          // 16-byte pieces of a row that a lane holds for the scores
@@ -101,27 +81,18 @@ template <bool BF16, int NH> struct Shape {
   static constexpr int NA = BF16 ? 8 : 4 * NH;          // accumulator tiles
 };
 
-// BF16: head width 128.  Float: NH = 1 for widths up to 64, 2 up to 128.  RT: tiles of 16 query rows that a workgroup takes.
-// TREE: rows from n_true on are seen as the tree's bits say.
+template <int HDP, int RT> struct Merge { float o[WAVES][16][HDP + 4], m[WAVES][RT * 16], l[WAVES][RT * 16]; };
+
+// One entry's blocks first .. last - 1 for one kv head and row block: the four waves take every fourth.
 template <bool BF16, int NH, int RT, bool TREE>
-__global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
+__device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape<BF16, NH>::HDP, RT>& sh, int b, int slot, const PagedRows rows,
+                                             int first, int last, bool whole, int part, int head, int rb) {
   using S = Shape<BF16, NH>;
-  constexpr int E = BF16 ? 2 : 4, HDP = BF16 ? 128 : 64 * NH;       // bytes of a value; padded head width
-  __shared__ float part_o[WAVES][16][HDP + 4];
-  __shared__ float part_m[WAVES][RT * 16], part_l[WAVES][RT * 16];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
-  // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
-  const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
-  if (ug >= heads8) return;
-  const int head = ug % a.G;
-  const Unit u = find_unit(a, ug / a.G, false);
-  if (u.b < 0) return;
-  const int slot = __builtin_amdgcn_readfirstlane(paged_slot(a.c, a.slots, u.b));
-  PagedRows rows = rows_of(a, slot, u.b);
-  rows.n = __builtin_amdgcn_readfirstlane(rows.n); rows.nt = __builtin_amdgcn_readfirstlane(rows.nt);
-  rows = paged_rows(rows.n, rows.nt, a.window, a.sinks);               // (the wave's, not a lane's)
+  constexpr int E = BF16 ? 2 : 4, HDP = S::HDP;              // bytes of a value; padded head width
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));            // what is made of it belongs to this entry: kept for the next one it would take registers
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int rep = a.H / a.G, R = a.M * rep;
-  const int first = u.i * u.chunk, last = min(first + u.chunk, rows.blocks);
   const int64_t row_bytes = (int64_t)a.G * a.d * E;
   const char* kbase = (const char*)a.c.k + (int64_t)head * a.d * E;
   const char* vbase = (const char*)a.c.v + (int64_t)head * a.d * E;
@@ -135,7 +106,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
   for (int t = 0; t < RT; ++t) {
     const int r = (rb * RT + t) * 16 + l16, m = r / rep;
     qm[t] = m;
-    const char* p = (const char*)a.q + ((((int64_t)u.b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
+    const char* p = (const char*)a.q + ((((int64_t)b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       const int piece = (4 * j + g4) * 16;
@@ -156,87 +127,15 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
   constexpr int SUB = PAGED_BLOCK / S::KROWS;
   const int steps = last > first + wave ? (last - first - wave + WAVES - 1) / WAVES * SUB : 0;
   const int shift = a.c.shift;
-  const bool wide = shift >= 4;            // 16 rows of a score tile stand on one page: its number is the wave's, not a lane's
   auto base_of = [&](int s) { return paged_block(rows, first + wave + s / SUB * WAVES) * PAGED_BLOCK + s % SUB * S::KROWS; };
-  auto page_of = [&](int row) { return paged_page(table, row, paged_seen(rows, row), shift, a.c.P); };
-  // page numbers of a step, a step ahead of the rows: of the tiles, if they stand on one page each
-  struct Ahead { int base, whole; int page[S::KT]; };
-  auto look = [&](int s) BEAGLE_INLINE_LAMBDA {
-    Ahead h;
-    h.base = __builtin_amdgcn_readfirstlane(s < steps ? base_of(s) : rows.n);
-    h.whole = wide && paged_all_seen(rows, h.base, S::KROWS);
-#pragma unroll
-    for (int t = 0; t < S::KT; ++t) h.page[t] = h.whole ? table[(h.base + 16 * t) >> shift] : 0;
-    return h;
+  auto next_whole = [&](int s) BEAGLE_INLINE_LAMBDA {          // the first step from s on whose rows every query sees
+    while (s < steps && !paged_all_seen(rows, base_of(s), S::KROWS)) ++s;
+    return s;
   };
-  // (an unreadable page number: the step goes row by row)
-  auto settle = [&](Ahead& h) BEAGLE_INLINE_LAMBDA {
-#pragma unroll
-    for (int t = 0; t < S::KT; ++t) {
-      h.page[t] = __builtin_amdgcn_readfirstlane(h.page[t]);
-      if ((unsigned)h.page[t] >= (unsigned)a.c.P) h.whole = 0;
-    }
-  };
-  uint32_t koff[S::NJ], voff[4][NH];       // of a lane's pieces, from the first row of a tile
-#pragma unroll
-  for (int j = 0; j < S::NJ; ++j) koff[j] = (uint32_t)(l16 * row_bytes) + (4 * j + g4) * 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int h = 0; h < NH; ++h) voff[i][h] = (uint32_t)((4 * g4 + i) * row_bytes) + (16 * h + l16) * 16;
   u32x4 k[S::KT][S::NJ], v[S::NV][NH];
-  // K rows, one in each lane's l16
-  auto request_k = [&](const Ahead& h) BEAGLE_INLINE_LAMBDA {
-#pragma unroll
-    for (int t = 0; t < S::KT; ++t) {
-      if (h.whole) {
-        const char* src = kbase + (((int64_t)h.page[t] << shift) + ((h.base + 16 * t) & in_page)) * row_bytes;
-#pragma unroll
-        for (int j = 0; j < S::NJ; ++j)
-          k[t][j] = BF16 || (4 * j + g4) * 16 < a.d * E ? *(const u32x4*)(src + koff[j]) : u32x4{0, 0, 0, 0};
-      } else {
-        const int row = h.base + 16 * t + l16, p = page_of(row);
-        const char* src = p >= 0 ? kbase + (((int64_t)p << shift) + (row & in_page)) * row_bytes : (const char*)zero_row;
-#pragma unroll
-        for (int j = 0; j < S::NJ; ++j) {
-          const int piece = (4 * j + g4) * 16;
-          k[t][j] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
-        }
-      }
-    }
-  };
-  // V rows, four neighbours in each lane's g4 (one page: its rows are a multiple of four)
-  auto request_v = [&](const Ahead& h) BEAGLE_INLINE_LAMBDA {
-#pragma unroll
-    for (int t = 0; t < S::KT; ++t) {
-      if (h.whole) {
-        const char* src = vbase + (((int64_t)h.page[t] << shift) + ((h.base + 16 * t) & in_page)) * row_bytes;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int n = 0; n < NH; ++n)
-            v[4 * t + i][n] = BF16 || (16 * n + l16) * 16 < a.d * E ? *(const u32x4*)(src + voff[i][n]) : u32x4{0, 0, 0, 0};
-      } else {
-        const int r0 = h.base + 16 * t + 4 * g4, p = paged_page(table, r0, r0 < rows.n, shift, a.c.P);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool seen = p >= 0 && paged_seen(rows, r0 + i);
-          const char* src = seen ? vbase + (((int64_t)p << shift) + ((r0 + i) & in_page)) * row_bytes : (const char*)zero_row;
-#pragma unroll
-          for (int n = 0; n < NH; ++n) {
-            const int piece = (16 * n + l16) * 16;
-            v[4 * t + i][n] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
-          }
-        }
-      }
-    }
-  };
-  Ahead now = look(0), next = look(1);
-  settle(now);
-  if (steps > 0) { request_k(now); request_v(now); }
-  for (int s = 0; s < steps; ++s) {
-    // ---- scores
-    f32x4 sc[RT][S::KT];
+  f32x4 sc[RT][S::KT];
+  float p[RT][S::KT][4];
+  auto scores = [&]() BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -250,62 +149,16 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
             for (int e = 0; e < 4; ++e) sc[t][kt] = mfma_f32(__uint_as_float(k[kt][j][e]), __uint_as_float(q[t][j][e]), sc[t][kt]);
         }
       }
-    // the registers of K are free: the next step's rows travel while this one's probabilities are computed
-    settle(next);
-    if (s + 1 < steps) request_k(next);
-    const Ahead after = look(s + 2);
-    bool seen[S::KT][4];
-    if (!now.whole) {
-#pragma unroll
-      for (int kt = 0; kt < S::KT; ++kt) {
-        const int r0 = now.base + 16 * kt + 4 * g4;
-        const bool there = paged_page(table, r0, r0 < rows.n, shift, a.c.P) >= 0;      // (a page number that is none hides its rows)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) seen[kt][i] = there && paged_seen(rows, r0 + i);
-      }
-    }
-    // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
-    // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
-    [[maybe_unused]] bool odd = false;
-    if constexpr (TREE)
-      if (now.base + S::KROWS > rows.nt) {
-        unsigned top = 0;
-#pragma unroll
-        for (int i = 0; i < S::NV; ++i)
-#pragma unroll
-          for (int h = 0; h < NH; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned x = v[i][h][e];
-              top = max(top, x & 0x7f800000u);
-              if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
-            }
-        odd = __ballot(top == 0x7f800000u) != 0;
-      }
-    // ---- running maximum and sum, probabilities
-    float p[RT][S::KT][4];
+  };
+  // running maximum and sum, probabilities
+  auto probabilities = [&]() BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      if (!now.whole) {
-#pragma unroll
-        for (int kt = 0; kt < S::KT; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            bool see = seen[kt][i];
-            if constexpr (TREE) {
-              const int bit = now.base + 16 * kt + 4 * g4 + i - rows.nt;
-              if (see && bit >= 0)
-                see = qm[t] < a.M && (bit >> 5) < a.words &&
-                      (a.tree[((int64_t)u.b * a.M + qm[t]) * a.words + (bit >> 5)] >> (bit & 31) & 1u);
-            }
-            if (!see) sc[t][kt][i] = -INFINITY;
-          }
-      }
       float top = sc[t][0][0];
 #pragma unroll
       for (int e = 1; e < 4 * S::KT; ++e) top = fmaxf(top, sc[t][e / 4][e % 4]);
       const float most = fmaxf(mx[t], max_over_keys(top) * c2), safe = most == -INFINITY ? 0.f : most;
-      if (__any(most > mx[t])) {
+      if (__any(most > mx[t])) {           // (after the first steps seldom)
         const float shrink = exp2_fast(mx[t] - safe);
         sum[t] *= shrink;
 #pragma unroll
@@ -317,33 +170,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
         for (int i = 0; i < 4; ++i) { p[t][kt][i] = exp2_fast(fmaf(sc[t][kt][i], c2, -safe)); sum[t] += p[t][kt][i]; }
     }
-    // ---- O^T += V^T P^T
-    if (TREE && odd) {
-      float* mine = part_o[wave][l16];       // (free until the end)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int kt = 0; kt < S::KT; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mine[16 * kt + 4 * g4 + i] = sc[t][kt][i] == -INFINITY ? -1.f : p[t][kt][i];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int j = 0; j < S::KROWS; ++j) {
-          const float w = mine[j];
-          const int row = now.base + j, pg = page_of(row);
-          if (w == -1.f || pg < 0) continue;
-          const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
-#pragma unroll
-          for (int c = 0; c < S::NA; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
-              if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
-              else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      }
-    } else if constexpr (BF16) {
+  };
+  // O^T += V^T P^T
+  auto values = [&]() BEAGLE_INLINE_LAMBDA {
+    if constexpr (BF16) {
       // a probability as two bf16 numbers, 16 bits in all: the matrix pipe has the time, and the rounding of one
       // would cost the output as much again as its own (2^-9)
       u32x4 hi[RT], lo[RT];
@@ -377,9 +207,168 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
 #pragma unroll
             for (int t = 0; t < RT; ++t) acc[t][4 * h + c] = mfma_f32(__uint_as_float(v[i][h][c]), p[t][0][i], acc[t][4 * h + c]);
     }
-    if (s + 1 < steps) request_v(next);
-    now = next;
-    next = after;
+  };
+
+  // ---- steps whose rows every query sees: the rows of the next one travel while this one is computed, its page numbers a
+  // step further ahead.  A lane holds one K row of each tile (l16) and four V rows (4 g4 ..; one page: its rows are a multiple of four).
+  // Where a page number is none, the step is left for below.
+  struct Pages { int k[S::KT], v[S::KT]; };
+  auto look = [&](int s) BEAGLE_INLINE_LAMBDA {
+    Pages h;
+    const int base = base_of(s);
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) { h.k[t] = table[(base + 16 * t + l16) >> shift]; h.v[t] = table[(base + 16 * t + 4 * g4) >> shift]; }
+    return h;
+  };
+  auto usable = [&](Pages& h) BEAGLE_INLINE_LAMBDA {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) {
+      if ((unsigned)h.k[t] >= (unsigned)a.c.P) { bad = true; h.k[t] = 0; }
+      if ((unsigned)h.v[t] >= (unsigned)a.c.P) { bad = true; h.v[t] = 0; }
+    }
+    return __ballot(bad) == 0;
+  };
+  auto request_k = [&](const Pages& h, int base) BEAGLE_INLINE_LAMBDA {
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) {
+      const char* src = kbase + (((int64_t)h.k[t] << shift) + ((base + 16 * t + l16) & in_page)) * row_bytes + 16 * g4;
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) k[t][j] = *(const u32x4*)(BF16 || (4 * j + g4) * 16 < a.d * E ? src + 64 * j : (const char*)zero_row);
+    }
+  };
+  auto request_v = [&](const Pages& h, int base) BEAGLE_INLINE_LAMBDA {
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) {
+      const char* src = vbase + (((int64_t)h.v[t] << shift) + ((base + 16 * t + 4 * g4) & in_page)) * row_bytes + 16 * l16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i, src += row_bytes)
+#pragma unroll
+        for (int n = 0; n < NH; ++n)
+          v[4 * t + i][n] = *(const u32x4*)(BF16 || (16 * n + l16) * 16 < a.d * E ? src + 256 * n : (const char*)zero_row);
+    }
+  };
+  int s = next_whole(0);
+  if (s < steps) {
+    Pages here = look(s), there;
+    int s1 = next_whole(s + 1);
+    bool ok = usable(here);
+    request_k(here, base_of(s));
+    if (s1 < steps) there = look(s1);
+    request_v(here, base_of(s));
+    while (true) {
+      scores();
+      const bool more = s1 < steps;
+      bool ok1 = false;
+      int s2 = s1;
+      Pages then = there;
+      if (more) {
+        ok1 = usable(there);
+        request_k(there, base_of(s1));
+        s2 = next_whole(s1 + 1);
+        if (s2 < steps) then = look(s2);
+      }
+      if (ok) {
+        probabilities();
+        values();
+      }
+      if (!more) break;
+      request_v(there, base_of(s1));
+      s = s1; s1 = s2; ok = ok1; there = then;
+    }
+  }
+
+  // ---- the others, row by row: rows behind the end, at a window's edges, under the tree, on pages that are none
+  auto page_of = [&](int row) { return paged_page(table, row, paged_seen(rows, row), shift, a.c.P); };
+  for (int i1 = 0; i1 < steps; ++i1) {
+    const int base = base_of(i1);
+    if (base >= rows.n) break;
+    if (paged_all_seen(rows, base, S::KROWS)) {
+      Pages h = look(i1);
+      if (usable(h)) continue;
+    }
+    bool seen[S::KT][4];
+#pragma unroll
+    for (int t = 0; t < S::KT; ++t) {
+      const int row = base + 16 * t + l16, pk = page_of(row);
+      const char* src = pk >= 0 ? kbase + (((int64_t)pk << shift) + (row & in_page)) * row_bytes : (const char*)zero_row;
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) {
+        const int piece = (4 * j + g4) * 16;
+        k[t][j] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
+      }
+      const int r0 = base + 16 * t + 4 * g4, pv = paged_page(table, r0, r0 < rows.n, shift, a.c.P);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        seen[t][i] = pv >= 0 && paged_seen(rows, r0 + i);
+        const char* from = seen[t][i] ? vbase + (((int64_t)pv << shift) + ((r0 + i) & in_page)) * row_bytes : (const char*)zero_row;
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+          const int piece = (16 * n + l16) * 16;
+          v[4 * t + i][n] = *(const u32x4*)(BF16 || piece < a.d * E ? from + piece : (const char*)zero_row);
+        }
+      }
+    }
+    scores();
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int kt = 0; kt < S::KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bool see = seen[kt][i];
+          if constexpr (TREE) {
+            const int bit = base + 16 * kt + 4 * g4 + i - rows.nt;
+            if (see && bit >= 0)
+              see = qm[t] < a.M && (bit >> 5) < a.words &&
+                    (a.tree[((int64_t)b * a.M + qm[t]) * a.words + (bit >> 5)] >> (bit & 31) & 1u);
+          }
+          if (!see) sc[t][kt][i] = -INFINITY;
+        }
+    probabilities();
+    // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
+    // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
+    if constexpr (TREE) {
+      unsigned top = 0;
+#pragma unroll
+      for (int i = 0; i < S::NV; ++i)
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const unsigned x = v[i][h][e];
+            top = max(top, x & 0x7f800000u);
+            if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
+          }
+      if (__ballot(top == 0x7f800000u)) {
+        float* mine = sh.o[wave][l16];       // (free until the end)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int kt = 0; kt < S::KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[16 * kt + 4 * g4 + i] = sc[t][kt][i] == -INFINITY ? -1.f : p[t][kt][i];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          for (int j = 0; j < S::KROWS; ++j) {
+            const float w = mine[j];
+            const int row = base + j, pg = page_of(row);
+            if (w == -1.f || pg < 0) continue;
+            const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
+#pragma unroll
+            for (int c = 0; c < S::NA; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
+                if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
+                else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
+              }
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        continue;
+      }
+    }
+    values();
   }
 
   // ---- the waves' shares, then the unit's result
@@ -388,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
     float l = sum[t];
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (g4 == 0) { part_m[wave][16 * t + l16] = mx[t]; part_l[wave][16 * t + l16] = l; }
+    if (g4 == 0) { sh.m[wave][16 * t + l16] = mx[t]; sh.l[wave][16 * t + l16] = l; }
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -399,114 +388,185 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(PagedAttnArgs a,
       for (int c = 0; c < S::NA; c += 4) {
         // accumulator row 4 g4 + i: bf16 channels 8 (4 g4 + i) + c, float channels 64 h + 4 (4 g4 + i) + c % 4
         const int ch = BF16 ? 8 * (4 * g4 + i) + c : 16 * c + 4 * (4 * g4 + i);
-        *(f32x4*)&part_o[wave][l16][ch] = f32x4{acc[t][c][i], acc[t][c + 1][i], acc[t][c + 2][i], acc[t][c + 3][i]};
+        *(f32x4*)&sh.o[wave][l16][ch] = f32x4{acc[t][c][i], acc[t][c + 1][i], acc[t][c + 2][i], acc[t][c + 3][i]};
       }
     __syncthreads();
-    const int col = threadIdx.x >> 4, r = (rb * RT + t) * 16 + col;
+    const int col = tid >> 4, r = (rb * RT + t) * 16 + col;
     if (r >= R) continue;
     float m = -INFINITY, l = 0.f, w[WAVES];
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) m = fmaxf(m, part_m[i][16 * t + col]);
+    for (int i = 0; i < WAVES; ++i) m = fmaxf(m, sh.m[i][16 * t + col]);
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-      w[i] = m == -INFINITY ? 0.f : exp2_fast(part_m[i][16 * t + col] - m);
-      l += part_l[i][16 * t + col] * w[i];
+      w[i] = m == -INFINITY ? 0.f : exp2_fast(sh.m[i][16 * t + col] - m);
+      l += sh.l[i][16 * t + col] * w[i];
     }
     const int qi = r / rep, h = head * rep + r % rep;
-    const bool whole = u.units == 1;
     const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-    const int64_t prow = ((int64_t)(u.first + u.i) * a.G + head) * R + r;      // (whole: not used)
+    const int64_t prow = ((int64_t)part * a.G + head) * R + r;      // (whole: not used)
 #pragma unroll
     for (int half = 0; half < HDP / 64; ++half) {
-      const int ch = 64 * half + 4 * (threadIdx.x & 15);
+      const int ch = 64 * half + 4 * (tid & 15);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < WAVES; ++i) o += *(const f32x4*)&part_o[i][col][ch] * w[i];
+      for (int i = 0; i < WAVES; ++i) o += *(const f32x4*)&sh.o[i][col][ch] * w[i];
       o *= inv;
       if (!whole) { *(f32x4*)(a.part + prow * HDP + ch) = o; continue; }
       if (ch >= a.d) continue;
-      const int64_t at = (((int64_t)u.b * a.M + qi) * a.H + h) * a.d + ch;
+      const int64_t at = (((int64_t)b * a.M + qi) * a.H + h) * a.d + ch;
       if constexpr (BF16) *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
       else *(f32x4*)((float*)a.o + at) = o;
     }
-    if ((threadIdx.x & 15) == 0) {
-      if (whole) a.lse[((int64_t)u.b * a.H + h) * a.M + qi] = (m + __log2f(l)) * LN2;
+    if ((tid & 15) == 0) {
+      if (whole) a.lse[((int64_t)b * a.H + h) * a.M + qi] = (m + __log2f(l)) * LN2;
       else *(float2*)(a.ml + prow * 2) = make_float2(m, l);
     }
   }
 }
 
-// The units of an entry, in order: eight of them at a time (a group of 32 lanes each), then the groups through LDS.
-template <bool BF16, int HDP>
+// BF16: head width 128.  Float: NH = 1 for widths up to 64, 2 up to 128.  RT: tiles of 16 query rows that a workgroup takes.
+// TREE: rows from n_true on are seen as the tree's bits say.
+template <bool BF16, int NH, int RT, bool TREE>
+__global__ __launch_bounds__(64 * WAVES, RESIDENT(RT, NH)) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
+  __shared__ Merge<Shape<BF16, NH>::HDP, RT> shared;
+  const int lane = threadIdx.x & 63;
+  // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
+  const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
+  const int head = ug % a.G, worker = ug / a.G;
+  const Entry group0 = entry_of(a, lane);
+  const int64_t all = all_blocks(a, group0);
+  const int workers = paged_workers(all, a.target, a.least);
+  if (worker >= workers) return;
+  const int64_t lo = paged_cut(all, workers, worker), hi = paged_cut(all, workers, worker + 1);
+  int64_t base0 = 0;                       // blocks before this group of entries
+  bool used = false;                       // LDS holds another entry's shares
+  for (int b0 = 0; b0 < a.B && base0 < hi; b0 += 64) {
+    Entry e = group0;
+    if (b0) e = entry_of(a, b0 + lane);
+    const int64_t start = base0 + e.upto - e.blocks;
+    const PagedShare share = paged_share(start, e.blocks, lo, hi, a.least);
+    unsigned long long mine = __ballot(share.from < share.to);
+    base0 += __builtin_amdgcn_readlane(e.upto, 63);
+    while (mine) {
+      const int l = __ffsll((long long)mine) - 1;
+      mine &= mine - 1;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      const int b = b0 + l, slot = of(e.slot), first = of(share.from), last = of(share.to);
+      const PagedRows rows = paged_rows(of(e.rows.n), of(e.rows.nt), a.window, a.sinks);
+      const bool whole = last - first == rows.blocks;
+      if (used) __syncthreads();
+      used = true;
+      // a part's sums: one place for the entry that the worker goes on with, one for the entry that it begins
+      attend_entry<BF16, NH, RT, TREE>(a, shared, b, slot, rows, first, last, whole, 2 * worker + (first == 0), head, rb);
+    }
+  }
+}
+
+// The units of an entry, in order.  A row is joined by 32 (narrow floats: 16) lanes; ROWS of them share a workgroup, whose other
+// lanes take every (groups / ROWS)-th unit of a row each and meet in LDS.
+template <bool BF16, int HDP, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
-  constexpr int GROUPS = 256 / (HDP / 4);
+  constexpr int LANES = HDP / 4, GROUPS = 256 / LANES, SPLIT = GROUPS / ROWS;
   __shared__ float so[GROUPS][HDP];
   __shared__ float sm[GROUPS], sl[GROUPS];
   const int rep = a.H / a.G, R = a.M * rep;
-  const Unit u = find_unit(a, blockIdx.y, true);
-  if (u.units <= 1) return;
-  const int h = blockIdx.x % a.H, qi = blockIdx.x / a.H, head = h / rep, r = qi * rep + h % rep;
-  const int group = threadIdx.x / (HDP / 4), ch = 4 * (threadIdx.x % (HDP / 4));
+  // the entry's blocks, and the workers that have a part of them
+  const int lane = threadIdx.x & 63, b = blockIdx.y;
+  const Entry group0 = entry_of(a, lane);
+  const int64_t all = all_blocks(a, group0);
+  const int workers = paged_workers(all, a.target, a.least);
+  int64_t start = 0;
+  Entry e = group0;
+  for (int b0 = 0;; b0 += 64) {
+    if (b0) e = entry_of(a, b0 + lane);
+    if (b < b0 + 64) break;
+    start += __builtin_amdgcn_readlane(e.upto, 63);
+  }
+  const int blocks = __builtin_amdgcn_readlane(e.blocks, b & 63);
+  start += __builtin_amdgcn_readlane(e.upto, b & 63) - blocks;
+  const int w0 = paged_worker_of(all, workers, start), units = paged_worker_of(all, workers, start + blocks - 1) - w0 + 1;
+  if (blocks <= a.least || units <= 1) return;
+  const int group = threadIdx.x / LANES, ch = 4 * (threadIdx.x % LANES);
+  const int n = blockIdx.x * ROWS + group / SPLIT;         // row of the entry: kv head, then query and head of the group
+  const int head = n / R, r = n % R, qi = r / rep, h = head * rep + r % rep;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  for (int i = group; i < u.units; i += GROUPS) {
-    const int64_t prow = ((int64_t)(u.first + i) * a.G + head) * R + r;
-    const float2 ml = *(const float2*)(a.ml + prow * 2);
-    const f32x4 po = *(const f32x4*)(a.part + prow * HDP + ch);
-    const float now = fmaxf(m, ml.x), safe = now == -INFINITY ? 0.f : now;
-    const float w0 = exp2_fast(m - safe), w1 = exp2_fast(ml.x - safe);
-    o = o * w0 + po * w1;
-    l = l * w0 + ml.y * w1;
+  auto join = [&](float m2, float l2, f32x4 o2) BEAGLE_INLINE_LAMBDA {
+    const float now = fmaxf(m, m2), safe = now == -INFINITY ? 0.f : now;
+    const float w0 = exp2_fast(m - safe), w1 = exp2_fast(m2 - safe);
+    o = o * w0 + o2 * w1;
+    l = l * w0 + l2 * w1;
     m = now;
+  };
+  if (n < a.G * R) {
+    const int64_t row0 = ((int64_t)2 * w0 * a.G + head) * R + r, step = (int64_t)a.G * R;
+    constexpr int AT_ONCE = 4;
+    for (int i = group % SPLIT; i < units; i += SPLIT * AT_ONCE) {
+      float2 ml[AT_ONCE];
+      f32x4 po[AT_ONCE];
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e) {
+        const int n = min(i + e * SPLIT, units - 1);
+        const int64_t row = row0 + step * (n ? 2 * n : 1);
+        ml[e] = *(const float2*)(a.ml + row * 2);
+        po[e] = *(const f32x4*)(a.part + row * HDP + ch);
+      }
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e)
+        if (i + e * SPLIT < units) join(ml[e].x, ml[e].y, po[e]);
+    }
   }
-  *(f32x4*)&so[group][ch] = o;
-  if (ch == 0) { sm[group] = m; sl[group] = l; }
-  __syncthreads();
-  if (group) return;
-  for (int i = 1; i < GROUPS; ++i) {
-    const float now = fmaxf(m, sm[i]), safe = now == -INFINITY ? 0.f : now;
-    const float w0 = exp2_fast(m - safe), w1 = exp2_fast(sm[i] - safe);
-    o = o * w0 + *(const f32x4*)&so[i][ch] * w1;
-    l = l * w0 + sl[i] * w1;
-    m = now;
+  if constexpr (SPLIT > 1) {
+    *(f32x4*)&so[group][ch] = o;
+    if (ch == 0) { sm[group] = m; sl[group] = l; }
+    __syncthreads();
+    if (group % SPLIT) return;
+#pragma unroll
+    for (int i = 1; i < SPLIT; ++i) join(sm[group + i], sl[group + i], *(const f32x4*)&so[group + i][ch]);
   }
-  if (ch == 0) a.lse[((int64_t)u.b * a.H + h) * a.M + qi] = (m + __log2f(l)) * LN2;
+  if (n >= a.G * R) return;
+  if (ch == 0) a.lse[((int64_t)b * a.H + h) * a.M + qi] = (m + __log2f(l)) * LN2;
   if (ch >= a.d) return;
   o *= l == 0.f ? 0.f : 1.f / l;
-  const int64_t at = (((int64_t)u.b * a.M + qi) * a.H + h) * a.d + ch;
+  const int64_t at = (((int64_t)b * a.M + qi) * a.H + h) * a.d + ch;
   if constexpr (BF16) *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
-constexpr int AIM = 1024;                  // workgroups
+#ifndef ROUNDS1
+#define ROUNDS1 1
+#define ROUNDS3 1
+#endif
 constexpr int MAX_TILES = 4;               // of 16 query rows that a workgroup takes
 struct Tiles { int each, blocks; };        // tiles of a workgroup, workgroups that the rows of a kv head take
 Tiles tiles_of(int R) {
   const int all = (R + 15) / 16, blocks = (all + MAX_TILES - 1) / MAX_TILES;
   return {(all + blocks - 1) / blocks, blocks};
 }
-int units_aimed(int R, int G) {
-  const int64_t per = (int64_t)G * tiles_of(R).blocks;
-  return per < AIM ? (int)(AIM / per) : 1;
+// workers of a kv head and row block: the compute units hold them all at once
+int workers_aimed(int R, int G, bool wide_f32) {
+  const Tiles tiles = tiles_of(R);
+  const int64_t per = (int64_t)G * tiles.blocks, slots = 256 * RESIDENT(tiles.each, wide_f32 ? 2 : 1) * (tiles.each == 1 ? ROUNDS1 : ROUNDS3);
+  return per < slots ? (int)(slots / per) : 1;
 }
 
 }  // namespace
 
-// Partial sums: only entries of several units have them, and those are at most twice the units aimed at.
+// Sums of parts: a worker has at most two (see paged_index.h).
 size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G) {
   const int64_t R = (int64_t)M * (H / G);
-  return (size_t)2 * units_aimed((int)R, G) * G * R * (128 + 2) * sizeof(float);
+  return (size_t)2 * workers_aimed((int)R, G, false) * G * R * (128 + 2) * sizeof(float);
 }
 
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const int R = a.M * (a.H / a.G);
   const Tiles tiles = tiles_of(R);
-  a.target = units_aimed(R, a.G);
+  a.target = workers_aimed(R, a.G, !bf16 && a.d > 64);       // (never more than the workspace is made for)
   a.least = WAVES;
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
-  const int heads8 = (a.target + a.B) * a.G;
+  const int heads8 = a.target * a.G;
   const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(64 * WAVES);
   const bool tree = a.n_true != nullptr, narrow = !bf16 && a.d <= 64;
   {
@@ -527,13 +587,19 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
     else if (narrow) with(int_c<0>{}, int_c<1>{});
     else with(int_c<0>{}, int_c<2>{});
   }
-  // no entry can have two units: nothing to join
+  // no entry is long enough to be cut: nothing to join
   if ((a.bound + PAGED_BLOCK - 1) / PAGED_BLOCK <= a.least) return;
   ProfScope ps("paged_join", s);
-  const dim3 jg((unsigned)(a.H * a.M), (unsigned)a.B);
-  if (bf16) hipLaunchKernelGGL((paged_join_kernel<true, 128>), jg, dim3(256), 0, s, a);
-  else if (narrow) hipLaunchKernelGGL((paged_join_kernel<false, 64>), jg, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_join_kernel<false, 128>), jg, dim3(256), 0, s, a);
+  auto join = [&](auto bf_, auto hdp_) {
+    constexpr bool BF = decltype(bf_)::value != 0;
+    constexpr int HDP = decltype(hdp_)::value, MANY = 256 / (HDP / 4);
+    const int64_t all = (int64_t)a.H * a.M;
+    if (all * a.B <= 1024) hipLaunchKernelGGL((paged_join_kernel<BF, HDP, 1>), dim3((unsigned)all, (unsigned)a.B), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join_kernel<BF, HDP, MANY>), dim3((unsigned)((all + MANY - 1) / MANY), (unsigned)a.B), dim3(256), 0, s, a);
+  };
+  if (bf16) join(int_c<1>{}, int_c<128>{});
+  else if (narrow) join(int_c<0>{}, int_c<64>{});
+  else join(int_c<0>{}, int_c<128>{});
 }
 
 }  // namespace beagle

@@ -32,7 +32,7 @@ PAGED_HD PagedRows paged_rows(int n, int nt, int window, int sinks) {
     r.lead = (paged_min(sinks, r.nt) + PAGED_BLOCK - 1) / PAGED_BLOCK;
     r.skip = paged_max(paged_max(r.nt - window, 0) / PAGED_BLOCK - r.lead, 0);
   }
-  r.blocks = (n + PAGED_BLOCK - 1) / PAGED_BLOCK - r.skip;
+  r.blocks = paged_max((n + PAGED_BLOCK - 1) / PAGED_BLOCK - r.skip, 1);     // (an empty entry has one, of rows that nobody sees)
   return r;
 }
 PAGED_HD int paged_block(const PagedRows& r, int i) { return i < r.lead ? i : i + r.skip; }
@@ -45,14 +45,22 @@ PAGED_HD bool paged_all_seen(const PagedRows& r, int first, int count) {
   return first + count <= r.nt && (r.window == 0 || first + count <= r.sinks || first >= r.nt - r.window);
 }
 
-// Units: runs of `chunk` blocks of one entry, at least one per entry.  With chunk at least all / target there are at most
-// target + entries of them, and at most 2 * target belong to entries that have several.
-PAGED_HD int paged_chunk(int64_t all, int target, int least) {
-  int64_t c = (all + target - 1) / target;
-  if (c < least) c = least;
-  return c < (1 << 24) ? (int)c : 1 << 24;              // (no entry has more blocks: 2^28 rows)
+// Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs.  Worker w of n takes
+// blocks paged_cut(w) .. paged_cut(w + 1) - 1 of that row; an entry of up to `least` blocks is not cut but goes whole to the worker that has
+// its first block.  A worker so has at most two entries in part, its first and its last.
+PAGED_HD int paged_workers(int64_t all, int target, int least) {
+  const int64_t n = (all + least - 1) / least;
+  return n < target ? (int)n : target;
 }
-PAGED_HD int paged_units(int blocks, int chunk) { return paged_max((blocks + chunk - 1) / chunk, 1); }
+PAGED_HD int64_t paged_cut(int64_t all, int n, int w) { return all * w / n; }
+PAGED_HD int paged_worker_of(int64_t all, int n, int64_t block) { return (int)(((block + 1) * n - 1) / all); }
+// blocks [from, to) of an entry that starts at `start` and has `blocks` fall to the worker of [lo, hi)
+struct PagedShare { int from, to; };
+PAGED_HD PagedShare paged_share(int64_t start, int blocks, int64_t lo, int64_t hi, int least) {
+  if (blocks <= least) return start >= lo && start < hi ? PagedShare{0, blocks} : PagedShare{0, 0};
+  const int64_t a = start < lo ? lo : start, b = start + blocks < hi ? start + blocks : hi;
+  return a < b ? PagedShare{(int)(a - start), (int)(b - start)} : PagedShare{0, 0};
+}
 
 // page of a row that paged_seen accepts (any other: -1); -1 where the table names no page of the pool
 PAGED_HD int paged_page(const int32_t* table, int row, bool seen, int shift, int n_pages) {
