@@ -37,14 +37,12 @@ __device__ __align__(16) const unsigned char zero_row[1024] = {};
 struct Entry { int slot, blocks, upto; PagedRows rows; };
 __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
   Entry e;
-  e.slot = -1; e.blocks = 0;
-  e.rows = PagedRows{};
-  if (b < a.B) {
-    const int nt = a.n_true ? a.n_true[b] : INT32_MAX;
-    e.slot = paged_slot(a.c, a.slots, b);
-    e.rows = paged_rows(min(paged_len(a.c, e.slot), a.bound), nt, a.window, a.sinks);
-    e.blocks = e.rows.blocks;
-  }
+  const int at = min(b, a.B - 1);
+  const int nt = a.n_true ? a.n_true[at] : INT32_MAX;
+  e.slot = paged_slot(a.c, a.slots, at);
+  const int len = a.c.lens[max(e.slot, 0)];
+  e.rows = paged_rows(min(e.slot < 0 ? 0 : paged_clamped(len, a.c.W, a.c.shift), a.bound), nt, a.window, a.sinks);
+  e.blocks = b < a.B ? e.rows.blocks : 0;
   e.upto = e.blocks;                       // (64 entries of 2^23 blocks: fits)
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
@@ -110,7 +108,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       const int piece = (4 * j + g4) * 16;
-      q[t][j] = r < R && piece < a.d * E ? *(const u32x4*)(p + piece) : u32x4{0, 0, 0, 0};
+      q[t][j] = *(const u32x4*)(r < R && (BF16 || piece < a.d * E) ? p + piece : (const char*)zero_row);
     }
   }
   f32x4 acc[RT][S::NA];
@@ -309,6 +307,18 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
         }
       }
     }
+    // the step's rows in a query's word of bits: true ones set, drafted ones as the tree has them
+    [[maybe_unused]] uint32_t bits[RT];
+    if constexpr (TREE) {
+      const int off = base - rows.nt, word = off >> 5;           // (rounds down)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const uint32_t* row = a.tree + ((int64_t)b * a.M + min(qm[t], a.M - 1)) * a.words;
+        const bool lo_in = (unsigned)word < (unsigned)a.words, hi_in = (unsigned)(word + 1) < (unsigned)a.words;
+        const uint32_t lo = lo_in ? row[word] : 0, hi = hi_in ? row[word + 1] : 0;
+        bits[t] = (uint32_t)((((uint64_t)hi << 32) | lo) >> (off & 31)) | (off <= -32 ? ~0u : off < 0 ? (1u << -off) - 1 : 0);
+      }
+    }
     scores();
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -317,12 +327,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           bool see = seen[kt][i];
-          if constexpr (TREE) {
-            const int bit = base + 16 * kt + 4 * g4 + i - rows.nt;
-            if (see && bit >= 0)
-              see = qm[t] < a.M && (bit >> 5) < a.words &&
-                    (a.tree[((int64_t)b * a.M + qm[t]) * a.words + (bit >> 5)] >> (bit & 31) & 1u);
-          }
+          if constexpr (TREE) see = see && (bits[t] >> (16 * kt + 4 * g4 + i) & 1u);
           if (!see) sc[t][kt][i] = -INFINITY;
         }
     probabilities();

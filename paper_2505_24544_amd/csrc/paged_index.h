@@ -64,8 +64,8 @@ PAGED_HD PagedShare paged_share(int64_t start, int blocks, int64_t lo, int64_t h
 
 // page of a row that paged_seen accepts (any other: -1); -1 where the table names no page of the pool
 PAGED_HD int paged_page(const int32_t* table, int row, bool seen, int shift, int n_pages) {
-  const int p = seen ? table[row >> shift] : -1;
-  return (unsigned)p < (unsigned)n_pages ? p : -1;
+  const int p = table[seen ? row >> shift : 0];          // (no branch: a lane without a row reads the first entry for nothing)
+  return seen && (unsigned)p < (unsigned)n_pages ? p : -1;
 }
 
 }  // namespace beagle
