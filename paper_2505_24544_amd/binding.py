@@ -139,13 +139,15 @@ def make_paged_cache(k_pages, v_pages, page_table, lens, refs) -> beagle_paged_c
         raise ValueError("k_pages and v_pages are [P, page_rows, G, d] of one type")
     if page_table.dim() != 2 or tuple(lens.shape) != tuple(page_table.shape[:1]) or tuple(refs.shape) != tuple(k_pages.shape[:1]):
         raise ValueError("page_table is [N, slot_pages], lens [N], refs [P]")
-    _device(k_pages, v_pages, page_table, lens, refs)
-    for t in (page_table, lens, refs):
-        _ints(t)
+    import torch
+    if {str(x.dtype) for x in (page_table, lens, refs)} != {"torch.int32"}:
+        raise ValueError("page_table, lens and refs are torch.int32")
+    if len({x.device for x in (k_pages, v_pages, page_table, lens, refs)}) > 1:
+        raise ValueError("the cache's tensors are on different devices")
     c = beagle_paged_cache(C.sizeof(beagle_paged_cache), k_pages.shape[0], k_pages.shape[1], page_table.shape[0],
                            page_table.shape[1], 0, *(_ptr(t) for t in (k_pages, v_pages, page_table, lens, refs)))
-    c.rows = tuple(k_pages.shape[2:])       # [G, d] of a row, its element type and its device: checked against a call's tensors
-    c.dtype, c.device = k_pages.dtype, k_pages.device
+    # what a call's tensors are checked against: rows [G, d] of this type on this device
+    c.rows, c.dtype, c.device, c.whole = tuple(k_pages.shape[2:]), k_pages.dtype, k_pages.device, (torch.int32, torch.uint32)
     return c
 
 
@@ -271,24 +273,6 @@ def _stream(stream):
         import torch
         return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _device(*tensors):
-    """The one device that the tensors among the arguments are on, or None."""
-    seen = {t.device for t in tensors if t is not None and not isinstance(t, int)}
-    if len(seen) > 1:
-        raise ValueError("tensor arguments are on different devices: %s" % ", ".join(sorted(str(d) for d in seen)))
-    return seen.pop() if seen else None
-
-
-def _ints(t, count=None):
-    """Address of a tensor of 32-bit whole numbers (of `count` of them), or of None or an address as it is."""
-    if t is not None and not isinstance(t, int):
-        if str(t.dtype) not in ("torch.int32", "torch.uint32"):
-            raise ValueError("an index argument is a tensor of 32-bit whole numbers, not of %s" % t.dtype)
-        if count is not None and t.numel() != count:
-            raise ValueError("an index argument has %d values, %d are needed" % (t.numel(), count))
-    return _ptr(t)
 
 
 def _nbytes(ws):
@@ -446,52 +430,73 @@ def beagle_xattn_kv_append(desc, x_new, wk, wv, k_cache, v_cache, pos, workspace
     return _check(st, "beagle_xattn_kv_append", check)
 
 
-def _paged_rows(desc, t, heads):
-    """Address of a tensor of desc.batch * desc.seq_q rows of `heads` heads (0: of width desc.hidden) in desc's type."""
-    if t is not None and not isinstance(t, int):
-        want = "torch.bfloat16" if desc.io_dtype == BEAGLE_BF16 else "torch.float32"
-        if str(t.dtype) != want:
-            raise ValueError("a tensor of %s is needed, not of %s" % (want, t.dtype))
-        if t.numel() != desc.batch * desc.seq_q * (heads * desc.head_dim if heads else desc.hidden):
-            raise ValueError("a tensor of shape %s does not hold batch * seq_q rows" % (tuple(t.shape),))
-    return _ptr(t)
+class _Paged:
+    """The tensors of one paged call, checked against its descriptor and its cache; addresses and None pass as they are."""
 
-
-def _paged_lse(desc, t):
-    if t is not None and not isinstance(t, int) and (str(t.dtype) != "torch.float32" or t.numel() != desc.batch * desc.n_q_heads * desc.seq_q):
-        raise ValueError("lse is a torch.float32 tensor [batch, heads, seq_q]")
-    return _ptr(t)
-
-
-def _paged_call(name, desc, cache, tensors, args, workspace, workspace_bytes, stream, check):
-    """One paged entry point: everything on the cache's device, and by default on that device's current stream."""
-    where = getattr(cache, "device", None)
-    dev = _device(workspace, *tensors)
-    if where is not None and dev is not None and dev != where:
-        raise ValueError("tensor arguments are on %s, the cache is on %s" % (dev, where))
-    dev = where if dev is None else dev
-    if dev is not None and dev.type != "cuda":
-        raise ValueError("tensor arguments are on %s, not on a GPU" % dev)
-    if cache is not None and where is not None and desc is not None:
-        if cache.rows != (desc.n_kv_heads, desc.head_dim) or \
-                str(cache.dtype) != ("torch.bfloat16" if desc.io_dtype == BEAGLE_BF16 else "torch.float32"):
+    def __init__(self, desc, cache):
+        self.dev = getattr(cache, "device", None)         # (None: a cache made of addresses)
+        self.n = desc.batch * desc.seq_q
+        self.desc = desc
+        if self.dev is None:
+            import torch
+            self.dtype, self.whole = torch.bfloat16 if desc.io_dtype == BEAGLE_BF16 else torch.float32, (torch.int32, torch.uint32)
+            return
+        self.dtype, self.whole = cache.dtype, cache.whole
+        if cache.rows != (desc.n_kv_heads, desc.head_dim) or self.dtype.itemsize != (2 if desc.io_dtype == BEAGLE_BF16 else 4):
             raise ValueError("the cache holds rows %s of %s, not what the descriptor says" % (cache.rows, cache.dtype))
 
-    def call():
-        return getattr(lib(), name)(C.byref(desc) if desc is not None else None, C.byref(cache) if cache is not None else None, *args,
-                                    _ptr(workspace), _nbytes(workspace) if workspace_bytes is None else workspace_bytes,
-                                    _stream(stream))
-    if dev is not None:
-        import torch
-        if dev.index != torch.cuda.current_device():
-            with torch.cuda.device(dev):
-                return _check(call(), name, check)
-    return _check(call(), name, check)
+    def _at(self, t, count):
+        if not t.is_cuda or (self.dev is not None and t.device != self.dev):
+            raise ValueError("a tensor argument is on %s, the cache is on %s" % (t.device, self.dev))
+        if t.numel() != count and count >= 0:
+            raise ValueError("a tensor of shape %s does not hold the %d values of the call" % (tuple(t.shape), count))
+        return _ptr(t)
 
+    def ints(self, t, count):
+        if t is None or isinstance(t, int):
+            return t
+        if t.dtype not in self.whole:
+            raise ValueError("an index argument is a tensor of 32-bit whole numbers, not of %s" % t.dtype)
+        return self._at(t, count)
 
-def _view(desc, slots, n_true, tree_mask, mask_words, window, sinks):
-    B, M = desc.batch, desc.seq_q
-    return (_ints(slots, B), _ints(n_true, B), _ints(tree_mask, B * M * int(mask_words)), int(mask_words), int(window), int(sinks))
+    def rows(self, t, width):
+        """[batch, seq_q, width] of the cache's type"""
+        if t is None or isinstance(t, int):
+            return t
+        if t.dtype != self.dtype:
+            raise ValueError("a tensor of %s is needed, not of %s" % (self.dtype, t.dtype))
+        return self._at(t, self.n * width)
+
+    def weight(self, t, count):
+        if t is None or isinstance(t, int):
+            return t
+        if t.dtype != self.dtype:
+            raise ValueError("a tensor of %s is needed, not of %s" % (self.dtype, t.dtype))
+        return self._at(t, count)
+
+    def lse(self, t):
+        if t is None or isinstance(t, int):
+            return t
+        if not t.dtype.is_floating_point or t.dtype.itemsize != 4:
+            raise ValueError("lse is a torch.float32 tensor [batch, heads, seq_q]")
+        return self._at(t, self.n * self.desc.n_q_heads)
+
+    def view(self, slots, n_true, tree_mask, mask_words, window, sinks):
+        B = self.desc.batch
+        return (self.ints(slots, B), self.ints(n_true, B), self.ints(tree_mask, self.n * int(mask_words)), int(mask_words),
+                int(window), int(sinks))
+
+    def call(self, name, cache, args, workspace, workspace_bytes, stream, check):
+        """By default on the current stream of the cache's device, which is made the current one meanwhile."""
+        ws = workspace if workspace is None or isinstance(workspace, int) else self._at(workspace, -1)
+        nbytes = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+        fn = getattr(lib(), name)
+        if self.dev is not None:
+            import torch
+            if self.dev.index != torch.cuda.current_device():
+                with torch.cuda.device(self.dev):
+                    return _check(fn(C.byref(self.desc), C.byref(cache), *args, ws, nbytes, _stream(stream)), name, check)
+        return _check(fn(C.byref(self.desc), C.byref(cache), *args, ws, nbytes, _stream(stream)), name, check)
 
 
 def beagle_xattn_paged_workspace_bytes(desc, cache, which) -> int:
@@ -500,48 +505,50 @@ def beagle_xattn_paged_workspace_bytes(desc, cache, which) -> int:
 
 def beagle_xattn_paged_attend(desc, cache, q, slots, n_true, tree_mask, mask_words, window, sinks, o, lse, workspace, stream=None,
                               *, workspace_bytes=None, check=True) -> int:
-    args = (_paged_rows(desc, q, desc.n_q_heads), *_view(desc, slots, n_true, tree_mask, mask_words, window, sinks),
-            _paged_rows(desc, o, desc.n_q_heads), _paged_lse(desc, lse))
-    return _paged_call("beagle_xattn_paged_attend", desc, cache, (q, slots, n_true, tree_mask, o, lse), args, workspace,
-                       workspace_bytes, stream, check)
+    c = _Paged(desc, cache)
+    width = desc.n_q_heads * desc.head_dim
+    args = (c.rows(q, width), *c.view(slots, n_true, tree_mask, mask_words, window, sinks), c.rows(o, width), c.lse(lse))
+    return c.call("beagle_xattn_paged_attend", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_paged_append(desc, cache, slots, pos, n_new, k_new, v_new, short_pages, workspace, stream=None, *,
                               workspace_bytes=None, check=True) -> int:
-    B = desc.batch
-    args = (_ints(slots, B), _ints(pos, B), _ints(n_new, B), _paged_rows(desc, k_new, desc.n_kv_heads),
-            _paged_rows(desc, v_new, desc.n_kv_heads), _ints(short_pages, 1))
-    return _paged_call("beagle_xattn_paged_append", desc, cache, (slots, pos, n_new, k_new, v_new, short_pages), args, workspace,
-                       workspace_bytes, stream, check)
+    c = _Paged(desc, cache)
+    B, width = desc.batch, desc.n_kv_heads * desc.head_dim
+    args = (c.ints(slots, B), c.ints(pos, B), c.ints(n_new, B), c.rows(k_new, width), c.rows(v_new, width), c.ints(short_pages, 1))
+    return c.call("beagle_xattn_paged_append", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_paged_fork(desc, cache, dst, src, rows, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
-    args = tuple(_ints(t, desc.batch) for t in (dst, src, rows))
-    return _paged_call("beagle_xattn_paged_fork", desc, cache, (dst, src, rows), args, workspace, workspace_bytes, stream, check)
+    c = _Paged(desc, cache)
+    args = (c.ints(dst, desc.batch), c.ints(src, desc.batch), c.ints(rows, desc.batch))
+    return c.call("beagle_xattn_paged_fork", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_paged_compact(desc, cache, into, short_pages, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
-    a, b = getattr(cache, "device", None), getattr(into, "device", None)
-    if a is not None and b is not None and (a != b or cache.rows != into.rows or cache.dtype != into.dtype):
+    c = _Paged(desc, cache)
+    if c.dev is not None and getattr(into, "device", None) is not None and (c.dev != into.device or cache.rows != into.rows or c.dtype != into.dtype):
         raise ValueError("the two pools hold different rows, or are on different devices")
-    args = (C.byref(into) if into is not None else None, _ints(short_pages, 1))
-    return _paged_call("beagle_xattn_paged_compact", desc, cache, (short_pages,), args, workspace, workspace_bytes, stream, check)
+    args = (C.byref(into), c.ints(short_pages, 1))
+    return c.call("beagle_xattn_paged_compact", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_draft_step_paged(desc, cache, x_draft, wq, wo, slots, n_true, tree_mask, mask_words, window, sinks, y, lse,
                                   workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
-    args = (_paged_rows(desc, x_draft, 0), _ptr(wq), _ptr(wo), *_view(desc, slots, n_true, tree_mask, mask_words, window, sinks),
-            _paged_rows(desc, y, 0), _paged_lse(desc, lse))
-    return _paged_call("beagle_xattn_draft_step_paged", desc, cache, (x_draft, wq, wo, slots, n_true, tree_mask, y, lse), args,
-                       workspace, workspace_bytes, stream, check)
+    c = _Paged(desc, cache)
+    D, HD = desc.hidden, desc.n_q_heads * desc.head_dim
+    args = (c.rows(x_draft, D), c.weight(wq, D * HD), c.weight(wo, D * HD),
+            *c.view(slots, n_true, tree_mask, mask_words, window, sinks), c.rows(y, D), c.lse(lse))
+    return c.call("beagle_xattn_draft_step_paged", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_kv_append_paged(desc, cache, x_new, wk, wv, slots, pos, n_new, short_pages, workspace, stream=None, *,
                                  workspace_bytes=None, check=True) -> int:
-    B = desc.batch
-    args = (_paged_rows(desc, x_new, 0), _ptr(wk), _ptr(wv), _ints(slots, B), _ints(pos, B), _ints(n_new, B), _ints(short_pages, 1))
-    return _paged_call("beagle_xattn_kv_append_paged", desc, cache, (x_new, wk, wv, slots, pos, n_new, short_pages), args, workspace,
-                       workspace_bytes, stream, check)
+    c = _Paged(desc, cache)
+    B, D, GD = desc.batch, desc.hidden, desc.n_kv_heads * desc.head_dim
+    args = (c.rows(x_new, D), c.weight(wk, D * GD), c.weight(wv, D * GD), c.ints(slots, B), c.ints(pos, B), c.ints(n_new, B),
+            c.ints(short_pages, 1))
+    return c.call("beagle_xattn_kv_append_paged", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_workspace_bytes(desc, which) -> int:

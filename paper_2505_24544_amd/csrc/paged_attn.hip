@@ -26,7 +26,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4;
 // workgroups that fit on a compute unit at a time (registers)
-constexpr int RESIDENT(int RT, int NH) { return RT == 1 && NH == 1 ? 3 : RT <= 2 ? 2 : 1; }
+// Workgroups that a compute unit holds at a time, and that the registers are made for.  Eight waves with 16 KB of rows on the way each keep
+// memory busy; three workgroups of one tile (168 registers, some of them spilled) took 113 us where two take 95 (48
+// sequences of up to 4096 rows, 8 kv heads), and more workgroups than fit, taken in turn, 108.
+constexpr int RESIDENT = 2;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // what rows that nobody sees are read from: their V must be a number (0 * NaN is NaN)
@@ -99,11 +102,9 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 
   // queries: column l16 of tile t is row r of this kv head's R = M * rep rows
   u32x4 q[RT][S::NJ];
-  int qm[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int r = (rb * RT + t) * 16 + l16, m = r / rep;
-    qm[t] = m;
     const char* p = (const char*)a.q + ((((int64_t)b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
@@ -126,10 +127,6 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   const int steps = last > first + wave ? (last - first - wave + WAVES - 1) / WAVES * SUB : 0;
   const int shift = a.c.shift;
   auto base_of = [&](int s) { return paged_block(rows, first + wave + s / SUB * WAVES) * PAGED_BLOCK + s % SUB * S::KROWS; };
-  auto next_whole = [&](int s) BEAGLE_INLINE_LAMBDA {          // the first step from s on whose rows every query sees
-    while (s < steps && !paged_all_seen(rows, base_of(s), S::KROWS)) ++s;
-    return s;
-  };
   u32x4 k[S::KT][S::NJ], v[S::NV][NH];
   f32x4 sc[RT][S::KT];
   float p[RT][S::KT][4];
@@ -207,133 +204,124 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
     }
   };
 
-  // ---- steps whose rows every query sees: the rows of the next one travel while this one is computed, its page numbers a
-  // step further ahead.  A lane holds one K row of each tile (l16) and four V rows (4 g4 ..; one page: its rows are a multiple of four).
-  // Where a page number is none, the step is left for below.
+  // ---- a step's rows: a lane holds one K row of each tile (l16) and four V rows (4 g4 ..; one page: its rows are a multiple of four).
+  // Rows that nobody sees, or whose page number is none, are read from zero_row, without a branch.
   struct Pages { int k[S::KT], v[S::KT]; };
   auto look = [&](int s) BEAGLE_INLINE_LAMBDA {
     Pages h;
-    const int base = base_of(s);
+    const int base = base_of(min(s, steps - 1)), last_row = max(rows.n - 1, 0);
 #pragma unroll
-    for (int t = 0; t < S::KT; ++t) { h.k[t] = table[(base + 16 * t + l16) >> shift]; h.v[t] = table[(base + 16 * t + 4 * g4) >> shift]; }
+    for (int t = 0; t < S::KT; ++t) {
+      h.k[t] = table[min(base + 16 * t + l16, last_row) >> shift];
+      h.v[t] = table[min(base + 16 * t + 4 * g4, last_row) >> shift];
+    }
     return h;
   };
-  auto usable = [&](Pages& h) BEAGLE_INLINE_LAMBDA {
+  // bit 4 t + i: row 16 t + 4 g4 + i is seen; bit 16 + t: row 16 t + l16
+  struct Step { int base; uint32_t seen; bool masked; };
+  auto judge = [&](const Pages& h, int s) BEAGLE_INLINE_LAMBDA {
+    Step st;
+    st.base = base_of(s);
+    st.seen = ~0u;
+    const bool all = paged_all_seen(rows, st.base, S::KROWS);
+    if (!all) {
+      st.seen = 0;
+#pragma unroll
+      for (int t = 0; t < S::KT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.seen |= (uint32_t)paged_seen(rows, st.base + 16 * t + 4 * g4 + i) << (4 * t + i);
+        st.seen |= (uint32_t)paged_seen(rows, st.base + 16 * t + l16) << (16 + t);
+      }
+    }
     bool bad = false;
 #pragma unroll
     for (int t = 0; t < S::KT; ++t) {
-      if ((unsigned)h.k[t] >= (unsigned)a.c.P) { bad = true; h.k[t] = 0; }
-      if ((unsigned)h.v[t] >= (unsigned)a.c.P) { bad = true; h.v[t] = 0; }
+      if ((unsigned)h.v[t] >= (unsigned)a.c.P) { st.seen &= ~(15u << 4 * t); bad = true; }
+      if ((unsigned)h.k[t] >= (unsigned)a.c.P) { st.seen &= ~(1u << (16 + t)); bad = true; }
     }
-    return __ballot(bad) == 0;
+    st.masked = __ballot(bad) != 0 || !all;
+    return st;
   };
-  auto request_k = [&](const Pages& h, int base) BEAGLE_INLINE_LAMBDA {
+  auto request_k = [&](const Pages& h, const Step& st) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < S::KT; ++t) {
-      const char* src = kbase + (((int64_t)h.k[t] << shift) + ((base + 16 * t + l16) & in_page)) * row_bytes + 16 * g4;
+      const char* src = kbase + (((int64_t)h.k[t] << shift) + ((st.base + 16 * t + l16) & in_page)) * row_bytes + 16 * g4;
+      if (!(st.seen >> (16 + t) & 1)) src = (const char*)zero_row;
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) k[t][j] = *(const u32x4*)(BF16 || (4 * j + g4) * 16 < a.d * E ? src + 64 * j : (const char*)zero_row);
     }
   };
-  auto request_v = [&](const Pages& h, int base) BEAGLE_INLINE_LAMBDA {
+  auto request_v = [&](const Pages& h, const Step& st) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < S::KT; ++t) {
-      const char* src = vbase + (((int64_t)h.v[t] << shift) + ((base + 16 * t + 4 * g4) & in_page)) * row_bytes + 16 * l16;
+      const char* src = vbase + (((int64_t)h.v[t] << shift) + ((st.base + 16 * t + 4 * g4) & in_page)) * row_bytes + 16 * l16;
 #pragma unroll
       for (int i = 0; i < 4; ++i, src += row_bytes)
 #pragma unroll
-        for (int n = 0; n < NH; ++n)
-          v[4 * t + i][n] = *(const u32x4*)(BF16 || (16 * n + l16) * 16 < a.d * E ? src + 256 * n : (const char*)zero_row);
+        for (int n = 0; n < NH; ++n) {
+          const bool there = (st.seen >> (4 * t + i) & 1) && (BF16 || (16 * n + l16) * 16 < a.d * E);
+          v[4 * t + i][n] = *(const u32x4*)(there ? src + 256 * n : (const char*)zero_row);
+        }
     }
   };
-  int s = next_whole(0);
-  if (s < steps) {
-    Pages here = look(s), there;
-    int s1 = next_whole(s + 1);
-    bool ok = usable(here);
-    request_k(here, base_of(s));
-    if (s1 < steps) there = look(s1);
-    request_v(here, base_of(s));
-    while (true) {
-      scores();
-      const bool more = s1 < steps;
-      bool ok1 = false;
-      int s2 = s1;
-      Pages then = there;
-      if (more) {
-        ok1 = usable(there);
-        request_k(there, base_of(s1));
-        s2 = next_whole(s1 + 1);
-        if (s2 < steps) then = look(s2);
-      }
-      if (ok) {
-        probabilities();
-        values();
-      }
-      if (!more) break;
-      request_v(there, base_of(s1));
-      s = s1; s1 = s2; ok = ok1; there = then;
-    }
-  }
-
-  // ---- the others, row by row: rows behind the end, at a window's edges, under the tree, on pages that are none
-  auto page_of = [&](int row) { return paged_page(table, row, paged_seen(rows, row), shift, a.c.P); };
-  for (int i1 = 0; i1 < steps; ++i1) {
-    const int base = base_of(i1);
-    if (base >= rows.n) break;
-    if (paged_all_seen(rows, base, S::KROWS)) {
-      Pages h = look(i1);
-      if (usable(h)) continue;
-    }
-    bool seen[S::KT][4];
-#pragma unroll
-    for (int t = 0; t < S::KT; ++t) {
-      const int row = base + 16 * t + l16, pk = page_of(row);
-      const char* src = pk >= 0 ? kbase + (((int64_t)pk << shift) + (row & in_page)) * row_bytes : (const char*)zero_row;
-#pragma unroll
-      for (int j = 0; j < S::NJ; ++j) {
-        const int piece = (4 * j + g4) * 16;
-        k[t][j] = *(const u32x4*)(BF16 || piece < a.d * E ? src + piece : (const char*)zero_row);
-      }
-      const int r0 = base + 16 * t + 4 * g4, pv = paged_page(table, r0, r0 < rows.n, shift, a.c.P);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        seen[t][i] = pv >= 0 && paged_seen(rows, r0 + i);
-        const char* from = seen[t][i] ? vbase + (((int64_t)pv << shift) + ((r0 + i) & in_page)) * row_bytes : (const char*)zero_row;
-#pragma unroll
-        for (int n = 0; n < NH; ++n) {
-          const int piece = (16 * n + l16) * 16;
-          v[4 * t + i][n] = *(const u32x4*)(BF16 || piece < a.d * E ? from + piece : (const char*)zero_row);
-        }
-      }
-    }
-    // the step's rows in a query's word of bits: true ones set, drafted ones as the tree has them
-    [[maybe_unused]] uint32_t bits[RT];
-    if constexpr (TREE) {
-      const int off = base - rows.nt, word = off >> 5;           // (rounds down)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const uint32_t* row = a.tree + ((int64_t)b * a.M + min(qm[t], a.M - 1)) * a.words;
-        const bool lo_in = (unsigned)word < (unsigned)a.words, hi_in = (unsigned)(word + 1) < (unsigned)a.words;
-        const uint32_t lo = lo_in ? row[word] : 0, hi = hi_in ? row[word + 1] : 0;
-        bits[t] = (uint32_t)((((uint64_t)hi << 32) | lo) >> (off & 31)) | (off <= -32 ? ~0u : off < 0 ? (1u << -off) - 1 : 0);
-      }
-    }
-    scores();
+  auto hide = [&](const Step& st) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int kt = 0; kt < S::KT; ++kt)
+      for (int e = 0; e < 4 * S::KT; ++e)
+        if (!(st.seen >> e & 1)) sc[t][e / 4][e % 4] = -INFINITY;
+  };
+  // Steps of true rows: the rows of the next step travel while this one is computed, its page numbers a step further ahead.
+  int plain = steps;
+  if constexpr (TREE)
+    while (plain > 0 && base_of(plain - 1) + S::KROWS > rows.nt) --plain;
+  [[maybe_unused]] Pages tail;
+  if (TREE && plain < steps) tail = look(plain);
+  if (plain > 0) {
+    Pages next = look(0);
+    Step st = judge(next, 0);
+    request_k(next, st);
+    request_v(next, st);
+    next = look(1);
+    for (int s = 0; s < plain; ++s) {
+      scores();
+      Step ahead = st;
+      const Pages now = next;
+      if (s + 1 < plain) {
+        ahead = judge(now, s + 1);
+        request_k(now, ahead);
+        next = look(s + 2);
+      }
+      if (st.masked) hide(st);
+      probabilities();
+      values();
+      if (s + 1 < plain) request_v(now, ahead);
+      st = ahead;
+    }
+  }
+  if constexpr (TREE)
+    for (int s = plain; s < steps; ++s) {
+      if (s > plain) tail = look(s);
+      const Step st = judge(tail, s);
+      request_k(tail, st);
+      request_v(tail, st);
+      scores();
+      hide(st);
+      // the step's rows in a query's word of bits: true ones set, drafted ones as the tree has them
+      const int off = st.base - rows.nt, word = off >> 5;          // (rounds down)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          bool see = seen[kt][i];
-          if constexpr (TREE) see = see && (bits[t] >> (16 * kt + 4 * g4 + i) & 1u);
-          if (!see) sc[t][kt][i] = -INFINITY;
-        }
-    probabilities();
-    // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
-    // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
-    if constexpr (TREE) {
+      for (int t = 0; t < RT; ++t) {
+        const uint32_t* row = a.tree + ((int64_t)b * a.M + min(((rb * RT + t) * 16 + l16) / rep, a.M - 1)) * a.words;
+        const bool lo_in = (unsigned)word < (unsigned)a.words, hi_in = (unsigned)(word + 1) < (unsigned)a.words;
+        const uint32_t lo = lo_in ? row[word] : 0, hi = hi_in ? row[word + 1] : 0;
+        const uint32_t bits = (uint32_t)((((uint64_t)hi << 32) | lo) >> (off & 31)) | (off <= -32 ? ~0u : off < 0 ? (1u << -off) - 1 : 0);
+#pragma unroll
+        for (int e = 0; e < 4 * S::KT; ++e)
+          if (!(bits >> (16 * (e / 4) + 4 * g4 + e % 4) & 1u)) sc[t][e / 4][e % 4] = -INFINITY;
+      }
+      probabilities();
+      // A drafted row that only some queries see may hold what is no number, which the others must not meet (0 * NaN is
+      // NaN).  The matrix instructions mix all rows into all queries, so such a step adds row by row where it is seen.
       unsigned top = 0;
 #pragma unroll
       for (int i = 0; i < S::NV; ++i)
@@ -345,36 +333,33 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
             top = max(top, x & 0x7f800000u);
             if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
           }
-      if (__ballot(top == 0x7f800000u)) {
-        float* mine = sh.o[wave][l16];       // (free until the end)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-#pragma unroll
-          for (int kt = 0; kt < S::KT; ++kt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[16 * kt + 4 * g4 + i] = sc[t][kt][i] == -INFINITY ? -1.f : p[t][kt][i];
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          for (int j = 0; j < S::KROWS; ++j) {
-            const float w = mine[j];
-            const int row = base + j, pg = page_of(row);
-            if (w == -1.f || pg < 0) continue;
-            const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
-#pragma unroll
-            for (int c = 0; c < S::NA; ++c)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
-                if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
-                else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
-              }
-          }
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
+      if (__ballot(top == 0x7f800000u) == 0) {
+        values();
         continue;
       }
+      float* mine = sh.o[wave][l16];             // (free until the end)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int e = 0; e < 4 * S::KT; ++e) mine[16 * (e / 4) + 4 * g4 + e % 4] = sc[t][e / 4][e % 4] == -INFINITY ? -1.f : p[t][e / 4][e % 4];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int j = 0; j < S::KROWS; ++j) {
+          const float w = mine[j];
+          const int row = st.base + j, pg = paged_page(table, row, paged_seen(rows, row), shift, a.c.P);
+          if (w == -1.f || pg < 0) continue;
+          const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
+#pragma unroll
+          for (int c = 0; c < S::NA; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int ch = BF16 ? 8 * (4 * g4 + i) + c : 64 * (c / 4) + 4 * (4 * g4 + i) + c % 4;
+              if constexpr (BF16) acc[t][c][i] += w * bf16_to_f32(((const bf16_t*)src)[ch]);
+              else if (ch < a.d) acc[t][c][i] += w * ((const float*)src)[ch];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
     }
-    values();
-  }
 
   // ---- the waves' shares, then the unit's result
 #pragma unroll
@@ -432,7 +417,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 // BF16: head width 128.  Float: NH = 1 for widths up to 64, 2 up to 128.  RT: tiles of 16 query rows that a workgroup takes.
 // TREE: rows from n_true on are seen as the tree's bits say.
 template <bool BF16, int NH, int RT, bool TREE>
-__global__ __launch_bounds__(64 * WAVES, RESIDENT(RT, NH)) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
+__global__ __launch_bounds__(64 * WAVES, RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
   __shared__ Merge<Shape<BF16, NH>::HDP, RT> shared;
   const int lane = threadIdx.x & 63;
   // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
@@ -538,20 +523,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
-#ifndef ROUNDS1
-#define ROUNDS1 1
-#define ROUNDS3 1
-#endif
-constexpr int MAX_TILES = 4;               // of 16 query rows that a workgroup takes
+constexpr int MAX_TILES = 2;               // of 16 query rows that a workgroup takes
 struct Tiles { int each, blocks; };        // tiles of a workgroup, workgroups that the rows of a kv head take
 Tiles tiles_of(int R) {
   const int all = (R + 15) / 16, blocks = (all + MAX_TILES - 1) / MAX_TILES;
   return {(all + blocks - 1) / blocks, blocks};
 }
 // workers of a kv head and row block: the compute units hold them all at once
-int workers_aimed(int R, int G, bool wide_f32) {
-  const Tiles tiles = tiles_of(R);
-  const int64_t per = (int64_t)G * tiles.blocks, slots = 256 * RESIDENT(tiles.each, wide_f32 ? 2 : 1) * (tiles.each == 1 ? ROUNDS1 : ROUNDS3);
+int workers_aimed(int R, int G) {
+  const int64_t per = (int64_t)G * tiles_of(R).blocks, slots = 256 * RESIDENT;
   return per < slots ? (int)(slots / per) : 1;
 }
 
@@ -560,13 +540,13 @@ int workers_aimed(int R, int G, bool wide_f32) {
 // Sums of parts: a worker has at most two (see paged_index.h).
 size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G) {
   const int64_t R = (int64_t)M * (H / G);
-  return (size_t)2 * workers_aimed((int)R, G, false) * G * R * (128 + 2) * sizeof(float);
+  return (size_t)2 * workers_aimed((int)R, G) * G * R * (128 + 2) * sizeof(float);
 }
 
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const int R = a.M * (a.H / a.G);
   const Tiles tiles = tiles_of(R);
-  a.target = workers_aimed(R, a.G, !bf16 && a.d > 64);       // (never more than the workspace is made for)
+  a.target = workers_aimed(R, a.G);
   a.least = WAVES;
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
@@ -584,9 +564,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
     };
     auto with = [&](auto bf_, auto nh_) {
       if (tiles.each == 1) go(bf_, nh_, int_c<1>{});
-      else if (tiles.each == 2) go(bf_, nh_, int_c<2>{});
-      else if (tiles.each == 3) go(bf_, nh_, int_c<3>{});
-      else go(bf_, nh_, int_c<4>{});
+      else go(bf_, nh_, int_c<2>{});
     };
     if (bf16) with(int_c<1>{}, int_c<1>{});
     else if (narrow) with(int_c<0>{}, int_c<1>{});

@@ -1,6 +1,6 @@
 // Host build of the paged cache's index code, under sanitizers.  Reads lines of whole numbers, prints what the code says:
 //   rows n nt window sinks   -> number of blocks, then for every row 0 .. n + 40: counted blocks that hold it * 4 + seen * 2 + (its block of 32 is all seen)
-//   units target least len.. -> chunk, then the units of every entry
+//   workers target least blocks.. -> their number, (worker, entry, from, to) of every share, (first, last) worker of every entry
 //   page n_pages shift row seen entry.. -> the page
 //   slot s n_slots len slot_pages shift -> slot, clamped length, its pages
 #include <cstdio>
@@ -30,12 +30,19 @@ int main() {
           std::printf(" %d", hold.at(row) * 4 + paged_seen(r, row) * 2 + paged_all_seen(r, row / 32 * 32, 32));
       }
       std::printf("\n");
-    } else if (what == "units") {
+    } else if (what == "workers") {
+      std::vector<long long> start;
       long long all = 0;
-      for (size_t i = 2; i < x.size(); ++i) all += (x[i] + PAGED_BLOCK - 1) / PAGED_BLOCK;
-      const int chunk = paged_chunk(all, (int)x[0], (int)x[1]);
-      std::printf("%d", chunk);
-      for (size_t i = 2; i < x.size(); ++i) std::printf(" %d", paged_units((int)((x[i] + PAGED_BLOCK - 1) / PAGED_BLOCK), chunk));
+      for (size_t i = 2; i < x.size(); ++i) { start.push_back(all); all += x[i]; }
+      const int n = paged_workers(all, (int)x[0], (int)x[1]);
+      std::printf("%d", n);
+      for (int w = 0; w < n; ++w)
+        for (size_t i = 2; i < x.size(); ++i) {
+          const PagedShare s = paged_share(start[i - 2], (int)x[i], paged_cut(all, n, w), paged_cut(all, n, w + 1), (int)x[1]);
+          if (s.from < s.to) std::printf(" %d %d %d %d", w, (int)i - 2, s.from, s.to);
+        }
+      for (size_t i = 2; i < x.size(); ++i)
+        std::printf(" %d %d", paged_worker_of(all, n, start[i - 2]), paged_worker_of(all, n, start[i - 2] + x[i] - 1));
       std::printf("\n");
     } else if (what == "page") {
       std::vector<int32_t> table(x.begin() + 4, x.end());

@@ -38,7 +38,7 @@ def test_rows_that_a_window_shows_and_the_blocks_that_hold_them(driver):
     for (n, nt, w, s), got in zip(cases, driver(["rows %d %d %d %d" % c for c in cases])):
         nt = min(max(nt, 0), n)
         seen = [j < n and (j >= nt or w == 0 or j < s or j >= nt - w) for j in range(n + 40)]
-        assert got[0] <= -(-n // 32)
+        assert 1 <= got[0] <= max(1, -(-n // 32))
         for j, v in enumerate(got[1:]):
             held, sees, whole = v // 4, bool(v & 2), bool(v & 1)
             assert sees == seen[j] and held <= 1, (n, nt, w, s, j)
@@ -50,18 +50,34 @@ def test_rows_that_a_window_shows_and_the_blocks_that_hold_them(driver):
     assert [g[0] for g in driver(["rows %d %d %d %d" % c for c in big])] == [2 ** 23, 2 ** 23, 1]
 
 
-def test_units_stay_within_what_the_workspace_holds(driver):
+def test_workers_share_all_blocks_evenly(driver):
     rng = random.Random(6)
-    cases = []
-    for _ in range(300):
-        lens = [int(2 ** rng.uniform(0, 15)) * rng.choice((0, 1, 1)) for _ in range(rng.choice((1, 2, 7, 64, 65, 300)))]
-        cases.append((rng.choice((1, 4, 25, 128, 1024)), rng.choice((1, 4, 8)), lens))
-    cases.append((1, 4, [2 ** 28] * 500))
-    for (target, least, lens), got in zip(cases, driver(["units %d %d %s" % (t, k, " ".join(map(str, n))) for t, k, n in cases])):
-        chunk, units = got[0], got[1:]
-        blocks = [-(-n // 32) for n in lens]
-        assert chunk >= least and units == [max(1, -(-b // chunk)) for b in blocks]
-        assert sum(units) <= target + len(lens) and sum(u for u in units if u > 1) <= 2 * target
+    cases = [(rng.choice((1, 4, 25, 64, 512)), rng.choice((1, 4, 8)), [max(1, int(2 ** rng.uniform(0, 9)) * rng.choice((0, 1, 1)))
+                                                                  for _ in range(rng.choice((1, 2, 7, 64, 65, 150)))]) for _ in range(200)]
+    cases.append((512, 4, [2 ** 23] * 300))
+    for (target, least, blocks), got in zip(cases, driver(["workers %d %d %s" % (t, k, " ".join(map(str, n))) for t, k, n in cases])):
+        n, ends = got[0], got[len(got) - 2 * len(blocks):]
+        shares = [got[i: i + 4] for i in range(1, len(got) - len(ends), 4)]
+        assert 1 <= n <= target and (n == target or n == -(-sum(blocks) // least))
+        parts = {}
+        for w, e, a, b in shares:
+            parts.setdefault(e, []).append((w, a, b))
+        even = sum(blocks) / n
+        work = [0] * n
+        for e, size in enumerate(blocks):
+            at = 0
+            for w, a, b in parts[e]:                    # in order, without a gap, from the first worker to the last
+                assert a == at
+                at, work[w] = b, work[w] + b - a
+            assert at == size
+            if size <= least:
+                assert len(parts[e]) == 1 and parts[e][0][0] == ends[2 * e]
+            else:
+                assert [p[0] for p in parts[e]] == list(range(ends[2 * e], ends[2 * e + 1] + 1))
+        assert max(work) <= even + 1 + least
+        for w in range(n):                              # at most one entry gone on with and one begun in part: two places for sums
+            part = [(a, b, e) for v, e, a, b in shares if v == w and b - a < blocks[e]]
+            assert sum(a > 0 for a, b, e in part) <= 1 and sum(a == 0 for a, b, e in part) <= 1
 
 
 def test_hostile_numbers(driver):
