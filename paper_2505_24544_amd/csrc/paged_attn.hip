@@ -24,7 +24,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int WAVES = 4;
 // workgroups that fit on a compute unit at a time (registers)
 // Workgroups that a compute unit holds at a time, and that the registers are made for.  Eight waves with 16 KB of rows on the way each keep
 // memory busy; three workgroups of one tile (168 registers, some of them spilled) took 113 us where two take 95 (48
@@ -35,6 +34,10 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 // what rows that nobody sees are read from: their V must be a number (0 * NaN is NaN)
 __device__ __align__(16) const unsigned char zero_row[1024] = {};
 
+// Addresses that are picked from two places are whole numbers until they are read: the compiler would not know a picked pointer
+// as one into global memory, and would wait for all loads wherever it needs one.
+typedef uint64_t addr_t;
+__device__ __forceinline__ u32x4 load16(addr_t p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
 // Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks of the row of all blocks that it
 // and the lanes before it have.
 struct Entry { int slot, blocks, upto; PagedRows rows; };
@@ -82,11 +85,11 @@ template <bool BF16, int NH> struct Shape {
   static constexpr int NA = BF16 ? 8 : 4 * NH;          // accumulator tiles
 };
 
-template <int HDP, int RT> struct Merge { float o[WAVES][16][HDP + 4], m[WAVES][RT * 16], l[WAVES][RT * 16]; };
+template <int HDP, int RT, int WAVES> struct Merge { float o[WAVES][16][HDP + 4], m[WAVES][RT * 16], l[WAVES][RT * 16]; };
 
-// One entry's blocks first .. last - 1 for one kv head and row block: the four waves take every fourth.
-template <bool BF16, int NH, int RT, bool TREE>
-__device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape<BF16, NH>::HDP, RT>& sh, int b, int slot, const PagedRows rows,
+// One entry's blocks first .. last - 1 for one kv head and row block: a wave takes every WAVES-th.
+template <bool BF16, int NH, int RT, bool TREE, int WAVES>
+__device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape<BF16, NH>::HDP, RT, WAVES>& sh, int b, int slot, const PagedRows rows,
                                              int first, int last, bool whole, int part, int head, int rb) {
   using S = Shape<BF16, NH>;
   constexpr int E = BF16 ? 2 : 4, HDP = S::HDP;              // bytes of a value; padded head width
@@ -95,8 +98,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int rep = a.H / a.G, R = a.M * rep;
   const int64_t row_bytes = (int64_t)a.G * a.d * E;
-  const char* kbase = (const char*)a.c.k + (int64_t)head * a.d * E;
-  const char* vbase = (const char*)a.c.v + (int64_t)head * a.d * E;
+  const addr_t kbase = (addr_t)a.c.k + (int64_t)head * a.d * E, vbase = (addr_t)a.c.v + (int64_t)head * a.d * E, zero = (addr_t)zero_row;
   const int32_t* table = a.c.table + (int64_t)max(slot, 0) * a.c.W;
   const int in_page = (1 << a.c.shift) - 1;
 
@@ -105,11 +107,11 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int r = (rb * RT + t) * 16 + l16, m = r / rep;
-    const char* p = (const char*)a.q + ((((int64_t)b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
+    const addr_t p = (addr_t)a.q + ((((int64_t)b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       const int piece = (4 * j + g4) * 16;
-      q[t][j] = *(const u32x4*)(r < R && (BF16 || piece < a.d * E) ? p + piece : (const char*)zero_row);
+      q[t][j] = load16(r < R && (BF16 || piece < a.d * E) ? p + piece : zero);
     }
   }
   f32x4 acc[RT][S::NA];
@@ -127,7 +129,9 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   const int steps = last > first + wave ? (last - first - wave + WAVES - 1) / WAVES * SUB : 0;
   const int shift = a.c.shift;
   auto base_of = [&](int s) { return paged_block(rows, first + wave + s / SUB * WAVES) * PAGED_BLOCK + s % SUB * S::KROWS; };
-  u32x4 k[S::KT][S::NJ], v[S::NV][NH];
+  u32x4 k[S::KT][S::NJ];
+  typedef u32x4 Values[S::NV][NH];
+  Values v;
   f32x4 sc[RT][S::KT];
   float p[RT][S::KT][4];
   auto scores = [&]() BEAGLE_INLINE_LAMBDA {
@@ -167,7 +171,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
     }
   };
   // O^T += V^T P^T
-  auto values = [&]() BEAGLE_INLINE_LAMBDA {
+  auto values = [&](const Values& v) BEAGLE_INLINE_LAMBDA {
     if constexpr (BF16) {
       // a probability as two bf16 numbers, 16 bits in all: the matrix pipe has the time, and the rounding of one
       // would cost the output as much again as its own (2^-9)
@@ -245,22 +249,22 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   auto request_k = [&](const Pages& h, const Step& st) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < S::KT; ++t) {
-      const char* src = kbase + (((int64_t)h.k[t] << shift) + ((st.base + 16 * t + l16) & in_page)) * row_bytes + 16 * g4;
-      if (!(st.seen >> (16 + t) & 1)) src = (const char*)zero_row;
+      addr_t src = kbase + (((int64_t)h.k[t] << shift) + ((st.base + 16 * t + l16) & in_page)) * row_bytes + 16 * g4;
+      if (!(st.seen >> (16 + t) & 1)) src = zero;
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j) k[t][j] = *(const u32x4*)(BF16 || (4 * j + g4) * 16 < a.d * E ? src + 64 * j : (const char*)zero_row);
+      for (int j = 0; j < S::NJ; ++j) k[t][j] = load16(BF16 || (4 * j + g4) * 16 < a.d * E ? src + 64 * j : zero);
     }
   };
-  auto request_v = [&](const Pages& h, const Step& st) BEAGLE_INLINE_LAMBDA {
+  auto request_v = [&](Values& v, const Pages& h, const Step& st) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
     for (int t = 0; t < S::KT; ++t) {
-      const char* src = vbase + (((int64_t)h.v[t] << shift) + ((st.base + 16 * t + 4 * g4) & in_page)) * row_bytes + 16 * l16;
+      addr_t src = vbase + (((int64_t)h.v[t] << shift) + ((st.base + 16 * t + 4 * g4) & in_page)) * row_bytes + 16 * l16;
 #pragma unroll
       for (int i = 0; i < 4; ++i, src += row_bytes)
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
           const bool there = (st.seen >> (4 * t + i) & 1) && (BF16 || (16 * n + l16) * 16 < a.d * E);
-          v[4 * t + i][n] = *(const u32x4*)(there ? src + 256 * n : (const char*)zero_row);
+          v[4 * t + i][n] = load16(there ? src + 256 * n : zero);
         }
     }
   };
@@ -271,7 +275,11 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
       for (int e = 0; e < 4 * S::KT; ++e)
         if (!(st.seen >> e & 1)) sc[t][e / 4][e % 4] = -INFINITY;
   };
-  // Steps of true rows: the rows of the next step travel while this one is computed, its page numbers a step further ahead.
+  // Steps of true rows: the rows of the next step travel while this one is computed, its page numbers a step further ahead.  K's registers
+  // are free once the scores are there; V has a second set where the registers suffice, else its next rows are asked for
+  // behind the products.  (Addresses of whole steps in scalar registers, and half the vector instructions with that: the registers that
+  // two ways of addressing take cost 3 to 30 % instead.)
+  constexpr bool TWICE = RT == 1;
   int plain = steps;
   if constexpr (TREE)
     while (plain > 0 && base_of(plain - 1) + S::KROWS > rows.nt) --plain;
@@ -281,22 +289,32 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
     Pages next = look(0);
     Step st = judge(next, 0);
     request_k(next, st);
-    request_v(next, st);
+    request_v(v, next, st);
     next = look(1);
-    for (int s = 0; s < plain; ++s) {
+    auto step = [&](int s, Values& mine, Values& others) BEAGLE_INLINE_LAMBDA {
       scores();
       Step ahead = st;
       const Pages now = next;
       if (s + 1 < plain) {
         ahead = judge(now, s + 1);
         request_k(now, ahead);
+        if (TWICE) request_v(others, now, ahead);
         next = look(s + 2);
       }
       if (st.masked) hide(st);
       probabilities();
-      values();
-      if (s + 1 < plain) request_v(now, ahead);
+      values(mine);
+      if (!TWICE && s + 1 < plain) request_v(mine, now, ahead);
       st = ahead;
+    };
+    if constexpr (TWICE) {
+      Values w;
+      for (int s = 0; s < plain; s += 2) {
+        step(s, v, w);
+        if (s + 1 < plain) step(s + 1, w, v);
+      }
+    } else {
+      for (int s = 0; s < plain; ++s) step(s, v, v);
     }
   }
   if constexpr (TREE)
@@ -304,7 +322,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
       if (s > plain) tail = look(s);
       const Step st = judge(tail, s);
       request_k(tail, st);
-      request_v(tail, st);
+      request_v(v, tail, st);
       scores();
       hide(st);
       // the step's rows in a query's word of bits: true ones set, drafted ones as the tree has them
@@ -334,7 +352,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
             if constexpr (BF16) top = max(top, (x << 16) & 0x7f800000u);
           }
       if (__ballot(top == 0x7f800000u) == 0) {
-        values();
+        values(v);
         continue;
       }
       float* mine = sh.o[wave][l16];             // (free until the end)
@@ -347,7 +365,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
           const float w = mine[j];
           const int row = st.base + j, pg = paged_page(table, row, paged_seen(rows, row), shift, a.c.P);
           if (w == -1.f || pg < 0) continue;
-          const char* src = vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
+          const char* src = (const char*)vbase + (((int64_t)pg << shift) + (row & in_page)) * row_bytes;
 #pragma unroll
           for (int c = 0; c < S::NA; ++c)
 #pragma unroll
@@ -382,7 +400,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
       }
     __syncthreads();
     const int col = tid >> 4, r = (rb * RT + t) * 16 + col;
-    if (r >= R) continue;
+    if (r >= R || col >= 16) continue;
     float m = -INFINITY, l = 0.f, w[WAVES];
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) m = fmaxf(m, sh.m[i][16 * t + col]);
@@ -416,13 +434,23 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 
 // BF16: head width 128.  Float: NH = 1 for widths up to 64, 2 up to 128.  RT: tiles of 16 query rows that a workgroup takes.
 // TREE: rows from n_true on are seen as the tree's bits say.
-template <bool BF16, int NH, int RT, bool TREE>
-__global__ __launch_bounds__(64 * WAVES, RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
-  __shared__ Merge<Shape<BF16, NH>::HDP, RT> shared;
+// WHOLE: a workgroup of eight waves takes an entry (`worker` is its number), for few and short ones: nothing to look up, to cut or to join.
+template <bool BF16, int NH, int RT, bool TREE, bool WHOLE>
+__global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
+  constexpr int WAVES = WHOLE ? 8 : 4;
+  __shared__ Merge<Shape<BF16, NH>::HDP, RT, WAVES> shared;
   const int lane = threadIdx.x & 63;
   // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
   const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
   const int head = ug % a.G, worker = ug / a.G;
+  if constexpr (WHOLE) {
+    if (worker >= a.B) return;
+    auto wave = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int slot = wave(paged_slot(a.c, a.slots, worker)), nt = wave(a.n_true ? a.n_true[worker] : INT32_MAX);
+    const PagedRows rows = paged_rows(min(wave(paged_len(a.c, slot)), a.bound), nt, a.window, a.sinks);
+    attend_entry<BF16, NH, RT, TREE, WAVES>(a, shared, worker, slot, rows, 0, rows.blocks, true, 0, head, rb);
+    return;
+  }
   const Entry group0 = entry_of(a, lane);
   const int64_t all = all_blocks(a, group0);
   const int workers = paged_workers(all, a.target, a.least);
@@ -447,7 +475,7 @@ __global__ __launch_bounds__(64 * WAVES, RESIDENT) void paged_attn_kernel(PagedA
       if (used) __syncthreads();
       used = true;
       // a part's sums: one place for the entry that the worker goes on with, one for the entry that it begins
-      attend_entry<BF16, NH, RT, TREE>(a, shared, b, slot, rows, first, last, whole, 2 * worker + (first == 0), head, rb);
+      attend_entry<BF16, NH, RT, TREE, WAVES>(a, shared, b, slot, rows, first, last, whole, 2 * worker + (first == 0), head, rb);
     }
   }
 }
@@ -523,6 +551,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
+// Entries of up to so many blocks (three steps of eight waves), on one workgroup each if there are no more than so many: a
+// compute unit gets some 50 GB/s to itself, 2.45 us a step, so longer ones are cut.  One sequence of 8 kv heads on one
+// workgroup a head / cut and joined by a second launch, us: 256 rows 7.1 / 10.8, 512 9.5 / 10.8, 1024 14.6 / 10.9; and a launch takes the
+// host 3.3.
+constexpr int WHOLE_BLOCKS = 24, WHOLE_GROUPS = 256;
 constexpr int MAX_TILES = 2;               // of 16 query rows that a workgroup takes
 struct Tiles { int each, blocks; };        // tiles of a workgroup, workgroups that the rows of a kv head take
 Tiles tiles_of(int R) {
@@ -546,32 +579,40 @@ size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G) {
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const int R = a.M * (a.H / a.G);
   const Tiles tiles = tiles_of(R);
+  // blocks that an entry can have: those of the longest sequence, or of the window's and the first rows (their edges not counted as whole)
+  int64_t most = (a.bound + PAGED_BLOCK - 1) / PAGED_BLOCK;
+  if (a.window > 0 && !a.n_true) {
+    const int64_t seen = (int64_t)(a.window / PAGED_BLOCK) + a.sinks / PAGED_BLOCK + 4;
+    if (seen < most) most = seen;
+  }
+  const bool whole = most <= WHOLE_BLOCKS && (int64_t)a.B * a.G * tiles.blocks <= WHOLE_GROUPS;
   a.target = workers_aimed(R, a.G);
-  a.least = WAVES;
+  a.least = 4;                             // a block for every wave
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
-  const int heads8 = a.target * a.G;
-  const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(64 * WAVES);
+  const int heads8 = (whole ? a.B : a.target) * a.G;
+  const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(whole ? 512 : 256);
   const bool tree = a.n_true != nullptr, narrow = !bf16 && a.d <= 64;
   {
     ProfScope ps("paged_attn", s);
-    auto go = [&](auto bf_, auto nh_, auto rt_) {
-      constexpr bool BF = decltype(bf_)::value != 0;
+    auto go = [&](auto bf_, auto nh_, auto rt_, auto whole_) {
+      constexpr bool BF = decltype(bf_)::value != 0, WH = decltype(whole_)::value != 0;
       constexpr int NH = decltype(nh_)::value, RT = decltype(rt_)::value;
-      if (tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, true>), grid, wg, 0, s, a, heads8, tiles.blocks);
-      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, false>), grid, wg, 0, s, a, heads8, tiles.blocks);
+      if (tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, true, WH>), grid, wg, 0, s, a, heads8, tiles.blocks);
+      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, false, WH>), grid, wg, 0, s, a, heads8, tiles.blocks);
     };
     auto with = [&](auto bf_, auto nh_) {
-      if (tiles.each == 1) go(bf_, nh_, int_c<1>{});
-      else go(bf_, nh_, int_c<2>{});
+      if (tiles.each == 1 && whole) go(bf_, nh_, int_c<1>{}, int_c<1>{});
+      else if (whole) go(bf_, nh_, int_c<2>{}, int_c<1>{});
+      else if (tiles.each == 1) go(bf_, nh_, int_c<1>{}, int_c<0>{});
+      else go(bf_, nh_, int_c<2>{}, int_c<0>{});
     };
     if (bf16) with(int_c<1>{}, int_c<1>{});
     else if (narrow) with(int_c<0>{}, int_c<1>{});
     else with(int_c<0>{}, int_c<2>{});
   }
-  // no entry is long enough to be cut: nothing to join
-  if ((a.bound + PAGED_BLOCK - 1) / PAGED_BLOCK <= a.least) return;
+  if (whole || most <= a.least) return;    // no entry is cut: nothing to join
   ProfScope ps("paged_join", s);
   auto join = [&](auto bf_, auto hdp_) {
     constexpr bool BF = decltype(bf_)::value != 0;
