@@ -85,11 +85,15 @@ template <bool BF16, int NH> struct Shape {
   static constexpr int NA = BF16 ? 8 : 4 * NH;          // accumulator tiles
 };
 
-template <int HDP, int RT, int WAVES> struct Merge { float o[WAVES][16][HDP + 4], m[WAVES][RT * 16], l[WAVES][RT * 16]; };
+// the waves' shares of an entry, and with two tiles its queries: their registers go to the rows on the way
+template <class S, int RT, int WAVES> struct Shared {
+  float o[WAVES][16][S::HDP + 4], m[WAVES][RT * 16], l[WAVES][RT * 16];
+  u32x4 q[RT > 1 ? RT : 1][RT > 1 ? S::NJ : 1][64];
+};
 
 // One entry's blocks first .. last - 1 for one kv head and row block: a wave takes every WAVES-th.
 template <bool BF16, int NH, int RT, bool TREE, int WAVES>
-__device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape<BF16, NH>::HDP, RT, WAVES>& sh, int b, int slot, const PagedRows rows,
+__device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shape<BF16, NH>, RT, WAVES>& sh, int b, int slot, const PagedRows rows,
                                              int first, int last, bool whole, int part, int head, int rb) {
   using S = Shape<BF16, NH>;
   constexpr int E = BF16 ? 2 : 4, HDP = S::HDP;              // bytes of a value; padded head width
@@ -103,17 +107,19 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   const int in_page = (1 << a.c.shift) - 1;
 
   // queries: column l16 of tile t is row r of this kv head's R = M * rep rows
-  u32x4 q[RT][S::NJ];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int r = (rb * RT + t) * 16 + l16, m = r / rep;
+  constexpr bool HELD = RT == 1;           // in registers, else in LDS
+  u32x4 q[S::NJ];
+  if (HELD || wave < RT) {
+    const int r = (rb * RT + (HELD ? 0 : wave)) * 16 + l16, m = r / rep;
     const addr_t p = (addr_t)a.q + ((((int64_t)b * a.M + m) * a.H + head * rep + r % rep) * a.d) * E;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       const int piece = (4 * j + g4) * 16;
-      q[t][j] = load16(r < R && (BF16 || piece < a.d * E) ? p + piece : zero);
+      q[j] = load16(r < R && (BF16 || piece < a.d * E) ? p + piece : zero);
+      if (!HELD) sh.q[wave][j][lane] = q[j];
     }
   }
+  if (!HELD) __syncthreads();
   f32x4 acc[RT][S::NA];
   float mx[RT], sum[RT];
 #pragma unroll
@@ -135,19 +141,24 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
   f32x4 sc[RT][S::KT];
   float p[RT][S::KT][4];
   auto scores = [&]() BEAGLE_INLINE_LAMBDA {
+    if (!HELD) asm volatile("" ::: "memory");        // (the queries are read again)
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+    for (int t = 0; t < RT; ++t) {
 #pragma unroll
-      for (int kt = 0; kt < S::KT; ++kt) {
-        sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < S::KT; ++kt) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) {
-          if constexpr (BF16) sc[t][kt] = mfma_bf16(k[kt][j], q[t][j], sc[t][kt]);
+      for (int j = 0; j < S::NJ; ++j) {
+        u32x4 x = q[j];
+        if (!HELD) x = sh.q[t][j][lane];
+#pragma unroll
+        for (int kt = 0; kt < S::KT; ++kt) {
+          if constexpr (BF16) sc[t][kt] = mfma_bf16(k[kt][j], x, sc[t][kt]);
           else
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[t][kt] = mfma_f32(__uint_as_float(k[kt][j][e]), __uint_as_float(q[t][j][e]), sc[t][kt]);
+            for (int e = 0; e < 4; ++e) sc[t][kt] = mfma_f32(__uint_as_float(k[kt][j][e]), __uint_as_float(x[e]), sc[t][kt]);
         }
       }
+    }
   };
   // running maximum and sum, probabilities
   auto probabilities = [&]() BEAGLE_INLINE_LAMBDA {
@@ -276,10 +287,8 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
         if (!(st.seen >> e & 1)) sc[t][e / 4][e % 4] = -INFINITY;
   };
   // Steps of true rows: the rows of the next step travel while this one is computed, its page numbers a step further ahead.  K's registers
-  // are free once the scores are there; V has a second set where the registers suffice, else its next rows are asked for
-  // behind the products.  (Addresses of whole steps in scalar registers, and half the vector instructions with that: the registers that
+  // are free once the scores are there; V has a second set (4 sequences of up to 32768 rows, 40 heads: 365 us without, 355 with).  (Addresses of whole steps in scalar registers, and half the vector instructions with that: the registers that
   // two ways of addressing take cost 3 to 30 % instead.)
-  constexpr bool TWICE = RT == 1;
   int plain = steps;
   if constexpr (TREE)
     while (plain > 0 && base_of(plain - 1) + S::KROWS > rows.nt) --plain;
@@ -298,23 +307,18 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
       if (s + 1 < plain) {
         ahead = judge(now, s + 1);
         request_k(now, ahead);
-        if (TWICE) request_v(others, now, ahead);
+        request_v(others, now, ahead);
         next = look(s + 2);
       }
       if (st.masked) hide(st);
       probabilities();
       values(mine);
-      if (!TWICE && s + 1 < plain) request_v(mine, now, ahead);
       st = ahead;
     };
-    if constexpr (TWICE) {
-      Values w;
-      for (int s = 0; s < plain; s += 2) {
-        step(s, v, w);
-        if (s + 1 < plain) step(s + 1, w, v);
-      }
-    } else {
-      for (int s = 0; s < plain; ++s) step(s, v, v);
+    Values w;
+    for (int s = 0; s < plain; s += 2) {
+      step(s, v, w);
+      if (s + 1 < plain) step(s + 1, w, v);
     }
   }
   if constexpr (TREE)
@@ -438,7 +442,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Merge<Shape
 template <bool BF16, int NH, int RT, bool TREE, bool WHOLE>
 __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
   constexpr int WAVES = WHOLE ? 8 : 4;
-  __shared__ Merge<Shape<BF16, NH>::HDP, RT, WAVES> shared;
+  __shared__ Shared<Shape<BF16, NH>, RT, WAVES> shared;
   const int lane = threadIdx.x & 63;
   // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
   const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
