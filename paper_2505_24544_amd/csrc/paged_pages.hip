@@ -52,97 +52,146 @@ struct Want { int slot, len, pos, n, keep, pages; bool room; };
 __device__ __forceinline__ Want want_of(const PagedAppendArgs& a, const int* owner, int b) {
   Want w;
   w.slot = paged_slot(a.c, a.slots, b);
+  const int pos = a.pos ? a.pos[b] : INT32_MAX, n = a.n_new ? a.n_new[b] : a.M;
+  const int len = a.c.lens[max(w.slot, 0)];                     // (one trip for all three)
   if (w.slot >= 0 && owner[w.slot] != b) w.slot = -1;           // the slot's first entry counts
-  w.len = paged_len(a.c, w.slot);
-  w.pos = a.pos ? min(max(a.pos[b], 0), w.len) : w.len;
-  w.n = w.slot < 0 ? 0 : a.n_new ? min(max(a.n_new[b], 0), a.M) : a.M;
+  w.len = w.slot < 0 ? 0 : paged_clamped(len, a.c.W, a.c.shift);
+  w.pos = min(max(pos, 0), w.len);
+  w.n = w.slot < 0 ? 0 : min(max(n, 0), a.M);
   w.room = (int64_t)w.pos + w.n <= (int64_t)a.c.W << a.c.shift;
   w.keep = paged_pages(w.pos, a.c.shift);
   w.pages = w.room ? paged_pages(w.pos + w.n, a.c.shift) : w.keep;
   return w;
 }
 
-// One workgroup: releases, then the pages that every entry wants, then the lowest free ones, handed out in order.
+// f(x, y, i) for every i in [lo, hi), with the lane's x and y: by the lane where they are few, by the wave together where they are many
+template <class F> __device__ __forceinline__ void each_page(int lo, int hi, int x, int y, F&& f) {
+  const bool many = hi - lo > 4;
+  if (!many)
+    for (int i = lo; i < hi; ++i) f(x, y, i);
+  for (unsigned long long left = __ballot(many); left; left &= left - 1) {
+    const int l = __ffsll((long long)left) - 1;
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    const int to = of(hi), xl = of(x), yl = of(y);
+    for (int i = of(lo) + (int)(threadIdx.x & 63); i < to; i += 64) f(xl, yl, i);
+  }
+}
+
+constexpr int LOOK = 16;                   // counts that a thread looks at in one trip to memory
+constexpr int NEAR = 4096;                 // taken pages that LDS holds
+
+// One workgroup, bound by its trips to memory one behind the other: releases, the pages that every entry wants, the lowest free
+// ones, handed out in order.
 __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs a, AppendWs ws) {
   __shared__ int owner[PAGED_MAX_BATCH];
+  __shared__ int taken[NEAR];
   __shared__ int wave_sums[PLAN_WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, in_page = (1 << a.c.shift) - 1;
+  __shared__ int lacking;
+  const int tid = threadIdx.x, in_page = (1 << a.c.shift) - 1;
   for (int s = tid; s < a.c.N; s += PLAN) owner[s] = INT32_MAX;
+  if (tid == 0) lacking = 0;
   __syncthreads();
   for (int b = tid; b < a.B; b += PLAN) {
     const int s = paged_slot(a.c, a.slots, b);
     if (s >= 0) atomicMin(&owner[s], b);
   }
   __syncthreads();
-  // pages behind the kept rows
-  for (int b = wave; b < a.B; b += PLAN_WAVES) {
-    const Want w = want_of(a, owner, b);
-    for (int i = w.keep + lane; i < paged_pages(w.len, a.c.shift); i += 64) {
-      const int p = a.c.table[(int64_t)w.slot * a.c.W + i];
-      if (is_page(a.c, p)) add_count(a.c.refs + p, -1);
-    }
-  }
-  settle();
-  // pages wanted; a page that is kept in part and shared is copied into one of its own
-  int wanted = 0, lacking = 0;
+  // pages behind the kept rows are given up; of the page that is kept in part, whether there is one
+  Want w{};
+  int part = -1;
   for (int b0 = 0; b0 < a.B; b0 += PLAN) {
     const int b = b0 + tid;
-    int need = 0, over = 0;
-    if (b < a.B) {
-      const Want w = want_of(a, owner, b);
-      int from = -1;
-      if (w.n > 0 && w.room && (w.pos & in_page)) {
-        const int p = a.c.table[(int64_t)w.slot * a.c.W + w.keep - 1];
-        if (!is_page(a.c, p)) from = -2;                        // (a page that is none: the rows go into a fresh one)
-        else if (load_count(a.c.refs + p) > 1) from = p;
-      }
-      need = w.pages - w.keep + (from != -1);
-      over = w.room ? 0 : (int)(((int64_t)w.pos + w.n - ((int64_t)a.c.W << a.c.shift) + in_page) >> a.c.shift);
-      ws.entry[b] = Entry{w.slot, w.pos, w.room ? w.n : 0, from};
+    w = Want{};
+    w.slot = -1;
+    part = -1;
+    if (b < a.B) w = want_of(a, owner, b);
+    const int32_t* row = a.c.table + (int64_t)max(w.slot, 0) * a.c.W;
+    if (w.n > 0 && w.room && (w.pos & in_page)) {
+      const int p = row[w.keep - 1];
+      part = is_page(a.c, p) ? p : -2;                          // (a page that is none: the rows go into a fresh one)
     }
-    int all, none;
-    const int upto = wanted + block_scan(need, wave_sums, all);
-    if (b < a.B) ws.upto[b] = upto;
+    each_page(w.keep, paged_pages(w.len, a.c.shift), w.slot, 0, [&](int slot, int, int i) {
+      const int p = a.c.table[(int64_t)slot * a.c.W + i];
+      if (is_page(a.c, p)) add_count(a.c.refs + p, -1);
+    });
+    if (a.B > PLAN && b < a.B) ws.entry[b] = Entry{w.slot, part, 0, 0};         // (looked at again below)
+  }
+  settle();
+  // pages wanted; a page that is kept in part and shared is copied into one of its own.  The first counts are looked at on the way.
+  const bool vec = (((uintptr_t)a.c.refs) & 15) == 0;
+  int held[LOOK];
+  auto look = [&](int64_t p0) {
+    const int64_t p = p0 + (int64_t)LOOK * tid;
+    if (vec && p + LOOK <= a.c.P) {
+#pragma unroll
+      for (int i = 0; i < LOOK; i += 4) {
+        const int4 x = *(const int4*)(a.c.refs + p + i);
+        held[i] = x.x; held[i + 1] = x.y; held[i + 2] = x.z; held[i + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOOK; ++i) held[i] = p + i < a.c.P ? a.c.refs[p + i] : 1;
+    }
+  };
+  look(0);
+  int wanted = 0;
+  Entry e{-1, 0, 0, -1};
+  int upto = 0;
+  for (int b0 = 0; b0 < a.B; b0 += PLAN) {
+    const int b = b0 + tid;
+    if (a.B > PLAN) {
+      w = Want{};
+      w.slot = -1;
+      part = -1;
+      if (b < a.B) { w = want_of(a, owner, b); part = ws.entry[b].pos; }
+    }
+    int from = -1;
+    if (part != -1) from = part == -2 ? -2 : a.c.refs[part] > 1 ? part : -1;
+    const int need = w.pages - w.keep + (from != -1);
+    if (b < a.B && !w.room) atomicAdd(&lacking, (int)(((int64_t)w.pos + w.n - ((int64_t)a.c.W << a.c.shift) + in_page) >> a.c.shift));
+    e = Entry{w.slot, w.pos, w.room ? w.n : 0, from};
+    int all;
+    upto = wanted + block_scan(need, wave_sums, all);
     wanted += all;
-    block_scan(over, wave_sums, none);
-    lacking += none;
+    if (b < a.B) { ws.entry[b] = e; ws.upto[b] = upto; }
   }
   // the lowest free pages
   int found = 0;
-  for (int64_t p0 = 0; p0 < a.c.P && found < wanted; p0 += 4 * PLAN) {
-    const int64_t p = p0 + 4 * tid;
-    int n = 0, is_free[4];
+  for (int64_t p0 = 0; p0 < a.c.P && found < wanted; p0 += LOOK * PLAN) {
+    if (p0) look(p0);
+    int n = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      is_free[i] = p + i < a.c.P && load_count(a.c.refs + p + i) <= 0;
-      n += is_free[i];
-    }
+    for (int i = 0; i < LOOK; ++i) n += held[i] <= 0;
     int all, at = block_scan(n, wave_sums, all) - n + found;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (is_free[i]) ws.taken[at++] = (int32_t)(p + i);
+    for (int i = 0; i < LOOK; ++i)
+      if (held[i] <= 0) {
+        if (at < NEAR) taken[at] = (int)(p0 + (int64_t)LOOK * tid + i); else ws.taken[at] = (int32_t)(p0 + (int64_t)LOOK * tid + i);
+        ++at;
+      }
     found += all;
   }
-  settle();
+  if (wanted > NEAR || a.B > PLAN) settle(); else __syncthreads();
   if (tid == 0 && a.short_pages) a.short_pages[0] = max(wanted - found, 0) + lacking;
-  for (int b = wave; b < a.B; b += PLAN_WAVES) {
-    const Entry e = ws.entry[b];
-    if (e.slot < 0) continue;
-    const int upto = ws.upto[b], keep = paged_pages(e.pos, a.c.shift), pages = paged_pages(e.pos + e.n, a.c.shift);
-    const int own = e.from != -1, need = pages - keep + own;
-    int32_t* row = a.c.table + (int64_t)e.slot * a.c.W;
-    if (need && upto > found) {                                 // not enough pages: the entry keeps its first rows
-      if (lane == 0) { ws.entry[b].n = 0; ws.entry[b].from = -1; a.c.lens[e.slot] = e.pos; }
-      continue;
+  for (int b0 = 0; b0 < a.B; b0 += PLAN) {
+    const int b = b0 + tid;
+    if (a.B > PLAN) {
+      e = Entry{-1, 0, 0, -1};
+      if (b < a.B) { e = ws.entry[b]; upto = ws.upto[b]; }
     }
-    for (int i = lane; i < need; i += 64) {
-      const int p = ws.taken[upto - need + i];
-      row[keep - own + i] = p;
+    const int keep = paged_pages(e.pos, a.c.shift), own = e.from != -1;
+    const int need = e.slot < 0 ? 0 : paged_pages(e.pos + e.n, a.c.shift) - keep + own;
+    const bool fits = need == 0 || upto <= found;               // else the entry keeps its first rows
+    const int first = upto - need;                              // of its pages among those taken
+    each_page(keep - own, keep - own + (fits ? need : 0), e.slot, first - (keep - own), [&](int slot, int shifted, int i) {
+      const int at = shifted + i, p = at < NEAR ? taken[at] : ws.taken[at];
+      a.c.table[(int64_t)slot * a.c.W + i] = p;
       __hip_atomic_store(a.c.refs + p, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    if (lane == 0) {
-      if (e.from >= 0) add_count(a.c.refs + e.from, -1);
-      a.c.lens[e.slot] = e.pos + e.n;
+    });
+    if (e.slot >= 0) {
+      if (!fits) { ws.entry[b].n = 0; ws.entry[b].from = -1; }
+      else if (e.from >= 0) add_count(a.c.refs + e.from, -1);
+      a.c.lens[e.slot] = fits ? e.pos + e.n : e.pos;
     }
   }
 }
