@@ -139,7 +139,6 @@ def make_paged_cache(k_pages, v_pages, page_table, lens, refs) -> beagle_paged_c
         raise ValueError("k_pages and v_pages are [P, page_rows, G, d] of one type")
     if page_table.dim() != 2 or tuple(lens.shape) != tuple(page_table.shape[:1]) or tuple(refs.shape) != tuple(k_pages.shape[:1]):
         raise ValueError("page_table is [N, slot_pages], lens [N], refs [P]")
-    import torch
     if {str(x.dtype) for x in (page_table, lens, refs)} != {"torch.int32"}:
         raise ValueError("page_table, lens and refs are torch.int32")
     if len({x.device for x in (k_pages, v_pages, page_table, lens, refs)}) > 1:
@@ -147,7 +146,7 @@ def make_paged_cache(k_pages, v_pages, page_table, lens, refs) -> beagle_paged_c
     c = beagle_paged_cache(C.sizeof(beagle_paged_cache), k_pages.shape[0], k_pages.shape[1], page_table.shape[0],
                            page_table.shape[1], 0, *(_ptr(t) for t in (k_pages, v_pages, page_table, lens, refs)))
     # what a call's tensors are checked against: rows [G, d] of this type on this device
-    c.rows, c.dtype, c.device, c.whole = tuple(k_pages.shape[2:]), k_pages.dtype, k_pages.device, (torch.int32, torch.uint32)
+    c.rows, c.dtype, c.device = tuple(k_pages.shape[2:]), k_pages.dtype, k_pages.device
     return c
 
 
@@ -430,73 +429,69 @@ def beagle_xattn_kv_append(desc, x_new, wk, wv, k_cache, v_cache, pos, workspace
     return _check(st, "beagle_xattn_kv_append", check)
 
 
+_torch = None
+
+
 class _Paged:
     """The tensors of one paged call, checked against its descriptor and its cache; addresses and None pass as they are."""
+    __slots__ = ("desc", "dev", "dtype", "whole", "n")
 
     def __init__(self, desc, cache):
+        global _torch
+        if _torch is None:
+            import torch
+            _torch = torch
+        self.desc = desc
         self.dev = getattr(cache, "device", None)         # (None: a cache made of addresses)
         self.n = desc.batch * desc.seq_q
-        self.desc = desc
-        if self.dev is None:
-            import torch
-            self.dtype, self.whole = torch.bfloat16 if desc.io_dtype == BEAGLE_BF16 else torch.float32, (torch.int32, torch.uint32)
-            return
-        self.dtype, self.whole = cache.dtype, cache.whole
-        if cache.rows != (desc.n_kv_heads, desc.head_dim) or self.dtype.itemsize != (2 if desc.io_dtype == BEAGLE_BF16 else 4):
+        self.whole = (_torch.int32, _torch.uint32)
+        self.dtype = _torch.bfloat16 if desc.io_dtype == BEAGLE_BF16 else _torch.float32
+        if self.dev is not None and (cache.dtype != self.dtype or cache.rows != (desc.n_kv_heads, desc.head_dim)):
             raise ValueError("the cache holds rows %s of %s, not what the descriptor says" % (cache.rows, cache.dtype))
 
-    def _at(self, t, count):
-        if not t.is_cuda or (self.dev is not None and t.device != self.dev):
-            raise ValueError("a tensor argument is on %s, the cache is on %s" % (t.device, self.dev))
-        if t.numel() != count and count >= 0:
-            raise ValueError("a tensor of shape %s does not hold the %d values of the call" % (tuple(t.shape), count))
-        return _ptr(t)
-
-    def ints(self, t, count):
+    def _at(self, t, count, dtypes):
         if t is None or isinstance(t, int):
             return t
-        if t.dtype not in self.whole:
-            raise ValueError("an index argument is a tensor of 32-bit whole numbers, not of %s" % t.dtype)
-        return self._at(t, count)
+        if t.dtype not in dtypes:
+            raise ValueError("a tensor of %s is needed, not of %s" % (" or ".join(map(str, dtypes)), t.dtype))
+        if t.device != self.dev and (self.dev is not None or not t.is_cuda):
+            raise ValueError("a tensor argument is on %s, the cache is on %s" % (t.device, self.dev or "a GPU"))
+        if t.numel() != count:
+            raise ValueError("a tensor of shape %s does not hold the %d values of the call" % (tuple(t.shape), count))
+        if not t.is_contiguous():
+            raise ValueError("tensor arguments must be contiguous")
+        return t.data_ptr()
+
+    def ints(self, t, count):
+        return self._at(t, count, self.whole)
 
     def rows(self, t, width):
         """[batch, seq_q, width] of the cache's type"""
-        if t is None or isinstance(t, int):
-            return t
-        if t.dtype != self.dtype:
-            raise ValueError("a tensor of %s is needed, not of %s" % (self.dtype, t.dtype))
-        return self._at(t, self.n * width)
+        return self._at(t, self.n * width, (self.dtype,))
 
     def weight(self, t, count):
-        if t is None or isinstance(t, int):
-            return t
-        if t.dtype != self.dtype:
-            raise ValueError("a tensor of %s is needed, not of %s" % (self.dtype, t.dtype))
-        return self._at(t, count)
+        return self._at(t, count, (self.dtype,))
 
     def lse(self, t):
-        if t is None or isinstance(t, int):
-            return t
-        if not t.dtype.is_floating_point or t.dtype.itemsize != 4:
-            raise ValueError("lse is a torch.float32 tensor [batch, heads, seq_q]")
-        return self._at(t, self.n * self.desc.n_q_heads)
+        return self._at(t, self.n * self.desc.n_q_heads, (_torch.float32,))
 
     def view(self, slots, n_true, tree_mask, mask_words, window, sinks):
         B = self.desc.batch
-        return (self.ints(slots, B), self.ints(n_true, B), self.ints(tree_mask, self.n * int(mask_words)), int(mask_words),
-                int(window), int(sinks))
+        return (self.ints(slots, B), self.ints(n_true, B), self.ints(tree_mask, self.n * mask_words), mask_words, window, sinks)
 
     def call(self, name, cache, args, workspace, workspace_bytes, stream, check):
         """By default on the current stream of the cache's device, which is made the current one meanwhile."""
-        ws = workspace if workspace is None or isinstance(workspace, int) else self._at(workspace, -1)
-        nbytes = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
-        fn = getattr(lib(), name)
-        if self.dev is not None:
-            import torch
-            if self.dev.index != torch.cuda.current_device():
-                with torch.cuda.device(self.dev):
-                    return _check(fn(C.byref(self.desc), C.byref(cache), *args, ws, nbytes, _stream(stream)), name, check)
-        return _check(fn(C.byref(self.desc), C.byref(cache), *args, ws, nbytes, _stream(stream)), name, check)
+        if workspace is not None and not isinstance(workspace, int):
+            if workspace_bytes is None:
+                workspace_bytes = workspace.numel() * workspace.element_size()
+            workspace = self._at(workspace, workspace.numel(), (workspace.dtype,))
+        fn = getattr(_lib or lib(), name)
+        if self.dev is not None and self.dev.type != "cuda":
+            raise ValueError("the cache is on %s, not on a GPU" % self.dev)
+        if self.dev is not None and self.dev.index != _torch.cuda.current_device():
+            with _torch.cuda.device(self.dev):
+                return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
+        return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
 
 
 def beagle_xattn_paged_workspace_bytes(desc, cache, which) -> int:
@@ -529,7 +524,7 @@ def beagle_xattn_paged_compact(desc, cache, into, short_pages, workspace, stream
     c = _Paged(desc, cache)
     if c.dev is not None and getattr(into, "device", None) is not None and (c.dev != into.device or cache.rows != into.rows or c.dtype != into.dtype):
         raise ValueError("the two pools hold different rows, or are on different devices")
-    args = (C.byref(into), c.ints(short_pages, 1))
+    args = (into, c.ints(short_pages, 1))
     return c.call("beagle_xattn_paged_compact", cache, args, workspace, workspace_bytes, stream, check)
 
 

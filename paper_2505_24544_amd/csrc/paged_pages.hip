@@ -17,8 +17,13 @@ constexpr int PLAN_WAVES = PLAN / 64;
 __device__ __forceinline__ int load_count(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void add_count(int32_t* p, int v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool is_page(const PagedCache& c, int p) { return (unsigned)p < (unsigned)c.P; }
-// every thread's earlier stores and atomics are seen by the workgroup's later loads
-__device__ __forceinline__ void settle() { __threadfence(); __syncthreads(); }
+// every thread's earlier stores and atomics are seen by the workgroup's later loads: a barrier, which waits for them, and vector
+// caches without what they held before (nobody else reads on, so nothing has to be written back for other dies: that fence
+// cost 2 us)
+__device__ __forceinline__ void settle() {
+  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+}
 
 // Inclusive sum over the workgroup's threads in order; `all` gets the sum of everything.
 __device__ __forceinline__ int block_scan(int v, int* wave_sums, int& all) {
@@ -31,14 +36,16 @@ __device__ __forceinline__ int block_scan(int v, int* wave_sums, int& all) {
   __syncthreads();                         // (the sums of the call before have been read)
   if (lane == 63) wave_sums[wave] = v;
   __syncthreads();
-  int before = 0;
-  all = 0;
-  for (int w = 0; w < PLAN_WAVES; ++w) {
-    const int x = wave_sums[w];
-    before += w < wave ? x : 0;
-    all += x;
+  // (a lane for each wave's sum)
+  const int x = lane < PLAN_WAVES ? wave_sums[lane] : 0;
+  int upto = x;
+#pragma unroll
+  for (int m = 1; m < PLAN_WAVES; m <<= 1) {
+    const int y = __shfl_up(upto, m);
+    if (lane >= m) upto += y;
   }
-  return v + before;
+  all = __builtin_amdgcn_readlane(upto, PLAN_WAVES - 1);
+  return v + __shfl(upto - x, wave);
 }
 
 // ------------------------------------------------------------------ append
@@ -303,6 +310,52 @@ __global__ __launch_bounds__(256) void paged_fork_write_kernel(PagedCache c, con
   if (tid == 0) c.lens[to] = n;
 }
 
+// The same by one workgroup in one launch where its registers hold all pages, old and new: 24 sequences of up to 3000 rows take 5 to 7 us
+// either way, but a launch takes the host 3.3 us and is the longer of the two (a pass 14.0 us with two, 11.3 with one).
+constexpr int FORK_EACH = 8;               // table entries of a thread
+constexpr int FORK_NEAR_ENTRIES = 256;
+__global__ __launch_bounds__(PLAN) void paged_fork_kernel(PagedCache c, const int32_t* dst, const int32_t* src, const int32_t* rows, int B) {
+  __shared__ int to[FORK_NEAR_ENTRIES], from[FORK_NEAR_ENTRIES], had[FORK_NEAR_ENTRIES], has[FORK_NEAR_ENTRIES];
+  const int tid = threadIdx.x;
+  int n = 0, mine = -1;
+  if (tid < B) {
+    const int s = src[tid], slot = (unsigned)s < (unsigned)c.N ? s : -1, want = rows ? rows[tid] : INT32_MAX;
+    mine = dst[tid];
+    const bool in = (unsigned)mine < (unsigned)c.N;
+    const int len = c.lens[max(slot, 0)], old = c.lens[in ? mine : 0];
+    n = slot < 0 ? 0 : min(max(want, 0), paged_clamped(len, c.W, c.shift));
+    to[tid] = mine = in ? mine : -1;
+    from[tid] = max(slot, 0);
+    had[tid] = paged_pages(paged_clamped(old, c.W, c.shift), c.shift);
+    has[tid] = paged_pages(n, c.shift);
+  }
+  __syncthreads();
+  for (int i = 0; i < min(tid, B); ++i)
+    if (to[i] == mine) mine = -1;          // the target's first entry counts
+  int old[FORK_EACH], now[FORK_EACH];
+#pragma unroll
+  for (int e = 0; e < FORK_EACH; ++e) {
+    const int at = tid + e * PLAN, b = min(at / c.W, B - 1), i = at - at / c.W * c.W;
+    now[e] = c.table[(int64_t)from[b] * c.W + i];
+    old[e] = c.table[(int64_t)max(to[b], 0) * c.W + i];
+    if (i >= has[b]) now[e] = -1;
+    if (i >= had[b]) old[e] = -1;
+  }
+  __syncthreads();                         // (everything has been read)
+  if (tid < B) to[tid] = mine;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < FORK_EACH; ++e) {
+    const int at = tid + e * PLAN, b = at / c.W;
+    if (b >= B || to[b] < 0) continue;
+    c.table[(int64_t)to[b] * c.W + at - b * c.W] = now[e];
+    if (old[e] == now[e]) continue;
+    if (is_page(c, old[e])) add_count(c.refs + old[e], -1);
+    if (is_page(c, now[e])) add_count(c.refs + now[e], 1);
+  }
+  if (tid < B && mine >= 0) c.lens[mine] = n;
+}
+
 // ------------------------------------------------------------------ compact
 struct CompactWs { int32_t *number, *live, *count; };   // [P] new number of a live page, [P] live pages in order, [1] how many move
 
@@ -370,6 +423,68 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache from, PagedC
   }
 }
 
+// The same in one launch for a small pool: every workgroup numbers the live pages for itself, the first one has the tables
+// and counts to itself, the others copy.  8 MB in 6.1 us instead of 6.7, a pass in 9.7 instead of 13.0 (the host's
+// launches are the longer).
+constexpr int COMPACT_NEAR = 4096, COMPACT_NEAR_ENTRIES = 16384;
+constexpr int64_t COMPACT_NEAR_BYTES = 32 << 20;          // of K; a large pool is copied better by small workgroups
+__global__ __launch_bounds__(PLAN) void paged_compact_kernel(PagedCache from, PagedCache into, int64_t page_bytes, int32_t* short_pages) {
+  __shared__ int number[COMPACT_NEAR], live[COMPACT_NEAR];
+  __shared__ int wave_sums[PLAN_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int EACH = COMPACT_NEAR / PLAN;
+  int n = 0, held[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int p = EACH * tid + i;
+    held[i] = p < from.P && from.refs[min(p, from.P - 1)] > 0;
+    n += held[i];
+  }
+  int len0 = 0, p0 = 0;                    // of the wave's first slot: on the way meanwhile
+  if (blockIdx.x == 0) {
+    for (int p = tid; p < into.P; p += PLAN) into.refs[p] = 0;
+    const int s = min(wave, from.N - 1);
+    len0 = from.lens[s];
+    p0 = from.table[(int64_t)s * from.W + min(lane, from.W - 1)];
+  }
+  int all, at = block_scan(n, wave_sums, all) - n;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    number[EACH * tid + i] = held[i] ? at : -1;
+    if (held[i]) live[at++] = EACH * tid + i;
+  }
+  const int moved = min(all, into.P);
+  if (blockIdx.x == 0) {
+    settle();
+    if (tid == 0 && short_pages) short_pages[0] = max(all - into.P, 0);
+    for (int s = wave; s < from.N; s += PLAN_WAVES) {
+      const int len = paged_clamped(s == wave ? len0 : from.lens[s], from.W, from.shift), pages = min(paged_pages(len, from.shift), into.W);
+      int stop = pages;                    // the first page that did not move, once it is met
+      for (int i0 = 0; i0 < into.W; i0 += 64) {
+        const int i = i0 + lane;
+        int p = p0;
+        if (s != wave || i0) p = from.table[(int64_t)s * from.W + min(i, from.W - 1)];
+        const int q = i < stop && is_page(from, p) ? number[p] : -1;
+        const unsigned long long lost = __ballot(i < stop && (unsigned)q >= (unsigned)moved);
+        if (lost) stop = i0 + __ffsll((long long)lost) - 1;
+        if (i >= into.W) continue;
+        into.table[(int64_t)s * into.W + i] = i < stop ? q : -1;
+        if (i < stop) add_count(into.refs + q, 1);
+      }
+      if (lane == 0) into.lens[s] = min((int64_t)len, (int64_t)stop << from.shift);
+    }
+    return;
+  }
+  __syncthreads();
+  const int64_t pieces = page_bytes / 16;
+  for (int64_t u = blockIdx.x - 1; u < 2 * (int64_t)moved; u += gridDim.x - 1) {       // K or V of a page
+    const int to = (int)(u >> 1);
+    const u32x4* src = (const u32x4*)(u & 1 ? from.v : from.k) + live[to] * pieces;
+    u32x4* dst = (u32x4*)(u & 1 ? into.v : into.k) + to * pieces;
+    for (int64_t i = tid; i < pieces; i += PLAN) dst[i] = src[i];
+  }
+}
+
 // where the queries of a draft step stand when the caller does not say: behind the rows that their sequence holds
 __global__ __launch_bounds__(256) void paged_positions_kernel(PagedCache c, const int32_t* slots, int B, int M, int32_t* pos) {
   const int i = blockIdx.x * 256 + threadIdx.x;
@@ -409,6 +524,11 @@ void launch_paged_positions(const PagedCache& c, const int32_t* slots, int32_t B
 size_t paged_fork_ws_bytes(const PagedCache& c, int32_t B) { return up256((size_t)B * 4) + up256((size_t)B * c.W * 4); }
 void launch_paged_fork(const PagedCache& c, const int32_t* dst, const int32_t* src, const int32_t* rows, int32_t B, void* ws,
                        hipStream_t s) {
+  if (B <= FORK_NEAR_ENTRIES && (int64_t)B * c.W <= FORK_EACH * PLAN) {
+    ProfScope ps("paged_fork", s);
+    hipLaunchKernelGGL(paged_fork_kernel, dim3(1), dim3(PLAN), 0, s, c, dst, src, rows, B);
+    return;
+  }
   ForkWs w;
   w.rows = (int32_t*)ws;
   w.pages = (int32_t*)((char*)ws + up256((size_t)B * 4));
@@ -423,6 +543,13 @@ void launch_paged_fork(const PagedCache& c, const int32_t* dst, const int32_t* s
 size_t paged_compact_ws_bytes(const PagedCache& c) { return 2 * up256((size_t)c.P * 4) + 256; }
 void launch_paged_compact(const PagedCache& from, const PagedCache& into, int64_t page_bytes, int32_t* short_pages, void* ws,
                           hipStream_t s) {
+  if (from.P <= COMPACT_NEAR && (int64_t)from.N * (from.W + into.W) <= COMPACT_NEAR_ENTRIES && into.P <= COMPACT_NEAR_ENTRIES &&
+      page_bytes * from.P <= COMPACT_NEAR_BYTES) {
+    ProfScope ps("paged_compact", s);
+    const int least = from.P < into.P ? from.P : into.P, blocks = 2 * least < 512 ? 2 * least : 512;
+    hipLaunchKernelGGL(paged_compact_kernel, dim3((unsigned)(1 + blocks)), dim3(PLAN), 0, s, from, into, page_bytes, short_pages);
+    return;
+  }
   CompactWs w;
   w.number = (int32_t*)ws;
   w.live = (int32_t*)((char*)ws + up256((size_t)from.P * 4));
