@@ -583,11 +583,12 @@ beagle_status beagle_xattn_draft_step_prepared(const beagle_xattn_desc* desc,
  * slot_pages * page_rows <= 2^28, n_pages <= 2^28 (the pool itself may be of
  * any size: offsets are 64 bits); BEAGLE_F32 any d <= 128 with d % 4 == 0,
  * BEAGLE_BF16 d == 128.  Of desc the calls read batch (B <= 8192 entries),
- * seq_q (M rows of each entry, B * M <= 2^28), n_q_heads, n_kv_heads, head_dim,
- * io_dtype, softmax_scale, flags (BEAGLE_FLAG_ROPE only), rope_base,
+ * seq_q (M rows of each entry; B * M and M * n_q_heads at most 2^24), n_q_heads,
+ * n_kv_heads, head_dim, io_dtype, softmax_scale, flags (BEAGLE_FLAG_ROPE only), rope_base,
  * rope_positions [B*M] and, where they say so, seq_kv and hidden.
  * Workspaces are 256-byte aligned (beagle_xattn_paged_workspace_bytes for the same
- * desc and cache); their content before a call does not matter.
+ * desc and cache); their content before a call does not matter, and calls that
+ * may overlap need one each.  Calls that change a cache must not overlap others on it.
  */
 typedef struct {
   int32_t struct_size;          /* sizeof(beagle_paged_cache); checked           */

@@ -15,6 +15,7 @@ struct Paged {
   Dims d;                                  // of desc; projections: Tq rows in all
   PagedCache c;
   int64_t page_bytes;                      // K (or V) of one page
+  double scale;                            // the definition's, not rounded to float
 };
 
 beagle_status check_cache(const beagle_paged_cache* p, PagedCache* c) {
@@ -41,7 +42,7 @@ beagle_status check_paged(const beagle_xattn_desc* desc, const beagle_paged_cach
   if (!desc) return BEAGLE_ERR_NULL;
   if (desc->struct_size != (int32_t)sizeof(beagle_xattn_desc)) return BEAGLE_ERR_SHAPE;
   if (desc->batch < 1 || desc->seq_q < 1 || desc->seq_kv < 1) return BEAGLE_ERR_SHAPE;
-  if (desc->batch > PAGED_MAX_BATCH || (int64_t)desc->batch * desc->seq_q > (1 << 28)) return BEAGLE_ERR_UNSUPPORTED;
+  if (desc->batch > PAGED_MAX_BATCH || (int64_t)desc->batch * desc->seq_q > (1 << 24)) return BEAGLE_ERR_UNSUPPORTED;
   if (desc->flags & ~(uint32_t)BEAGLE_FLAG_ROPE) return BEAGLE_ERR_UNSUPPORTED;
   // the remaining checks are those of the draft step on all rows of the call as one batch entry
   beagle_xattn_desc one = *desc;
@@ -53,9 +54,10 @@ beagle_status check_paged(const beagle_xattn_desc* desc, const beagle_paged_cach
   if (st != BEAGLE_OK) return st;
   Dims& d = out->d;
   d.B = desc->batch; d.S = desc->seq_q; d.L = desc->seq_kv; d.Tq = d.B * d.S;
-  // grids: 16 rows a workgroup at least
+  out->scale = desc->softmax_scale > 0.f ? (double)desc->softmax_scale : 1.0 / sqrt((double)d.d);
+  // grids of less than 2^32 threads a side
   const int64_t rows = d.S * (d.H / d.G);
-  if (rows > (1 << 24) || d.G * ((rows + 15) / 16) > (1 << 24) || d.H * d.S > (1 << 28)) return BEAGLE_ERR_UNSUPPORTED;
+  if (rows > (1 << 24) || d.G * ((rows + 15) / 16) > (1 << 24) || d.H * d.S > (1 << 24)) return BEAGLE_ERR_UNSUPPORTED;
   st = check_cache(cache, &out->c);
   if (st != BEAGLE_OK) return st;
   out->page_bytes = ((int64_t)1 << out->c.shift) * d.GD * (int64_t)d.esz;
@@ -96,7 +98,7 @@ PagedAttnArgs attn_of(const Paged& p) {
   a.B = (int32_t)p.d.B; a.M = (int32_t)p.d.S; a.H = (int32_t)p.d.H; a.G = (int32_t)p.d.G; a.d = (int32_t)p.d.d;
   const int64_t most = (int64_t)p.c.W << p.c.shift;
   a.bound = (int32_t)(p.d.L < most ? p.d.L : most);
-  a.scale = p.d.scale;
+  a.scale = p.scale;
   return a;
 }
 PagedAppendArgs append_of(const Paged& p) {

@@ -20,7 +20,8 @@ struct PagedAttnArgs {
   PagedCache c;
   int32_t B, M, H, G, d;
   int32_t bound;                           // no sequence is taken to hold more rows
-  float scale;
+  double scale;
+  float c2, c2_low;                        // scale * log2(e), set at the launch
   const void* q; void* o; float* lse;      // [B, M, H, d] x2, [B, H, M]
   const int32_t* slots;                    // [B] or null: entry b reads slot b
   const int32_t* n_true;                   // [B] or null: every row is a true one

@@ -16,6 +16,7 @@
 // read in 16-byte pieces of eight (float: four) channels; the channel that a lane's row of V^T stands for is free to
 // choose, so the transposition is a matter of picking halves of registers.
 #include "paged.h"
+#include <math.h>
 
 namespace beagle {
 namespace {
@@ -29,7 +30,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // memory busy; three workgroups of one tile (168 registers, some of them spilled) took 113 us where two take 95 (48
 // sequences of up to 4096 rows, 8 kv heads), and more workgroups than fit, taken in turn, 108.
 constexpr int RESIDENT = 2;
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float LN2 = 0.69314718055994530942f;
 
 // what rows that nobody sees are read from: their V must be a number (0 * NaN is NaN)
 __device__ __align__(16) const unsigned char zero_row[1024] = {};
@@ -128,7 +129,8 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
 #pragma unroll
     for (int c = 0; c < S::NA; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float c2 = fmaxf(a.scale * LOG2E, 1.1754944e-38f);           // (0 * -infinity is no number)
+  // scale * log2(e): float storage takes it as two numbers, since its rounding moves every score alike (2^-24 of scores of 20 is 1e-6)
+  const float c2 = a.c2, c2_low = a.c2_low;
 
   // ---- the steps of this wave: KROWS rows each, of every WAVES-th block of the unit
   constexpr int SUB = PAGED_BLOCK / S::KROWS;
@@ -160,6 +162,10 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
       }
     }
   };
+  auto scaled = [&](float x, float less) BEAGLE_INLINE_LAMBDA {
+    if constexpr (BF16) return fmaf(x, c2, -less);
+    else return fmaf(x, c2_low, fmaf(x, c2, -less));
+  };
   // running maximum and sum, probabilities
   auto probabilities = [&]() BEAGLE_INLINE_LAMBDA {
 #pragma unroll
@@ -167,7 +173,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
       float top = sc[t][0][0];
 #pragma unroll
       for (int e = 1; e < 4 * S::KT; ++e) top = fmaxf(top, sc[t][e / 4][e % 4]);
-      const float most = fmaxf(mx[t], max_over_keys(top) * c2), safe = most == -INFINITY ? 0.f : most;
+      const float most = fmaxf(mx[t], scaled(max_over_keys(top), 0.f)), safe = most == -INFINITY ? 0.f : most;
       if (__any(most > mx[t])) {           // (after the first steps seldom)
         const float shrink = exp2_fast(mx[t] - safe);
         sum[t] *= shrink;
@@ -178,7 +184,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
 #pragma unroll
       for (int kt = 0; kt < S::KT; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { p[t][kt][i] = exp2_fast(fmaf(sc[t][kt][i], c2, -safe)); sum[t] += p[t][kt][i]; }
+        for (int i = 0; i < 4; ++i) { p[t][kt][i] = exp2_fast(scaled(sc[t][kt][i], safe)); sum[t] += p[t][kt][i]; }
     }
   };
   // O^T += V^T P^T
@@ -592,6 +598,11 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const bool whole = most <= WHOLE_BLOCKS && (int64_t)a.B * a.G * tiles.blocks <= WHOLE_GROUPS;
   a.target = workers_aimed(R, a.G);
   a.least = 4;                             // a block for every wave
+  // both parts above zero: a hidden row's score is -infinity and has to stay it
+  const double c2 = fmax(a.scale * 1.44269504088896340736, 2e-38);
+  a.c2 = (float)c2;
+  if ((double)a.c2 >= c2) a.c2 = nextafterf(a.c2, 0.f);
+  a.c2_low = fmaxf((float)(c2 - a.c2), 1.1754944e-38f);
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;

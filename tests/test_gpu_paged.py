@@ -122,9 +122,10 @@ HEADS = [("bf16", 4, 4, 128), ("bf16", 8, 2, 128), ("bf16", 5, 1, 128), ("f32", 
 
 @pytest.mark.parametrize("dtype,H,G,d", HEADS)
 @pytest.mark.parametrize("M,page,lens", [(1, 16, [1, 0, 31, 33, 700]), (3, 4, [129, 2, 64]), (7, 64, [65, 1000, 5, 128])])
-def test_lengths_heads_and_pages(dtype, H, G, d, M, page, lens):
+@pytest.mark.parametrize("room", [1, 1000])              # short sequences by what a slot can hold, or not: another launch
+def test_lengths_heads_and_pages(dtype, H, G, d, M, page, lens, room):
     rng = np.random.default_rng(hash((H, G, d, M)) % 1000)
-    W = po.pages_of(max(lens), page) + 1
+    W = po.pages_of(max(lens), page) + room
     c = make(rng, lens, page, W, sum(po.pages_of(n, page) for n in lens) + 3, G, d, dtype)
     check_attend(c, queries(rng, len(lens), M, H, d, dtype), dtype)
 
@@ -140,10 +141,11 @@ def test_window_and_sinks(dtype, H, G, d, window, sinks):
 
 @pytest.mark.parametrize("dtype,H,G,d", [("bf16", 8, 2, 128), ("f32", 4, 4, 64), ("f32", 2, 2, 100)])
 @pytest.mark.parametrize("M,T,window", [(5, 40, 0), (10, 3, 50), (1, 33, 0), (20, 64, 20)])
-def test_drafted_rows_under_a_tree(dtype, H, G, d, M, T, window):
+@pytest.mark.parametrize("W", [96, 1000])
+def test_drafted_rows_under_a_tree(dtype, H, G, d, M, T, window, W):
     rng = np.random.default_rng(M + T)
     true = [300, 0, 31, 64, 700]
-    c = make(rng, [n + T for n in true], 8, 100, 220, G, d, dtype)
+    c = make(rng, [n + T for n in true], 8, W, 220, G, d, dtype)
     tree = rng.random((5, M, T)) < 0.4
     tree[1, 0] = False                                    # with no true row: sees nothing at all
     tree[3] = False
@@ -151,10 +153,11 @@ def test_drafted_rows_under_a_tree(dtype, H, G, d, M, T, window):
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
-def test_drafted_rows_that_are_no_numbers_reach_only_who_sees_them(dtype, d):
+@pytest.mark.parametrize("M,W", [(18, 10), (18, 1000), (6, 10), (6, 1000)])
+def test_drafted_rows_that_are_no_numbers_reach_only_who_sees_them(dtype, d, M, W):
     rng = np.random.default_rng(17)
-    T, M = 20, 18
-    c = make(rng, [90 + T, 33 + T], 16, 10, 20, 2, d, dtype)
+    T = 20
+    c = make(rng, [90 + T, 33 + T], 16, W, 20, 2, d, dtype)
     for s, n in ((0, 90), (1, 33)):
         place = po.rows_of(c, s, n + T)
         c["v"][place[n + 2]][0, ::3] = np.inf
@@ -170,17 +173,18 @@ def test_drafted_rows_that_are_no_numbers_reach_only_who_sees_them(dtype, d):
         clean[name] = np.where(np.isfinite(clean[name]), clean[name], 0.0)
     o2, lse2 = check_attend(clean, q, dtype, n_true=[90, 33], tree=tree)
     spared = ~tree[:, :, [2, 5, 7]].any(-1)
-    assert spared.sum() >= 18
+    assert spared.sum() >= M
     a, b = host(o)[spared], host(o2)[spared]
     assert np.isfinite(a).all() and np.abs(a - b).max() <= (2 ** -7 if dtype == "bf16" else 2 ** -20) * np.abs(b).max()
     assert np.array_equal(host(lse).transpose(0, 2, 1)[spared], host(lse2).transpose(0, 2, 1)[spared])
     assert np.isnan(host(o)[:, 1]).all()
 
 
-@pytest.mark.parametrize("dtype,H,G,d", [("bf16", 32, 8, 128), ("f32", 8, 2, 64)])
-def test_more_rows_than_one_tile(dtype, H, G, d):
+@pytest.mark.parametrize("dtype,H,G,d", [("bf16", 32, 8, 128), ("f32", 8, 2, 64), ("f32", 8, 2, 128)])
+@pytest.mark.parametrize("W", [9, 100])
+def test_more_rows_than_one_tile(dtype, H, G, d, W):
     rng = np.random.default_rng(23)
-    c = make(rng, [260, 31], 32, 9, 12, G, d, dtype)
+    c = make(rng, [260, 31], 32, W, 12, G, d, dtype)
     check_attend(c, queries(rng, 2, 25, H, d, dtype), dtype)                # 100 rows a kv head: tiles of 32, the last ragged
 
 
@@ -408,6 +412,15 @@ def test_fork():
     assert c["refs"] == [0] * 60 and c["lens"] == [0] * 6
     c["table"][2], c["lens"][2] = [60, -7, 3] + [-1] * 27, 20      # pages that are none are passed on, and counted nowhere
     run_fork(c, [2, 0], [2, 2], [10, 20])
+
+
+def test_fork_of_more_than_one_workgroup_takes():
+    rng = np.random.default_rng(23)
+    N = 300
+    c = make(rng, [int(n) for n in rng.integers(0, 120, N)], 4, 40, 12000, 1, 4, "f32", stale=0.0)
+    order = [int(s) for s in rng.permutation(N)]
+    c = run_fork(c, order + order[:20], [int(s) for s in rng.integers(-1, N, N + 20)], [int(n) for n in rng.integers(0, 130, N + 20)])
+    run_fork(c, list(range(N)), order)                             # a permutation
 
 
 def run_compact(c, into, dtype):
