@@ -77,7 +77,7 @@ StepWs draft_layout(const Dims& d) {
   w.b = o; o += align_up((size_t)(d.Tq * d.HD) * d.esz);       // o
   w.pos = o; o += align_up((size_t)d.Tq * sizeof(int32_t));
   w.proj = o; o += align_up(larger(proj_bytes(d, d.HD, d.D, false), proj_bytes(d, d.D, d.HD, false)));
-  w.call = o; o += align_up(paged_attn_ws_bytes((int32_t)d.S, (int32_t)d.H, (int32_t)d.G));
+  w.call = o; o += align_up(paged_attn_ws_bytes((int32_t)d.B, (int32_t)d.S, (int32_t)d.H, (int32_t)d.G));
   w.total = o;
   return w;
 }
@@ -134,7 +134,7 @@ size_t beagle_xattn_paged_workspace_bytes(const beagle_xattn_desc* desc, const b
   Paged p;
   if (check_paged(desc, cache, which == BEAGLE_WS_PAGED_DRAFT || which == BEAGLE_WS_PAGED_KV_APPEND, &p) != BEAGLE_OK) return 0;
   switch (which) {
-    case BEAGLE_WS_PAGED_ATTEND: return align_up(paged_attn_ws_bytes((int32_t)p.d.S, (int32_t)p.d.H, (int32_t)p.d.G));
+    case BEAGLE_WS_PAGED_ATTEND: return align_up(paged_attn_ws_bytes((int32_t)p.d.B, (int32_t)p.d.S, (int32_t)p.d.H, (int32_t)p.d.G));
     case BEAGLE_WS_PAGED_APPEND: return align_up(paged_append_ws_bytes(p.c, (int32_t)p.d.B));
     case BEAGLE_WS_PAGED_FORK: return align_up(paged_fork_ws_bytes(p.c, (int32_t)p.d.B));
     case BEAGLE_WS_PAGED_COMPACT: return align_up(paged_compact_ws_bytes(p.c));

@@ -474,7 +474,8 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
     const int64_t start = base0 + e.upto - e.blocks;
     const PagedShare share = paged_share(start, e.blocks, lo, hi, a.least);
     unsigned long long mine = __ballot(share.from < share.to);
-    base0 += __builtin_amdgcn_readlane(e.upto, 63);
+    const int total = __builtin_amdgcn_readlane(e.upto, 63);
+    base0 += total;
     while (mine) {
       const int l = __ffsll((long long)mine) - 1;
       mine &= mine - 1;
@@ -482,6 +483,10 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
       const int b = b0 + l, slot = of(e.slot), first = of(share.from), last = of(share.to);
       const PagedRows rows = paged_rows(of(e.rows.n), of(e.rows.nt), a.window, a.sinks);
       const bool whole = last - first == rows.blocks;
+      if (first == 0 && head == 0 && rb == 0 && threadIdx.x == 0) {        // for the join: the entry's first worker, and how many have a part
+        const int64_t end = base0 - total + of(e.upto) - 1;
+        a.parts[b] = make_int2(worker, whole ? 1 : paged_worker_of(all, workers, end) - worker + 1);
+      }
       if (used) __syncthreads();
       used = true;
       // a part's sums: one place for the entry that the worker goes on with, one for the entry that it begins
@@ -490,30 +495,18 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
   }
 }
 
-// The units of an entry, in order.  A row is joined by 32 (narrow floats: 16) lanes; ROWS of them share a workgroup, whose other
-// lanes take every (groups / ROWS)-th unit of a row each and meet in LDS.
+// The parts of an entry, in order.  A row is joined by 32 (narrow floats: 16) lanes; ROWS of them share a workgroup, whose other
+// lanes take every (groups / ROWS)-th part of a row each and meet in LDS.
 template <bool BF16, int HDP, int ROWS>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int LANES = HDP / 4, GROUPS = 256 / LANES, SPLIT = GROUPS / ROWS;
   __shared__ float so[GROUPS][HDP];
   __shared__ float sm[GROUPS], sl[GROUPS];
   const int rep = a.H / a.G, R = a.M * rep;
-  // the entry's blocks, and the workers that have a part of them
-  const int lane = threadIdx.x & 63, b = blockIdx.y;
-  const Entry group0 = entry_of(a, lane);
-  const int64_t all = all_blocks(a, group0);
-  const int workers = paged_workers(all, a.target, a.least);
-  int64_t start = 0;
-  Entry e = group0;
-  for (int b0 = 0;; b0 += 64) {
-    if (b0) e = entry_of(a, b0 + lane);
-    if (b < b0 + 64) break;
-    start += __builtin_amdgcn_readlane(e.upto, 63);
-  }
-  const int blocks = __builtin_amdgcn_readlane(e.blocks, b & 63);
-  start += __builtin_amdgcn_readlane(e.upto, b & 63) - blocks;
-  const int w0 = paged_worker_of(all, workers, start), units = paged_worker_of(all, workers, start + blocks - 1) - w0 + 1;
-  if (blocks <= a.least || units <= 1) return;
+  const int b = blockIdx.y;
+  const int2 from = a.parts[b];
+  const int w0 = min(max(from.x, 0), a.target - 1), units = min(from.y, a.target - w0);
+  if (units <= 1) return;
   const int group = threadIdx.x / LANES, ch = 4 * (threadIdx.x % LANES);
   const int n = blockIdx.x * ROWS + group / SPLIT;         // row of the entry: kv head, then query and head of the group
   const int head = n / R, r = n % R, qi = r / rep, h = head * rep + r % rep;
@@ -580,10 +573,10 @@ int workers_aimed(int R, int G) {
 
 }  // namespace
 
-// Sums of parts: a worker has at most two (see paged_index.h).
-size_t paged_attn_ws_bytes(int32_t M, int32_t H, int32_t G) {
+// Sums of parts: a worker has at most two (see paged_index.h).  And for each entry who has them.
+size_t paged_attn_ws_bytes(int32_t B, int32_t M, int32_t H, int32_t G) {
   const int64_t R = (int64_t)M * (H / G);
-  return (size_t)2 * workers_aimed((int)R, G) * G * R * (128 + 2) * sizeof(float);
+  return (size_t)2 * workers_aimed((int)R, G) * G * R * (128 + 2) * sizeof(float) + (size_t)B * sizeof(int2);
 }
 
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
@@ -606,6 +599,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const int64_t rows = (int64_t)2 * a.target * a.G * R;
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
+  a.parts = (int2*)(a.ml + rows * 2);
   const int heads8 = (whole ? a.B : a.target) * a.G;
   const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(whole ? 512 : 256);
   const bool tree = a.n_true != nullptr, narrow = !bf16 && a.d <= 64;
