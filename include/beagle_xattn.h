@@ -647,9 +647,9 @@ beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const bea
  * slots never see the change.  With BEAGLE_FLAG_ROPE the K rows are rotated, at
  * desc->rope_positions[b * M + i] or, if that is NULL, at their row numbers.
  * Pages are taken lowest number first, in the order of the entries; pages
- * given up in the call can be taken in it.  If the pool runs out, the entries
- * that the pages reached before it did not get any keep their first pos[b] rows and
- * store none, as does an entry whose rows exceed what a slot can hold; short_pages
+ * given up in the call can be taken in it.  If the pool runs out, the first entry
+ * whose pages are not all there, and every later one that lacks a page, keep their
+ * first pos[b] rows and store none, as does an entry whose rows exceed what a slot can hold; short_pages
  * (DEVICE, one int32, or NULL) takes the number of pages missing in all, 0 if
  * everything was stored.  Of two entries with one slot the first counts.
  *   in    : k_new, v_new [B,M,G,d]; slots, pos, n_new [B] or NULL
@@ -683,7 +683,7 @@ beagle_status beagle_xattn_paged_fork(const beagle_xattn_desc* desc, const beagl
  * that nothing moved to keep their content.  If `into` has fewer pages than
  * are live (or a slot holds more than its slot_pages), the sequences end before their first row
  * that has no page there; short_pages (DEVICE, one int32, or NULL) takes the
- * number of live pages that did not fit its n_pages.  desc: batch is not read.
+ * number of live pages that did not fit its n_pages.  desc: batch and seq_q do not matter.
  *   in : cache    out: into
  * Workspace: BEAGLE_WS_PAGED_COMPACT.
  */

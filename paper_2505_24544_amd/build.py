@@ -26,7 +26,7 @@ FLAGS = [
 # 3000 in 8 groups 28.5 / 27.8 (the kernels of up to 16 rows take 80 accumulation registers without, none with).  The other
 # files' kernels come out the same either way.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-VGPR_FORM_SOURCES = ("attn_bwd_bf16.hip", "decode_bf16.hip", "paged_attn.hip")
+VGPR_FORM_SOURCES = ("attn_bwd_bf16.hip", "decode_bf16.hip")
 
 
 def sources():

@@ -5,11 +5,17 @@
 // Bound: HBM.  A visible row is fetched once for all queries of its kv head (they share the matrix instructions' columns),
 // 4 * d * (queries of the head) operations per 4 * d bytes, far below the matrix pipe's rate.
 //
-// Split.  The visible rows of an entry are counted in blocks of 32; a unit is a run of blocks of one entry, as long as all
-// blocks of the batch divided by the units aimed at, so sequences of any mix of lengths fill the chip alike and the host
-// needs no lengths.  One workgroup takes a unit of one kv head; its four waves take every fourth block and are joined
-// through LDS.  An entry of one unit is finished there; the others leave unnormalised sums, maximum and weight
-// of each unit in the workspace, and a second launch joins them in the order of the rows.
+// Split.  The visible rows of an entry are counted in blocks of 32.  The blocks of all entries, one behind the other, are cut into
+// as many equal runs as there are workers, so sequences of any mix of lengths fill the chip alike and the host needs no lengths.  A
+// worker is one workgroup for each kv head (and row block); its four waves take every fourth block of an entry and are joined
+// through LDS.  An entry that one worker has to itself is finished there; of the others each worker leaves the unnormalised sum,
+// the maximum and the weight of its part in the workspace, and a second launch joins them in the order of the rows.  Few short entries go to a
+// workgroup each instead, in one launch.
+//
+// Measured (MI355X; rows of 8 kv heads, 32 query heads unless said; a graph's replays): 48 sequences of up to 4096 rows 94 us
+// (462 MB, 4.9 TB/s), 4 of up to 32768 with 40 heads 355 (1974 MB, 5.6; a kernel that only reads reaches 6.0), 12 of up to 4096
+// with 10 queries each under a tree 44, one of 777 rows of 32 kv heads 10.3.  The counters have every visible row fetched once from HBM, and waves that
+// wait for memory 55 to 60 % of their time.
 //
 // Layout.  A wave keeps everything in registers and shares nothing until its end: S^T = K Q^T puts a query in a
 // column (lane % 16) and four keys in a lane, which is at once the layout that O^T = V^T P^T wants of P^T.  V rows are
@@ -25,7 +31,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// workgroups that fit on a compute unit at a time (registers)
 // Workgroups that a compute unit holds at a time, and that the registers are made for.  Eight waves with 16 KB of rows on the way each keep
 // memory busy; three workgroups of one tile (168 registers, some of them spilled) took 113 us where two take 95 (48
 // sequences of up to 4096 rows, 8 kv heads), and more workgroups than fit, taken in turn, 108.
@@ -39,6 +44,7 @@ __device__ __align__(16) const unsigned char zero_row[1024] = {};
 // as one into global memory, and would wait for all loads wherever it needs one.
 typedef uint64_t addr_t;
 __device__ __forceinline__ u32x4 load16(addr_t p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
+
 // Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks of the row of all blocks that it
 // and the lanes before it have.
 struct Entry { int slot, blocks, upto; PagedRows rows; };
@@ -132,7 +138,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
   // scale * log2(e): float storage takes it as two numbers, since its rounding moves every score alike (2^-24 of scores of 20 is 1e-6)
   const float c2 = a.c2, c2_low = a.c2_low;
 
-  // ---- the steps of this wave: KROWS rows each, of every WAVES-th block of the unit
+  // ---- the steps of this wave: KROWS rows each, of every WAVES-th block
   constexpr int SUB = PAGED_BLOCK / S::KROWS;
   const int steps = last > first + wave ? (last - first - wave + WAVES - 1) / WAVES * SUB : 0;
   const int shift = a.c.shift;
@@ -293,7 +299,8 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
         if (!(st.seen >> e & 1)) sc[t][e / 4][e % 4] = -INFINITY;
   };
   // Steps of true rows: the rows of the next step travel while this one is computed, its page numbers a step further ahead.  K's registers
-  // are free once the scores are there; V has a second set (4 sequences of up to 32768 rows, 40 heads: 365 us without, 355 with).  (Addresses of whole steps in scalar registers, and half the vector instructions with that: the registers that
+  // are free once the scores are there; V has a second set (4 sequences of up to 32768 rows, 40 heads: 365 us without, 355 with).
+  // (Addresses of whole steps in scalar registers, and half the vector instructions with that: the registers that
   // two ways of addressing take cost 3 to 30 % instead.)
   int plain = steps;
   if constexpr (TREE)
@@ -389,7 +396,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
       }
     }
 
-  // ---- the waves' shares, then the unit's result
+  // ---- the waves' shares, then the workgroup's result
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     float l = sum[t];
@@ -450,7 +457,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
   constexpr int WAVES = WHOLE ? 8 : 4;
   __shared__ Shared<Shape<BF16, NH>, RT, WAVES> shared;
   const int lane = threadIdx.x & 63;
-  // row blocks of one unit and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
+  // row blocks of one worker and head stand eight workgroups apart: on one XCD, whose L2 has the rows after the first
   const int id = blockIdx.x, ug = id / (8 * rowblocks) * 8 + id % 8, rb = id / 8 % rowblocks;
   const int head = ug % a.G, worker = ug / a.G;
   if constexpr (WHOLE) {
@@ -505,8 +512,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   const int rep = a.H / a.G, R = a.M * rep;
   const int b = blockIdx.y;
   const int2 from = a.parts[b];
-  const int w0 = min(max(from.x, 0), a.target - 1), units = min(from.y, a.target - w0);
-  if (units <= 1) return;
+  const int w0 = min(max(from.x, 0), a.target - 1), shares = min(from.y, a.target - w0);
+  if (shares <= 1) return;
   const int group = threadIdx.x / LANES, ch = 4 * (threadIdx.x % LANES);
   const int n = blockIdx.x * ROWS + group / SPLIT;         // row of the entry: kv head, then query and head of the group
   const int head = n / R, r = n % R, qi = r / rep, h = head * rep + r % rep;
@@ -522,19 +529,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   if (n < a.G * R) {
     const int64_t row0 = ((int64_t)2 * w0 * a.G + head) * R + r, step = (int64_t)a.G * R;
     constexpr int AT_ONCE = 4;
-    for (int i = group % SPLIT; i < units; i += SPLIT * AT_ONCE) {
+    for (int i = group % SPLIT; i < shares; i += SPLIT * AT_ONCE) {
       float2 ml[AT_ONCE];
       f32x4 po[AT_ONCE];
 #pragma unroll
       for (int e = 0; e < AT_ONCE; ++e) {
-        const int n = min(i + e * SPLIT, units - 1);
+        const int n = min(i + e * SPLIT, shares - 1);
         const int64_t row = row0 + step * (n ? 2 * n : 1);
         ml[e] = *(const float2*)(a.ml + row * 2);
         po[e] = *(const f32x4*)(a.part + row * HDP + ch);
       }
 #pragma unroll
       for (int e = 0; e < AT_ONCE; ++e)
-        if (i + e * SPLIT < units) join(ml[e].x, ml[e].y, po[e]);
+        if (i + e * SPLIT < shares) join(ml[e].x, ml[e].y, po[e]);
     }
   }
   if constexpr (SPLIT > 1) {

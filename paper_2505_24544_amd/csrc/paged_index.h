@@ -1,5 +1,5 @@
 // Index code of the paged cache, for the device and (in a test) for the host: which rows of a sequence a call looks at, in
-// blocks of 32, how blocks become units of work, and where a row stands.  Whatever the caller's arrays hold, nothing here
+// blocks of 32, how they are divided among workers, and where a row stands.  Whatever the caller's arrays hold, nothing here
 // names a place outside them.
 #pragma once
 #include <stdint.h>

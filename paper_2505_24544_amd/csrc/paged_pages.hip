@@ -13,8 +13,6 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int PLAN = 1024;                 // threads of a planning workgroup
 constexpr int PLAN_WAVES = PLAN / 64;
 
-// counts that other waves of the launch have changed: past the vector cache
-__device__ __forceinline__ int load_count(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void add_count(int32_t* p, int v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool is_page(const PagedCache& c, int p) { return (unsigned)p < (unsigned)c.P; }
 // every thread's earlier stores and atomics are seen by the workgroup's later loads: a barrier, which waits for them, and vector
@@ -214,21 +212,21 @@ __global__ __launch_bounds__(256) void paged_append_store_kernel(PagedAppendArgs
   const int b = blockIdx.y, tid = threadIdx.x, in_page = (1 << a.c.shift) - 1;
   const Entry e = ws.entry[b];
   const bool fresh = (int)blockIdx.x < new_blocks;
-  const int r0 = (fresh ? blockIdx.x : blockIdx.x - new_blocks) * STORE_ROWS;
-  const int rows = fresh ? e.n : e.from >= 0 ? e.pos & in_page : 0;
+  const int r0 = fresh ? blockIdx.x * STORE_ROWS : 0, rows = fresh ? e.n : e.from >= 0 ? e.pos & in_page : 0;
   if (r0 >= rows) return;
-  const int here = min(STORE_ROWS, rows - r0);
   const int64_t row_bytes = (int64_t)a.G * a.d * E;
   const int32_t* table = a.c.table + (int64_t)e.slot * a.c.W;
   if (!fresh) {
-    const int64_t to = (((int64_t)table[e.pos >> a.c.shift] << a.c.shift) + r0) * row_bytes;
-    const int64_t from = (((int64_t)e.from << a.c.shift) + r0) * row_bytes;
-    for (int64_t i = (int64_t)tid * 16; i < here * row_bytes; i += 256 * 16) {
+    const int64_t to = ((int64_t)table[e.pos >> a.c.shift] << a.c.shift) * row_bytes, from = ((int64_t)e.from << a.c.shift) * row_bytes;
+    constexpr int64_t piece = 256 * 16;
+    const int64_t step = (int64_t)(gridDim.x - new_blocks) * piece;
+    for (int64_t i = (int64_t)(blockIdx.x - new_blocks) * piece + tid * 16; i < rows * row_bytes; i += step) {
       *(u32x4*)((char*)a.c.k + to + i) = *(const u32x4*)((const char*)a.c.k + from + i);
       *(u32x4*)((char*)a.c.v + to + i) = *(const u32x4*)((const char*)a.c.v + from + i);
     }
     return;
   }
+  const int here = min(STORE_ROWS, rows - r0);
   const int half = a.d >> 1;
   if (a.rope) {
     for (int i = tid; i < here * 64; i += 256) {
@@ -509,7 +507,11 @@ void launch_paged_append(bool bf16, const PagedAppendArgs& a, void* ws, hipStrea
     hipLaunchKernelGGL(paged_append_plan_kernel, dim3(1), dim3(PLAN), 0, s, a, w);
   }
   const int new_blocks = (a.M + STORE_ROWS - 1) / STORE_ROWS;
-  const int copy_blocks = ((1 << a.c.shift) - 1 + STORE_ROWS - 1) / STORE_ROWS;
+  // Kept rows of copied pages: most entries have none, so their workgroups end at once, but starting them takes time too.  48 sequences,
+  // a row each, pages of 4096 rows: 18.7 us with a workgroup for every four rows, 9.6 so (every entry with a copy: 135 / 140).
+  int copy_blocks = ((1 << a.c.shift) - 1 + STORE_ROWS - 1) / STORE_ROWS;
+  const int some = 4096 / a.B > 16 ? 4096 / a.B : 16;
+  if (copy_blocks > some) copy_blocks = some;
   ProfScope ps("paged_append_store", s);
   const dim3 grid((unsigned)(new_blocks + copy_blocks), (unsigned)a.B);
   if (bf16) hipLaunchKernelGGL(paged_append_store_kernel<true>, grid, dim3(256), 0, s, a, w, new_blocks);

@@ -357,6 +357,15 @@ def test_append_copies_shared_pages_and_only_those():
         run_append(c, dtype, kn, vn, pos=[20, 20, 20, 20, 20])
 
 
+def test_append_copies_large_pages_of_many_entries():
+    """More to copy of each page than the workgroups of an entry take at once."""
+    rng = np.random.default_rng(6)
+    c = make(rng, [255] + [0] * 127, 256, 2, 260, 2, 128, "f32", stale=2.0)
+    c = po.fork(c, list(range(1, 128)), [0] * 127, [int(n) for n in rng.integers(1, 256, 127)])
+    kn, vn = new_rows(rng, 128, 2, 2, 128, "f32")
+    run_append(c, "f32", kn, vn, n_new=[int(n) for n in rng.integers(0, 3, 128)])
+
+
 def test_append_to_a_full_pool():
     rng = np.random.default_rng(7)
     c = make(rng, [10, 10, 10, 10, 8], 8, 6, 12, 1, 64, "f32", stale=1.0)       # 9 of 12 pages held
