@@ -14,8 +14,8 @@
 //
 // Measured (MI355X; rows of 8 kv heads, 32 query heads unless said; a graph's replays): 48 sequences of up to 4096 rows 94 us
 // (462 MB, 4.9 TB/s), 4 of up to 32768 with 40 heads 355 (1974 MB, 5.6; a kernel that only reads reaches 6.0), 12 of up to 4096
-// with 10 queries each under a tree 44, one of 777 rows of 32 kv heads 10.3.  The counters have every visible row fetched once from HBM, and waves that
-// wait for memory 55 to 60 % of their time.
+// with 10 queries each under a tree 44, one of 777 rows of 32 kv heads 10.3.  The counters have every visible row fetched once from HBM, and
+// vector and matrix instructions issue in a tenth of the waves' time: they wait for rows, or for room to ask for more.
 //
 // Layout.  A wave keeps everything in registers and shares nothing until its end: S^T = K Q^T puts a query in a
 // column (lane % 16) and four keys in a lane, which is at once the layout that O^T = V^T P^T wants of P^T.  V rows are
