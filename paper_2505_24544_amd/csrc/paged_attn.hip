@@ -45,9 +45,19 @@ __device__ __align__(16) const unsigned char zero_row[1024] = {};
 typedef uint64_t addr_t;
 __device__ __forceinline__ u32x4 load16(addr_t p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
 
-// Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks of the row of all blocks that it
-// and the lanes before it have.
-struct Entry { int slot, blocks, upto; PagedRows rows; };
+// Inclusive sum over the lanes: within rows of 16, then what the rows before have.
+__device__ __forceinline__ int sum_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);        // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+// Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks and runs of blocks that it and the lanes
+// before it have.
+struct Entry { int slot, blocks, upto, runs_upto; PagedRows rows; };
 __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
   Entry e;
   const int at = min(b, a.B - 1);
@@ -56,17 +66,19 @@ __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
   const int len = a.c.lens[max(e.slot, 0)];
   e.rows = paged_rows(min(e.slot < 0 ? 0 : paged_clamped(len, a.c.W, a.c.shift), a.bound), nt, a.window, a.sinks);
   e.blocks = b < a.B ? e.rows.blocks : 0;
-  e.upto = e.blocks;                       // (64 entries of 2^23 blocks: fits)
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int x = __shfl_up(e.upto, m);
-    if ((int)(threadIdx.x & 63) >= m) e.upto += x;
-  }
+  e.upto = sum_upto(e.blocks);             // (64 entries of 2^23 blocks: fits)
+  e.runs_upto = sum_upto(paged_runs(e.blocks, a.least));
   return e;
 }
-__device__ __forceinline__ int64_t all_blocks(const PagedAttnArgs& a, const Entry& first) {
-  int64_t all = __builtin_amdgcn_readlane(first.upto, 63);
-  for (int b0 = 64; b0 < a.B; b0 += 64) all += __builtin_amdgcn_readlane(entry_of(a, b0 + (threadIdx.x & 63)).upto, 63);
+struct All { int64_t blocks, runs; };
+__device__ __forceinline__ All all_of(const PagedAttnArgs& a, const Entry& first) {
+  auto last = [](int v) { return __builtin_amdgcn_readlane(v, 63); };
+  All all = {last(first.upto), last(first.runs_upto)};
+  for (int b0 = 64; b0 < a.B; b0 += 64) {
+    const Entry e = entry_of(a, b0 + (threadIdx.x & 63));
+    all.blocks += last(e.upto);
+    all.runs += last(e.runs_upto);
+  }
   return all;
 }
 
@@ -469,7 +481,9 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
     return;
   }
   const Entry group0 = entry_of(a, lane);
-  const int64_t all = all_blocks(a, group0);
+  const All sums = all_of(a, group0);
+  const bool apart = paged_apart(sums.runs, a.target);
+  const int64_t all = apart ? sums.runs * a.least : sums.blocks;         // blocks as they are counted here
   const int workers = paged_workers(all, a.target, a.least);
   if (worker >= workers) return;
   const int64_t lo = paged_cut(all, workers, worker), hi = paged_cut(all, workers, worker + 1);
@@ -478,11 +492,12 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
   for (int b0 = 0; b0 < a.B && base0 < hi; b0 += 64) {
     Entry e = group0;
     if (b0) e = entry_of(a, b0 + lane);
-    const int64_t start = base0 + e.upto - e.blocks;
+    const int runs = paged_runs(e.blocks, a.least), upto = paged_counted(apart, e.upto, e.runs_upto, a.least);
+    const int64_t start = base0 + upto - paged_counted(apart, e.blocks, runs, a.least);
     const PagedShare share = paged_share(start, e.blocks, lo, hi, a.least);
     unsigned long long mine = __ballot(share.from < share.to);
-    const int total = __builtin_amdgcn_readlane(e.upto, 63);
-    base0 += total;
+    const int64_t before = base0;
+    base0 += __builtin_amdgcn_readlane(upto, 63);
     while (mine) {
       const int l = __ffsll((long long)mine) - 1;
       mine &= mine - 1;
@@ -491,7 +506,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
       const PagedRows rows = paged_rows(of(e.rows.n), of(e.rows.nt), a.window, a.sinks);
       const bool whole = last - first == rows.blocks;
       if (first == 0 && head == 0 && rb == 0 && threadIdx.x == 0) {        // for the join: the entry's first worker, and how many have a part
-        const int64_t end = base0 - total + of(e.upto) - 1;
+        const int64_t end = before + of((int)(start - before)) + rows.blocks - 1;
         a.parts[b] = make_int2(worker, whole ? 1 : paged_worker_of(all, workers, end) - worker + 1);
       }
       if (used) __syncthreads();
@@ -561,11 +576,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
-// Entries of up to so many blocks (three steps of eight waves), on one workgroup each if there are no more than so many: a
-// compute unit gets some 50 GB/s to itself, 2.45 us a step, so longer ones are cut.  One sequence of 8 kv heads on one
-// workgroup a head / cut and joined by a second launch, us: 256 rows 7.1 / 10.8, 512 9.5 / 10.8, 1024 14.6 / 10.9; and a launch takes the
-// host 3.3.
-constexpr int WHOLE_BLOCKS = 24, WHOLE_GROUPS = 256;
+// An entry goes whole to a workgroup for each head if there are at most WHOLE_GROUPS of them (a compute unit each) and it has at most two
+// blocks for each of the eight waves, one if a wave reads a block in two steps of more than 64 floats; or, in bf16, no more blocks than a quarter of
+// the workgroups: then the cut calls are bound by the memory's rate and these, without a second launch, reach as much.
+// A workgroup of its own / cut and joined, us (bf16, 1 query, rows in the caches of a graph's replays): 1 sequence of 8 heads, 400 rows 9.3 / 10.1, 700
+// 11.9 / 10.0; 8 sequences of 32 heads, 1000 rows 24.0 / 27.5, 2000 42.3 / 46.1 (uneven lengths 33.8 / 34.3); 20 of 4 heads of 128 floats, 400 rows
+// 20.9 / 19.3.
+constexpr int WHOLE_GROUPS = 256;
+int whole_blocks(bool bf16, int d, int64_t groups) {
+  if (!bf16) return d <= 64 ? 16 : 8;
+  return groups / 4 > 16 ? (int)(groups / 4) : 16;
+}
 constexpr int MAX_TILES = 2;               // of 16 query rows that a workgroup takes
 struct Tiles { int each, blocks; };        // tiles of a workgroup, workgroups that the rows of a kv head take
 Tiles tiles_of(int R) {
@@ -595,7 +616,8 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
     const int64_t seen = (int64_t)(a.window / PAGED_BLOCK) + a.sinks / PAGED_BLOCK + 4;
     if (seen < most) most = seen;
   }
-  const bool whole = most <= WHOLE_BLOCKS && (int64_t)a.B * a.G * tiles.blocks <= WHOLE_GROUPS;
+  const int64_t groups = (int64_t)a.B * a.G * tiles.blocks;
+  const bool whole = groups <= WHOLE_GROUPS && most <= whole_blocks(bf16, a.d, groups);
   a.target = workers_aimed(R, a.G);
   a.least = 4;                             // a block for every wave
   // both parts above zero: a hidden row's score is -infinity and has to stay it

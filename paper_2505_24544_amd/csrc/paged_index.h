@@ -48,6 +48,11 @@ PAGED_HD bool paged_all_seen(const PagedRows& r, int first, int count) {
 // Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs.  Worker w of n takes
 // blocks paged_cut(w) .. paged_cut(w + 1) - 1 of that row; an entry of up to `least` blocks is not cut but goes whole to the worker that has
 // its first block.  A worker so has at most two entries in part, its first and its last.
+// If there are workers enough for every `least` blocks of every entry, an entry counts as a multiple of `least`: then no worker has two
+// entries, one behind the other.
+PAGED_HD int paged_runs(int blocks, int least) { return (blocks + least - 1) / least; }
+PAGED_HD bool paged_apart(int64_t runs, int target) { return runs <= target; }
+PAGED_HD int paged_counted(bool apart, int blocks, int runs, int least) { return apart ? runs * least : blocks; }
 PAGED_HD int paged_workers(int64_t all, int target, int least) {
   const int64_t n = (all + least - 1) / least;
   return n < target ? (int)n : target;

@@ -32,8 +32,13 @@ int main() {
       std::printf("\n");
     } else if (what == "workers") {
       std::vector<long long> start;
-      long long all = 0;
-      for (size_t i = 2; i < x.size(); ++i) { start.push_back(all); all += x[i]; }
+      long long all = 0, runs = 0;
+      for (size_t i = 2; i < x.size(); ++i) runs += paged_runs((int)x[i], (int)x[1]);
+      const bool apart = paged_apart(runs, (int)x[0]);
+      for (size_t i = 2; i < x.size(); ++i) {
+        start.push_back(all);
+        all += paged_counted(apart, (int)x[i], paged_runs((int)x[i], (int)x[1]), (int)x[1]);
+      }
       const int n = paged_workers(all, (int)x[0], (int)x[1]);
       std::printf("%d", n);
       for (int w = 0; w < n; ++w)

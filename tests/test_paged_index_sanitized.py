@@ -1,5 +1,5 @@
 """The paged cache's index code (csrc/paged_index.h) compiled for the HOST with AddressSanitizer and
-UndefinedBehaviorSanitizer: which rows a window shows, which blocks are walked, how they become units, and what hostile slot
+UndefinedBehaviorSanitizer: which rows a window shows, which blocks are walked, how workers share them, and what hostile slot
 numbers, lengths and page numbers turn into.  CPU only."""
 import os
 import random
@@ -58,7 +58,8 @@ def test_workers_share_all_blocks_evenly(driver):
     for (target, least, blocks), got in zip(cases, driver(["workers %d %d %s" % (t, k, " ".join(map(str, n))) for t, k, n in cases])):
         n, ends = got[0], got[len(got) - 2 * len(blocks):]
         shares = [got[i: i + 4] for i in range(1, len(got) - len(ends), 4)]
-        assert 1 <= n <= target and (n == target or n == -(-sum(blocks) // least))
+        runs = sum(-(-size // least) for size in blocks)
+        assert 1 <= n <= target and n == (runs if runs <= target else min(target, -(-sum(blocks) // least)))
         parts = {}
         for w, e, a, b in shares:
             parts.setdefault(e, []).append((w, a, b))
@@ -74,7 +75,9 @@ def test_workers_share_all_blocks_evenly(driver):
                 assert len(parts[e]) == 1 and parts[e][0][0] == ends[2 * e]
             else:
                 assert [p[0] for p in parts[e]] == list(range(ends[2 * e], ends[2 * e + 1] + 1))
-        assert max(work) <= even + 1 + least
+        assert max(work) <= (least if runs <= target else even + 1 + least)
+        if runs <= target:                              # a worker for every run: nobody has two entries
+            assert sorted(v for v, e, a, b in shares) == list(range(n))
         for w in range(n):                              # at most one entry gone on with and one begun in part: two places for sums
             part = [(a, b, e) for v, e, a, b in shares if v == w and b - a < blocks[e]]
             assert sum(a > 0 for a, b, e in part) <= 1 and sum(a == 0 for a, b, e in part) <= 1
