@@ -29,7 +29,8 @@ struct PagedAttnArgs {
   int32_t window, sinks;                   // window 0: none
   float* part; float* ml;                  // sums of the parts of entries that several workers share
   int2* parts;                             // [B] first worker of an entry, how many have a part of it
-  int32_t target, least;                   // see paged_workers
+  int32_t target;                          // workers, at most
+  bool long_runs;                          // see paged_split
 };
 size_t paged_attn_ws_bytes(int32_t B, int32_t M, int32_t H, int32_t G);
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s);

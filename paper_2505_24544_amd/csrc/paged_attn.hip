@@ -55,9 +55,8 @@ __device__ __forceinline__ int sum_upto(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
-// Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks and runs of blocks that it and the lanes
-// before it have.
-struct Entry { int slot, blocks, upto, runs_upto; PagedRows rows; };
+// Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks that it and the lanes before it have.
+struct Entry { int slot, blocks, upto; PagedRows rows; };
 __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
   Entry e;
   const int at = min(b, a.B - 1);
@@ -67,19 +66,25 @@ __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {
   e.rows = paged_rows(min(e.slot < 0 ? 0 : paged_clamped(len, a.c.W, a.c.shift), a.bound), nt, a.window, a.sinks);
   e.blocks = b < a.B ? e.rows.blocks : 0;
   e.upto = sum_upto(e.blocks);             // (64 entries of 2^23 blocks: fits)
-  e.runs_upto = sum_upto(paged_runs(e.blocks, a.least));
   return e;
 }
-struct All { int64_t blocks, runs; };
-__device__ __forceinline__ All all_of(const PagedAttnArgs& a, const Entry& first) {
+__device__ __forceinline__ PagedSplit split_of(const PagedAttnArgs& a, const Entry& first) {
   auto last = [](int v) { return __builtin_amdgcn_readlane(v, 63); };
-  All all = {last(first.upto), last(first.runs_upto)};
+  auto runs_of = [&](const Entry& e, int shift) { return last(sum_upto(paged_runs(e.blocks, shift))); };
+  int64_t all = last(first.upto), runs = runs_of(first, PAGED_RUN);
   for (int b0 = 64; b0 < a.B; b0 += 64) {
     const Entry e = entry_of(a, b0 + (threadIdx.x & 63));
-    all.blocks += last(e.upto);
-    all.runs += last(e.runs_upto);
+    all += last(e.upto);
+    runs += runs_of(e, PAGED_RUN);
   }
-  return all;
+  int shift = PAGED_RUN;
+  bool apart = paged_apart(all, runs, shift, a.target);
+  if (!apart && a.long_runs && a.B <= 64) {
+    shift = PAGED_LONG_RUN;
+    runs = runs_of(first, shift);
+    apart = paged_apart(all, runs, shift, a.target);
+  }
+  return paged_split(all, runs, shift, apart, a.target);
 }
 
 // over the four lanes that hold a column's keys
@@ -481,20 +486,17 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
     return;
   }
   const Entry group0 = entry_of(a, lane);
-  const All sums = all_of(a, group0);
-  const bool apart = paged_apart(sums.runs, a.target);
-  const int64_t all = apart ? sums.runs * a.least : sums.blocks;         // blocks as they are counted here
-  const int workers = paged_workers(all, a.target, a.least);
-  if (worker >= workers) return;
-  const int64_t lo = paged_cut(all, workers, worker), hi = paged_cut(all, workers, worker + 1);
+  const PagedSplit split = split_of(a, group0);
+  if (worker >= split.workers) return;
+  const int64_t lo = paged_cut(split, worker), hi = paged_cut(split, worker + 1);
   int64_t base0 = 0;                       // blocks before this group of entries
   bool used = false;                       // LDS holds another entry's shares
   for (int b0 = 0; b0 < a.B && base0 < hi; b0 += 64) {
     Entry e = group0;
     if (b0) e = entry_of(a, b0 + lane);
-    const int runs = paged_runs(e.blocks, a.least), upto = paged_counted(apart, e.upto, e.runs_upto, a.least);
-    const int64_t start = base0 + upto - paged_counted(apart, e.blocks, runs, a.least);
-    const PagedShare share = paged_share(start, e.blocks, lo, hi, a.least);
+    const int counted = paged_counted(split, e.blocks), upto = split.apart ? sum_upto(counted) : e.upto;
+    const int64_t start = base0 + upto - counted;
+    const PagedShare share = paged_share(split, start, e.blocks, lo, hi);
     unsigned long long mine = __ballot(share.from < share.to);
     const int64_t before = base0;
     base0 += __builtin_amdgcn_readlane(upto, 63);
@@ -507,7 +509,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged
       const bool whole = last - first == rows.blocks;
       if (first == 0 && head == 0 && rb == 0 && threadIdx.x == 0) {        // for the join: the entry's first worker, and how many have a part
         const int64_t end = before + of((int)(start - before)) + rows.blocks - 1;
-        a.parts[b] = make_int2(worker, whole ? 1 : paged_worker_of(all, workers, end) - worker + 1);
+        a.parts[b] = make_int2(worker, whole ? 1 : paged_worker_of(split, end) - worker + 1);
       }
       if (used) __syncthreads();
       used = true;
@@ -619,7 +621,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   const int64_t groups = (int64_t)a.B * a.G * tiles.blocks;
   const bool whole = groups <= WHOLE_GROUPS && most <= whole_blocks(bf16, a.d, groups);
   a.target = workers_aimed(R, a.G);
-  a.least = 4;                             // a block for every wave
+  a.long_runs = bf16;                      // (floats: what a block costs is its products, and more workers take less)
   // both parts above zero: a hidden row's score is -infinity and has to stay it
   const double c2 = fmax(a.scale * 1.44269504088896340736, 2e-38);
   a.c2 = (float)c2;
@@ -650,7 +652,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
     else if (narrow) with(int_c<0>{}, int_c<1>{});
     else with(int_c<0>{}, int_c<2>{});
   }
-  if (whole || most <= a.least) return;    // no entry is cut: nothing to join
+  if (whole || most <= 1 << PAGED_RUN) return;    // no entry is cut: nothing to join
   ProfScope ps("paged_join", s);
   auto join = [&](auto bf_, auto hdp_) {
     constexpr bool BF = decltype(bf_)::value != 0;

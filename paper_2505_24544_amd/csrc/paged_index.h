@@ -45,24 +45,32 @@ PAGED_HD bool paged_all_seen(const PagedRows& r, int first, int count) {
   return first + count <= r.nt && (r.window == 0 || first + count <= r.sinks || first >= r.nt - r.window);
 }
 
-// Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs.  Worker w of n takes
-// blocks paged_cut(w) .. paged_cut(w + 1) - 1 of that row; an entry of up to `least` blocks is not cut but goes whole to the worker that has
-// its first block.  A worker so has at most two entries in part, its first and its last.
-// If there are workers enough for every `least` blocks of every entry, an entry counts as a multiple of `least`: then no worker has two
-// entries, one behind the other.
-PAGED_HD int paged_runs(int blocks, int least) { return (blocks + least - 1) / least; }
-PAGED_HD bool paged_apart(int64_t runs, int target) { return runs <= target; }
-PAGED_HD int paged_counted(bool apart, int blocks, int runs, int least) { return apart ? runs * least : blocks; }
-PAGED_HD int paged_workers(int64_t all, int target, int least) {
-  const int64_t n = (all + least - 1) / least;
-  return n < target ? (int)n : target;
+// Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs, one for each; an entry of up to
+// four blocks is not cut but goes whole to the worker that has its first block.  A worker so has at most two entries in part, its first
+// and its last.  Where each entry can be cut for itself into runs of four blocks (or of eight, if that is not much more than an equal share), with
+// a worker for each run, entries count as multiples of the run's length instead: then no worker has two, one behind the other.
+constexpr int PAGED_RUN = 2, PAGED_LONG_RUN = 3;         // runs of 1 << PAGED_RUN or 1 << PAGED_LONG_RUN blocks
+struct PagedSplit { int64_t all; int workers, shift; bool apart; };
+PAGED_HD int paged_runs(int blocks, int shift) { return (blocks + (1 << shift) - 1) >> shift; }
+PAGED_HD bool paged_apart(int64_t all, int64_t runs, int shift, int target) {
+  return runs <= target && (shift == PAGED_RUN || ((1 << shift) - 5) * (int64_t)target <= all);
 }
-PAGED_HD int64_t paged_cut(int64_t all, int n, int w) { return all * w / n; }
-PAGED_HD int paged_worker_of(int64_t all, int n, int64_t block) { return (int)(((block + 1) * n - 1) / all); }
+// `runs`: those of all entries, each for itself; not read unless `apart`
+PAGED_HD PagedSplit paged_split(int64_t all, int64_t runs, int shift, bool apart, int target) {
+  if (apart) return PagedSplit{runs << shift, (int)runs, shift, true};
+  const int64_t n = (all + (1 << PAGED_RUN) - 1) >> PAGED_RUN;
+  return PagedSplit{all, n < target ? (int)n : target, PAGED_RUN, false};
+}
+PAGED_HD int paged_counted(const PagedSplit& s, int blocks) { return s.apart ? paged_runs(blocks, s.shift) << s.shift : blocks; }
+// worker w takes blocks paged_cut(w) .. paged_cut(w + 1) - 1 of the row
+PAGED_HD int64_t paged_cut(const PagedSplit& s, int w) { return s.apart ? (int64_t)w << s.shift : s.all * w / s.workers; }
+PAGED_HD int paged_worker_of(const PagedSplit& s, int64_t block) {
+  return (int)(s.apart ? block >> s.shift : ((block + 1) * s.workers - 1) / s.all);
+}
 // blocks [from, to) of an entry that starts at `start` and has `blocks` fall to the worker of [lo, hi)
 struct PagedShare { int from, to; };
-PAGED_HD PagedShare paged_share(int64_t start, int blocks, int64_t lo, int64_t hi, int least) {
-  if (blocks <= least) return start >= lo && start < hi ? PagedShare{0, blocks} : PagedShare{0, 0};
+PAGED_HD PagedShare paged_share(const PagedSplit& s, int64_t start, int blocks, int64_t lo, int64_t hi) {
+  if (blocks <= 1 << s.shift) return start >= lo && start < hi ? PagedShare{0, blocks} : PagedShare{0, 0};
   const int64_t a = start < lo ? lo : start, b = start + blocks < hi ? start + blocks : hi;
   return a < b ? PagedShare{(int)(a - start), (int)(b - start)} : PagedShare{0, 0};
 }

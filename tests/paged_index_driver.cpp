@@ -1,6 +1,6 @@
 // Host build of the paged cache's index code, under sanitizers.  Reads lines of whole numbers, prints what the code says:
 //   rows n nt window sinks   -> number of blocks, then for every row 0 .. n + 40: counted blocks that hold it * 4 + seen * 2 + (its block of 32 is all seen)
-//   workers target least blocks.. -> their number, (worker, entry, from, to) of every share, (first, last) worker of every entry
+//   workers target longest blocks.. -> their number, the run where each entry is cut for itself (else 0), (worker, entry, from, to) of every share, (first, last) worker of every entry
 //   page n_pages shift row seen entry.. -> the page
 //   slot s n_slots len slot_pages shift -> slot, clamped length, its pages
 #include <cstdio>
@@ -32,22 +32,30 @@ int main() {
       std::printf("\n");
     } else if (what == "workers") {
       std::vector<long long> start;
-      long long all = 0, runs = 0;
-      for (size_t i = 2; i < x.size(); ++i) runs += paged_runs((int)x[i], (int)x[1]);
-      const bool apart = paged_apart(runs, (int)x[0]);
+      long long all = 0;
+      const int target = (int)x[0], longest = (int)x[1];
+      auto runs_of = [&](int shift) {
+        long long runs = 0;
+        for (size_t i = 2; i < x.size(); ++i) runs += paged_runs((int)x[i], shift);
+        return runs;
+      };
+      for (size_t i = 2; i < x.size(); ++i) all += x[i];
+      int shift = PAGED_RUN;
+      while (!paged_apart(all, runs_of(shift), shift, target) && shift < longest) ++shift;
+      const PagedSplit split = paged_split(all, runs_of(shift), shift, paged_apart(all, runs_of(shift), shift, target), target);
+      all = 0;
       for (size_t i = 2; i < x.size(); ++i) {
         start.push_back(all);
-        all += paged_counted(apart, (int)x[i], paged_runs((int)x[i], (int)x[1]), (int)x[1]);
+        all += paged_counted(split, (int)x[i]);
       }
-      const int n = paged_workers(all, (int)x[0], (int)x[1]);
-      std::printf("%d", n);
-      for (int w = 0; w < n; ++w)
+      std::printf("%d %d", split.workers, split.apart ? 1 << split.shift : 0);
+      for (int w = 0; w < split.workers; ++w)
         for (size_t i = 2; i < x.size(); ++i) {
-          const PagedShare s = paged_share(start[i - 2], (int)x[i], paged_cut(all, n, w), paged_cut(all, n, w + 1), (int)x[1]);
+          const PagedShare s = paged_share(split, start[i - 2], (int)x[i], paged_cut(split, w), paged_cut(split, w + 1));
           if (s.from < s.to) std::printf(" %d %d %d %d", w, (int)i - 2, s.from, s.to);
         }
       for (size_t i = 2; i < x.size(); ++i)
-        std::printf(" %d %d", paged_worker_of(all, n, start[i - 2]), paged_worker_of(all, n, start[i - 2] + x[i] - 1));
+        std::printf(" %d %d", paged_worker_of(split, start[i - 2]), paged_worker_of(split, start[i - 2] + x[i] - 1));
       std::printf("\n");
     } else if (what == "page") {
       std::vector<int32_t> table(x.begin() + 4, x.end());

@@ -52,14 +52,16 @@ def test_rows_that_a_window_shows_and_the_blocks_that_hold_them(driver):
 
 def test_workers_share_all_blocks_evenly(driver):
     rng = random.Random(6)
-    cases = [(rng.choice((1, 4, 25, 64, 512)), rng.choice((1, 4, 8)), [max(1, int(2 ** rng.uniform(0, 9)) * rng.choice((0, 1, 1)))
+    cases = [(rng.choice((1, 4, 25, 64, 512)), rng.choice((2, 3)), [max(1, int(2 ** rng.uniform(0, 9)) * rng.choice((0, 1, 1)))
                                                                   for _ in range(rng.choice((1, 2, 7, 64, 65, 150)))]) for _ in range(200)]
-    cases.append((512, 4, [2 ** 23] * 300))
-    for (target, least, blocks), got in zip(cases, driver(["workers %d %d %s" % (t, k, " ".join(map(str, n))) for t, k, n in cases])):
-        n, ends = got[0], got[len(got) - 2 * len(blocks):]
-        shares = [got[i: i + 4] for i in range(1, len(got) - len(ends), 4)]
-        runs = sum(-(-size // least) for size in blocks)
-        assert 1 <= n <= target and n == (runs if runs <= target else min(target, -(-sum(blocks) // least)))
+    cases.append((512, 3, [2 ** 23] * 300))
+    for (target, longest, blocks), got in zip(cases, driver(["workers %d %d %s" % (t, k, " ".join(map(str, n))) for t, k, n in cases])):
+        n, run, ends = got[0], got[1], got[len(got) - 2 * len(blocks):]
+        shares = [got[i: i + 4] for i in range(2, len(got) - len(ends), 4)]
+        fits = [r for r in (4, 8) if r <= 1 << longest and sum(-(-size // r) for size in blocks) <= target
+                and (r == 4 or (r - 5) * target <= sum(blocks))]
+        assert run == (fits[0] if fits else 0)
+        assert 1 <= n <= target and n == (sum(-(-size // run) for size in blocks) if run else min(target, -(-sum(blocks) // 4)))
         parts = {}
         for w, e, a, b in shares:
             parts.setdefault(e, []).append((w, a, b))
@@ -71,12 +73,12 @@ def test_workers_share_all_blocks_evenly(driver):
                 assert a == at
                 at, work[w] = b, work[w] + b - a
             assert at == size
-            if size <= least:
+            if size <= (run or 4):
                 assert len(parts[e]) == 1 and parts[e][0][0] == ends[2 * e]
             else:
                 assert [p[0] for p in parts[e]] == list(range(ends[2 * e], ends[2 * e + 1] + 1))
-        assert max(work) <= (least if runs <= target else even + 1 + least)
-        if runs <= target:                              # a worker for every run: nobody has two entries
+        assert max(work) <= (run or even + 1 + 4)
+        if run:                              # a worker for every run: nobody has two entries
             assert sorted(v for v, e, a, b in shares) == list(range(n))
         for w in range(n):                              # at most one entry gone on with and one begun in part: two places for sums
             part = [(a, b, e) for v, e, a, b in shares if v == w and b - a < blocks[e]]
