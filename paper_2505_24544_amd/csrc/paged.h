@@ -62,4 +62,15 @@ void launch_paged_compact(const PagedCache& from, const PagedCache& into, int64_
 __device__ __forceinline__ int paged_slot(const PagedCache& c, const int32_t* slots, int b) { return paged_slot_of(slots ? slots[b] : b, c.N); }
 __device__ __forceinline__ int paged_len(const PagedCache& c, int slot) { return slot < 0 ? 0 : paged_clamped(c.lens[slot], c.W, c.shift); }
 
+// Inclusive sum over the lanes: within rows of 16, then what the rows before have.  All 64 lanes have to be active.
+__device__ __forceinline__ int sum_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);        // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 }  // namespace beagle

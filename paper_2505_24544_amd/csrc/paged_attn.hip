@@ -45,16 +45,6 @@ __device__ __align__(16) const unsigned char zero_row[1024] = {};
 typedef uint64_t addr_t;
 __device__ __forceinline__ u32x4 load16(addr_t p) { return *(const __attribute__((address_space(1))) u32x4*)p; }
 
-// Inclusive sum over the lanes: within rows of 16, then what the rows before have.
-__device__ __forceinline__ int sum_upto(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);        // row_shr 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // row_bcast 15, 31
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-  return v;
-}
 // Every wave walks the entries by itself, 64 at a time: a lane's entry, its rows, and the blocks that it and the lanes before it have.
 struct Entry { int slot, blocks, upto; PagedRows rows; };
 __device__ __forceinline__ Entry entry_of(const PagedAttnArgs& a, int b) {

@@ -23,27 +23,30 @@ __device__ __forceinline__ void settle() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 }
 
-// Inclusive sum over the workgroup's threads in order; `all` gets the sum of everything.
-__device__ __forceinline__ int block_scan(int v, int* wave_sums, int& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Inclusive sum over the workgroup's threads in order, of K numbers at once; `all` gets the sums of everything.
+template <int K> struct Sums { int at[K]; };
+template <int K> __device__ __forceinline__ Sums<K> block_scan(Sums<K> v, int (*wave_sums)[PLAN_WAVES], Sums<K>& all) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int x = __shfl_up(v, m);
-    if (lane >= m) v += x;
-  }
+  for (int k = 0; k < K; ++k) v.at[k] = sum_upto(v.at[k]);
   __syncthreads();                         // (the sums of the call before have been read)
-  if (lane == 63) wave_sums[wave] = v;
-  __syncthreads();
-  // (a lane for each wave's sum)
-  const int x = lane < PLAN_WAVES ? wave_sums[lane] : 0;
-  int upto = x;
+  if (lane == 63)
 #pragma unroll
-  for (int m = 1; m < PLAN_WAVES; m <<= 1) {
-    const int y = __shfl_up(upto, m);
-    if (lane >= m) upto += y;
+    for (int k = 0; k < K; ++k) wave_sums[k][wave] = v.at[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) {            // (a lane for each wave's sum)
+    const int x = lane < PLAN_WAVES ? wave_sums[k][lane] : 0, upto = sum_upto(x);
+    all.at[k] = __builtin_amdgcn_readlane(upto, PLAN_WAVES - 1);
+    v.at[k] += __builtin_amdgcn_readlane(upto - x, wave);
   }
-  all = __builtin_amdgcn_readlane(upto, PLAN_WAVES - 1);
-  return v + __shfl(upto - x, wave);
+  return v;
+}
+__device__ __forceinline__ int block_scan(int v, int (*wave_sums)[PLAN_WAVES], int& all) {
+  Sums<1> sum;
+  v = block_scan(Sums<1>{{v}}, wave_sums, sum).at[0];
+  all = sum.at[0];
+  return v;
 }
 
 // ------------------------------------------------------------------ append
@@ -52,21 +55,32 @@ __device__ __forceinline__ int block_scan(int v, int* wave_sums, int& all) {
 struct Entry { int32_t slot, pos, n, from; };
 struct AppendWs { Entry* entry; int32_t *upto, *taken; };       // [B], [B] pages wanted by the entries up to this one, [P]
 
-// pages that an entry keeps, and holds when all its rows are there
+// What the arrays say of an entry, and what the call makes of it: pages that it keeps, and holds when all its rows are there.
+struct Asked { int slot, len, pos, n; };
+__device__ __forceinline__ Asked asked_of(const PagedAppendArgs& a, int b) {
+  Asked x;
+  x.slot = paged_slot(a.c, a.slots, b);
+  x.pos = a.pos ? a.pos[b] : INT32_MAX;
+  x.n = a.n_new ? a.n_new[b] : a.M;
+  x.len = a.c.lens[max(x.slot, 0)];
+  return x;
+}
 struct Want { int slot, len, pos, n, keep, pages; bool room; };
-__device__ __forceinline__ Want want_of(const PagedAppendArgs& a, const int* owner, int b) {
+__device__ __forceinline__ Want want_of(const PagedAppendArgs& a, const Asked& x) {
   Want w;
-  w.slot = paged_slot(a.c, a.slots, b);
-  const int pos = a.pos ? a.pos[b] : INT32_MAX, n = a.n_new ? a.n_new[b] : a.M;
-  const int len = a.c.lens[max(w.slot, 0)];                     // (one trip for all three)
-  if (w.slot >= 0 && owner[w.slot] != b) w.slot = -1;           // the slot's first entry counts
-  w.len = w.slot < 0 ? 0 : paged_clamped(len, a.c.W, a.c.shift);
-  w.pos = min(max(pos, 0), w.len);
-  w.n = w.slot < 0 ? 0 : min(max(n, 0), a.M);
+  w.slot = x.slot;
+  w.len = w.slot < 0 ? 0 : paged_clamped(x.len, a.c.W, a.c.shift);
+  w.pos = min(max(x.pos, 0), w.len);
+  w.n = w.slot < 0 ? 0 : min(max(x.n, 0), a.M);
   w.room = (int64_t)w.pos + w.n <= (int64_t)a.c.W << a.c.shift;
   w.keep = paged_pages(w.pos, a.c.shift);
   w.pages = w.room ? paged_pages(w.pos + w.n, a.c.shift) : w.keep;
   return w;
+}
+// the page that an entry's first row joins, -1 if it begins one, -2 if the table names none (the rows go into a fresh one)
+__device__ __forceinline__ bool joins_page(const PagedAppendArgs& a, const Want& w) { return w.n > 0 && w.room && (w.pos & ((1 << a.c.shift) - 1)); }
+__device__ __forceinline__ int page_before(const PagedAppendArgs& a, const Want& w) {        // (read whether it joins or not)
+  return a.c.table[(int64_t)max(w.slot, 0) * a.c.W + max(w.keep - 1, 0)];
 }
 
 // f(x, y, i) for every i in [lo, hi), with the lane's x and y: by the lane where they are few, by the wave together where they are many
@@ -90,39 +104,48 @@ constexpr int NEAR = 4096;                 // taken pages that LDS holds
 __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs a, AppendWs ws) {
   __shared__ int owner[PAGED_MAX_BATCH];
   __shared__ int taken[NEAR];
-  __shared__ int wave_sums[PLAN_WAVES];
+  __shared__ int wave_sums[2][PLAN_WAVES];
   __shared__ int lacking;
   const int tid = threadIdx.x, in_page = (1 << a.c.shift) - 1;
+  const bool one = a.B <= PLAN;            // every thread has at most one entry, and keeps it
   for (int s = tid; s < a.c.N; s += PLAN) owner[s] = INT32_MAX;
   if (tid == 0) lacking = 0;
+  Asked asked{-1, 0, 0, 0};
+  if (one && tid < a.B) asked = asked_of(a, tid);
   __syncthreads();
-  for (int b = tid; b < a.B; b += PLAN) {
-    const int s = paged_slot(a.c, a.slots, b);
+  for (int b = tid; b < a.B; b += PLAN) {  // the slot's first entry counts
+    const int s = one ? asked.slot : paged_slot(a.c, a.slots, b);
     if (s >= 0) atomicMin(&owner[s], b);
   }
+  Want w = want_of(a, asked);
+  int before = one ? page_before(a, w) : -1;                    // (on the way meanwhile)
   __syncthreads();
+  auto entry_at = [&](int b) {
+    asked = Asked{-1, 0, 0, 0};
+    if (b < a.B) asked = asked_of(a, b);
+    if (asked.slot >= 0 && owner[asked.slot] != b) asked.slot = -1;
+    w = want_of(a, asked);
+  };
   // pages behind the kept rows are given up; of the page that is kept in part, whether there is one
-  Want w{};
   int part = -1;
   for (int b0 = 0; b0 < a.B; b0 += PLAN) {
     const int b = b0 + tid;
-    w = Want{};
-    w.slot = -1;
-    part = -1;
-    if (b < a.B) w = want_of(a, owner, b);
-    const int32_t* row = a.c.table + (int64_t)max(w.slot, 0) * a.c.W;
-    if (w.n > 0 && w.room && (w.pos & in_page)) {
-      const int p = row[w.keep - 1];
-      part = is_page(a.c, p) ? p : -2;                          // (a page that is none: the rows go into a fresh one)
+    if (!one) {
+      entry_at(b);
+      before = page_before(a, w);
+    } else if (w.slot >= 0 && owner[w.slot] != b) {
+      asked.slot = -1;
+      w = want_of(a, asked);
     }
+    part = joins_page(a, w) ? is_page(a.c, before) ? before : -2 : -1;
     each_page(w.keep, paged_pages(w.len, a.c.shift), w.slot, 0, [&](int slot, int, int i) {
       const int p = a.c.table[(int64_t)slot * a.c.W + i];
       if (is_page(a.c, p)) add_count(a.c.refs + p, -1);
     });
-    if (a.B > PLAN && b < a.B) ws.entry[b] = Entry{w.slot, part, 0, 0};         // (looked at again below)
+    if (!one && b < a.B) ws.entry[b] = Entry{w.slot, part, 0, 0};         // (looked at again below)
   }
   settle();
-  // pages wanted; a page that is kept in part and shared is copied into one of its own.  The first counts are looked at on the way.
+  // Pages wanted; a page that is kept in part and shared is copied into one of its own.  The first counts are looked at on the way.
   const bool vec = (((uintptr_t)a.c.refs) & 15) == 0;
   int held[LOOK];
   auto look = [&](int64_t p0) {
@@ -138,36 +161,42 @@ __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs
       for (int i = 0; i < LOOK; ++i) held[i] = p + i < a.c.P ? a.c.refs[p + i] : 1;
     }
   };
+  auto count_free = [&]() {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < LOOK; ++i) n += held[i] <= 0;
+    return n;
+  };
   look(0);
-  int wanted = 0;
+  int wanted = 0, upto = 0, free0 = 0, all0 = 0;         // free pages among the first counts: of the threads up to this one, of all
+  Sums<2> sums{};
   Entry e{-1, 0, 0, -1};
-  int upto = 0;
   for (int b0 = 0; b0 < a.B; b0 += PLAN) {
     const int b = b0 + tid;
-    if (a.B > PLAN) {
-      w = Want{};
-      w.slot = -1;
-      part = -1;
-      if (b < a.B) { w = want_of(a, owner, b); part = ws.entry[b].pos; }
+    if (!one) {
+      entry_at(b);
+      part = b < a.B ? ws.entry[b].pos : -1;
     }
     int from = -1;
     if (part != -1) from = part == -2 ? -2 : a.c.refs[part] > 1 ? part : -1;
     const int need = w.pages - w.keep + (from != -1);
     if (b < a.B && !w.room) atomicAdd(&lacking, (int)(((int64_t)w.pos + w.n - ((int64_t)a.c.W << a.c.shift) + in_page) >> a.c.shift));
     e = Entry{w.slot, w.pos, w.room ? w.n : 0, from};
-    int all;
-    upto = wanted + block_scan(need, wave_sums, all);
-    wanted += all;
+    const Sums<2> v = block_scan(Sums<2>{{need, b0 ? 0 : count_free()}}, wave_sums, sums);
+    if (!b0) { free0 = v.at[1]; all0 = sums.at[1]; }
+    upto = wanted + v.at[0];
+    wanted += sums.at[0];
     if (b < a.B) { ws.entry[b] = e; ws.upto[b] = upto; }
   }
   // the lowest free pages
   int found = 0;
   for (int64_t p0 = 0; p0 < a.c.P && found < wanted; p0 += LOOK * PLAN) {
-    if (p0) look(p0);
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < LOOK; ++i) n += held[i] <= 0;
-    int all, at = block_scan(n, wave_sums, all) - n + found;
+    int all = all0, at = free0;
+    if (p0) {
+      look(p0);
+      at = block_scan(count_free(), wave_sums, all);
+    }
+    at += found - count_free();
 #pragma unroll
     for (int i = 0; i < LOOK; ++i)
       if (held[i] <= 0) {
@@ -176,11 +205,11 @@ __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs
       }
     found += all;
   }
-  if (wanted > NEAR || a.B > PLAN) settle(); else __syncthreads();
+  if (wanted > NEAR || !one) settle(); else __syncthreads();
   if (tid == 0 && a.short_pages) a.short_pages[0] = max(wanted - found, 0) + lacking;
   for (int b0 = 0; b0 < a.B; b0 += PLAN) {
     const int b = b0 + tid;
-    if (a.B > PLAN) {
+    if (!one) {
       e = Entry{-1, 0, 0, -1};
       if (b < a.B) { e = ws.entry[b]; upto = ws.upto[b]; }
     }
@@ -359,7 +388,7 @@ struct CompactWs { int32_t *number, *live, *count; };   // [P] new number of a l
 
 // Workgroup 0 numbers the live pages; the others clear the target's counts.
 __global__ __launch_bounds__(PLAN) void paged_number_kernel(PagedCache from, PagedCache into, int32_t* short_pages, CompactWs ws) {
-  __shared__ int wave_sums[PLAN_WAVES];
+  __shared__ int wave_sums[1][PLAN_WAVES];
   const int tid = threadIdx.x;
   if (blockIdx.x) {
     for (int64_t p = (int64_t)(blockIdx.x - 1) * PLAN + tid; p < into.P; p += (int64_t)(gridDim.x - 1) * PLAN) into.refs[p] = 0;
@@ -428,7 +457,7 @@ constexpr int COMPACT_NEAR = 4096, COMPACT_NEAR_ENTRIES = 16384;
 constexpr int64_t COMPACT_NEAR_BYTES = 32 << 20;          // of K; a large pool is copied better by small workgroups
 __global__ __launch_bounds__(PLAN) void paged_compact_kernel(PagedCache from, PagedCache into, int64_t page_bytes, int32_t* short_pages) {
   __shared__ int number[COMPACT_NEAR], live[COMPACT_NEAR];
-  __shared__ int wave_sums[PLAN_WAVES];
+  __shared__ int wave_sums[1][PLAN_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   constexpr int EACH = COMPACT_NEAR / PLAN;
   int n = 0, held[EACH];
