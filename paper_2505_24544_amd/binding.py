@@ -482,9 +482,13 @@ class _Paged:
     def call(self, name, cache, args, workspace, workspace_bytes, stream, check):
         """By default on the current stream of the cache's device, which is made the current one meanwhile."""
         if workspace is not None and not isinstance(workspace, int):
+            if workspace.device != self.dev and (self.dev is not None or not workspace.is_cuda):
+                raise ValueError("the workspace is on %s, the cache is on %s" % (workspace.device, self.dev or "a GPU"))
+            if not workspace.is_contiguous():
+                raise ValueError("tensor arguments must be contiguous")
             if workspace_bytes is None:
-                workspace_bytes = workspace.numel() * workspace.element_size()
-            workspace = self._at(workspace, workspace.numel(), (workspace.dtype,))
+                workspace_bytes = workspace.nbytes
+            workspace = workspace.data_ptr()
         fn = getattr(_lib or lib(), name)
         if self.dev is not None and self.dev.type != "cuda":
             raise ValueError("the cache is on %s, not on a GPU" % self.dev)

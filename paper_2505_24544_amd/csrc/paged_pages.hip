@@ -100,7 +100,8 @@ constexpr int LOOK = 16;                   // counts that a thread looks at in o
 constexpr int NEAR = 4096;                 // taken pages that LDS holds
 
 // One workgroup, bound by its trips to memory one behind the other: releases, the pages that every entry wants, the lowest free
-// ones, handed out in order.
+// ones, handed out in order.  64 entries of 5 rows over some 15000 pages: 7.5 us, a launch's 2 and four trips (slots; lengths; table;
+// counts), which nothing here depends on less.
 __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs a, AppendWs ws) {
   __shared__ int owner[PAGED_MAX_BATCH];
   __shared__ int taken[NEAR];
@@ -451,7 +452,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache from, PagedC
 }
 
 // The same in one launch for a small pool: every workgroup numbers the live pages for itself, the first one has the tables
-// and counts to itself, the others copy.  8 MB in 6.1 us instead of 6.7, a pass in 9.7 instead of 13.0 (the host's
+// and counts to itself, the others copy.  8 MB in 6.1 us instead of 6.7 (both measured together; now 5.6), a pass in 9.7 instead of 13.0 (the host's
 // launches are the longer).
 constexpr int COMPACT_NEAR = 4096, COMPACT_NEAR_ENTRIES = 16384;
 constexpr int64_t COMPACT_NEAR_BYTES = 32 << 20;          // of K; a large pool is copied better by small workgroups
