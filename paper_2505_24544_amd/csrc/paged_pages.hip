@@ -100,8 +100,8 @@ constexpr int LOOK = 16;                   // counts that a thread looks at in o
 constexpr int NEAR = 4096;                 // taken pages that LDS holds
 
 // One workgroup, bound by its trips to memory one behind the other: releases, the pages that every entry wants, the lowest free
-// ones, handed out in order.  64 entries of 5 rows over some 15000 pages: 7.5 us, a launch's 2 and four trips (slots; lengths; table;
-// counts), which nothing here depends on less.
+// ones, handed out in order.  64 entries of 5 rows over some 15000 pages: 7.5 us, a launch's 2 and four trips (slots, lengths,
+// table, counts).
 __global__ __launch_bounds__(PLAN) void paged_append_plan_kernel(PagedAppendArgs a, AppendWs ws) {
   __shared__ int owner[PAGED_MAX_BATCH];
   __shared__ int taken[NEAR];

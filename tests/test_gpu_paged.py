@@ -229,6 +229,21 @@ def test_split_sequences_are_reproducible_and_do_not_depend_on_the_batch():
     assert torch.equal(o1.view(torch.int16), o2.view(torch.int16)) and torch.equal(l1.view(torch.int32), l2.view(torch.int32))
 
 
+@pytest.mark.parametrize("lens,W", [([900, 700, 500, 300], 100), ([900, 700, 500, 300], 57), ([2000, 1800, 100, 5], 130), ([400, 0, 333, 1], 100)])
+def test_how_entries_are_cut(lens, W):
+    """16 workers a head: runs of eight blocks each, whole entries, equal runs of all, runs of four."""
+    rng = np.random.default_rng(sum(lens) + W)
+    c = make(rng, lens, 16, W, sum(-(-n // 16) for n in lens) + 1, 32, 128, "bf16")
+    check_attend(c, queries(rng, 4, 1, 32, 128, "bf16"), "bf16", rows=2000)
+
+
+def test_more_entries_than_workers_and_than_a_wave_has_lanes():
+    rng = np.random.default_rng(44)
+    lens = [int(n) for n in rng.integers(0, 300, 70)]
+    c = make(rng, lens, 16, 200, 1400, 8, 4, "f32")
+    check_attend(c, queries(rng, 70, 2, 16, 4, "f32"), "f32")
+
+
 def test_many_entries():
     """More entries than a wave looks at once."""
     rng = np.random.default_rng(43)
