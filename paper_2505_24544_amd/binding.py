@@ -146,7 +146,11 @@ def make_paged_cache(k_pages, v_pages, page_table, lens, refs) -> beagle_paged_c
     c = beagle_paged_cache(C.sizeof(beagle_paged_cache), k_pages.shape[0], k_pages.shape[1], page_table.shape[0],
                            page_table.shape[1], 0, *(_ptr(t) for t in (k_pages, v_pages, page_table, lens, refs)))
     # what a call's tensors are checked against: rows [G, d] of this type on this device
-    c.rows, c.dtype, c.device = tuple(k_pages.shape[2:]), k_pages.dtype, k_pages.device
+    c.rows, c.dtype, c.device, c.index = tuple(k_pages.shape[2:]), k_pages.dtype, k_pages.device, k_pages.get_device()
+    c.alone = False                                       # the only device is the current one
+    if k_pages.is_cuda:
+        import torch
+        c.alone = torch.cuda.device_count() == 1
     return c
 
 
@@ -429,51 +433,60 @@ def beagle_xattn_kv_append(desc, x_new, wk, wv, k_cache, v_cache, pos, workspace
     return _check(st, "beagle_xattn_kv_append", check)
 
 
-_torch = None
+_torch = _WHOLE = _FLOAT = _BF16 = None
 
 
 class _Paged:
-    """The tensors of one paged call, checked against its descriptor and its cache; addresses and None pass as they are."""
-    __slots__ = ("desc", "dev", "dtype", "whole", "n")
+    """The tensors of one paged call, checked against its descriptor and its cache; addresses and None pass as they are.  (A call of
+    few rows takes the device about as long as the host: a tensor that is as it should be goes through one test.)"""
+    __slots__ = ("desc", "dev", "index", "dtypes", "n")
 
     def __init__(self, desc, cache):
-        global _torch
+        global _torch, _WHOLE, _FLOAT, _BF16
         if _torch is None:
             import torch
+            _WHOLE, _FLOAT, _BF16 = (torch.int32, torch.uint32), (torch.float32,), (torch.bfloat16,)
             _torch = torch
         self.desc = desc
-        self.dev = getattr(cache, "device", None)         # (None: a cache made of addresses)
         self.n = desc.batch * desc.seq_q
-        self.whole = (_torch.int32, _torch.uint32)
-        self.dtype = _torch.bfloat16 if desc.io_dtype == BEAGLE_BF16 else _torch.float32
-        if self.dev is not None and (cache.dtype != self.dtype or cache.rows != (desc.n_kv_heads, desc.head_dim)):
-            raise ValueError("the cache holds rows %s of %s, not what the descriptor says" % (cache.rows, cache.dtype))
+        self.dtypes = _BF16 if desc.io_dtype == BEAGLE_BF16 else _FLOAT
+        self.dev = dev = getattr(cache, "device", None)         # (None: a cache made of addresses)
+        self.index = None
+        if dev is not None:
+            self.index = cache.index
+            if cache.dtype not in self.dtypes or cache.rows != (desc.n_kv_heads, desc.head_dim):
+                raise ValueError("the cache holds rows %s of %s, not what the descriptor says" % (cache.rows, cache.dtype))
 
     def _at(self, t, count, dtypes):
         if t is None or isinstance(t, int):
             return t
+        if t.dtype in dtypes and t.numel() == count and t.get_device() == self.index and t.is_contiguous():
+            return t.data_ptr()
         if t.dtype not in dtypes:
             raise ValueError("a tensor of %s is needed, not of %s" % (" or ".join(map(str, dtypes)), t.dtype))
-        if t.device != self.dev and (self.dev is not None or not t.is_cuda):
-            raise ValueError("a tensor argument is on %s, the cache is on %s" % (t.device, self.dev or "a GPU"))
+        self._on_device(t)
         if t.numel() != count:
             raise ValueError("a tensor of shape %s does not hold the %d values of the call" % (tuple(t.shape), count))
         if not t.is_contiguous():
             raise ValueError("tensor arguments must be contiguous")
         return t.data_ptr()
 
+    def _on_device(self, t):
+        if t.device != self.dev and (self.dev is not None or not t.is_cuda):
+            raise ValueError("a tensor argument is on %s, the cache is on %s" % (t.device, self.dev or "a GPU"))
+
     def ints(self, t, count):
-        return self._at(t, count, self.whole)
+        return self._at(t, count, _WHOLE)
 
     def rows(self, t, width):
         """[batch, seq_q, width] of the cache's type"""
-        return self._at(t, self.n * width, (self.dtype,))
+        return self._at(t, self.n * width, self.dtypes)
 
     def weight(self, t, count):
-        return self._at(t, count, (self.dtype,))
+        return self._at(t, count, self.dtypes)
 
     def lse(self, t):
-        return self._at(t, self.n * self.desc.n_q_heads, (_torch.float32,))
+        return self._at(t, self.n * self.desc.n_q_heads, _FLOAT)
 
     def view(self, slots, n_true, tree_mask, mask_words, window, sinks):
         B = self.desc.batch
@@ -482,8 +495,8 @@ class _Paged:
     def call(self, name, cache, args, workspace, workspace_bytes, stream, check):
         """By default on the current stream of the cache's device, which is made the current one meanwhile."""
         if workspace is not None and not isinstance(workspace, int):
-            if workspace.device != self.dev and (self.dev is not None or not workspace.is_cuda):
-                raise ValueError("the workspace is on %s, the cache is on %s" % (workspace.device, self.dev or "a GPU"))
+            if workspace.get_device() != self.index:
+                self._on_device(workspace)
             if not workspace.is_contiguous():
                 raise ValueError("tensor arguments must be contiguous")
             if workspace_bytes is None:
@@ -492,7 +505,7 @@ class _Paged:
         fn = getattr(_lib or lib(), name)
         if self.dev is not None and self.dev.type != "cuda":
             raise ValueError("the cache is on %s, not on a GPU" % self.dev)
-        if self.dev is not None and self.dev.index != _torch.cuda.current_device():
+        if self.dev is not None and not cache.alone and self.index != _torch.cuda.current_device():
             with _torch.cuda.device(self.dev):
                 return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
         return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
@@ -526,7 +539,7 @@ def beagle_xattn_paged_fork(desc, cache, dst, src, rows, workspace, stream=None,
 
 def beagle_xattn_paged_compact(desc, cache, into, short_pages, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
     c = _Paged(desc, cache)
-    if c.dev is not None and getattr(into, "device", None) is not None and (c.dev != into.device or cache.rows != into.rows or c.dtype != into.dtype):
+    if c.dev is not None and getattr(into, "device", None) is not None and (c.dev != into.device or cache.rows != into.rows or cache.dtype != into.dtype):
         raise ValueError("the two pools hold different rows, or are on different devices")
     args = (into, c.ints(short_pages, 1))
     return c.call("beagle_xattn_paged_compact", cache, args, workspace, workspace_bytes, stream, check)
