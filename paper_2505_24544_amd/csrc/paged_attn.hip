@@ -253,7 +253,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
   };
   // bit 4 t + i: row 16 t + 4 g4 + i is seen; bit 16 + t: row 16 t + l16
   struct Step { int base; uint32_t seen; bool masked; };
-  auto judge = [&](const Pages& h, int s) BEAGLE_INLINE_LAMBDA {
+  auto seen_of = [&](const Pages& h, int s) BEAGLE_INLINE_LAMBDA {
     Step st;
     st.base = base_of(s);
     st.seen = ~0u;
@@ -316,7 +316,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
   if (TREE && plain < steps) tail = look(plain);
   if (plain > 0) {
     Pages next = look(0);
-    Step st = judge(next, 0);
+    Step st = seen_of(next, 0);
     request_k(next, st);
     request_v(v, next, st);
     next = look(1);
@@ -325,7 +325,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
       Step ahead = st;
       const Pages now = next;
       if (s + 1 < plain) {
-        ahead = judge(now, s + 1);
+        ahead = seen_of(now, s + 1);
         request_k(now, ahead);
         request_v(others, now, ahead);
         next = look(s + 2);
@@ -344,7 +344,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
   if constexpr (TREE)
     for (int s = plain; s < steps; ++s) {
       if (s > plain) tail = look(s);
-      const Step st = judge(tail, s);
+      const Step st = seen_of(tail, s);
       request_k(tail, st);
       request_v(v, tail, st);
       scores();
