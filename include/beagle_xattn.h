@@ -644,7 +644,9 @@ beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const bea
  * [0, M]) rows at pos[b] .. pos[b] + n - 1: resetting a sequence to its true rows
  * and appending the next ones is one call, n = 0 alone drops rows.  A page that
  * the slot keeps a part of and shares with others is copied first, so other
- * slots never see the change.  With BEAGLE_FLAG_ROPE the K rows are rotated, at
+ * slots never see the change.  (Where the table names no page for the kept part, the
+ * new rows go into a fresh one, whose rows before them hold what they held.)
+ * With BEAGLE_FLAG_ROPE the K rows are rotated, at
  * desc->rope_positions[b * M + i] or, if that is NULL, at their row numbers.
  * Pages are taken lowest number first, in the order of the entries; pages
  * given up in the call can be taken in it.  If the pool runs out, the first entry
