@@ -1,0 +1,41 @@
+"""What the paged attention computes with: probabilities and scale of 24 bits, infinities in rows that are seen.
+
+Every tolerance counts the roundings of the case at hand, in units u = 2^-24 of a float; bf16 results round by 2^-8 of themselves."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+from test_gpu_paged import attend, host, make, pytestmark, queries, stored  # noqa: F401
+
+U = 2.0 ** -24
+
+
+@pytest.mark.parametrize("M", [1, 64])                   # an entry for each query (one tile), or all in one entry (two tiles)
+@pytest.mark.parametrize("W", [1, 40])                   # a workgroup an entry, or equal runs
+def test_probabilities_have_all_their_bits(M, W):
+    """Two rows of scores 0 and -t, t another for every query.  Channel m holds a and -b with a / b next to exp(-t) of query m, so the terms
+    of o = (a - b exp(-t)) / (1 + exp(-t)) all but cancel and the probability's error is what remains.
+
+    The probability is off by 4 u of itself: two roundings of the scaled score (below 1.45, in log2 units: 2 u) and the hardware's exp2
+    (one unit in the last place, 2 u).  Products of bf16 numbers are exact in float; a sum of four terms, cut off at worst, is off by 4 * 2 u
+    of the sum of magnitudes.  Half of that sum is the probability's: 8 u + 4 u / 2 = 10 u in all."""
+    t = stored(np.linspace(0.26, 0.99, 64), "bf16")
+    assert len(set(t)) == 64
+    p = np.exp(-t)
+    b = np.arange(128, 256)
+    off = np.abs(np.rint(p[:, None] * b) - p[:, None] * b)
+    b = b[off.argmin(1)]
+    a = np.rint(p * b)
+    assert (np.abs(a - p * b) <= 2.0 ** -5).all()
+    c = dict(k=np.zeros((3, 16, 1, 128)), v=np.zeros((3, 16, 1, 128)), table=[[1] + [-1] * (W - 1)], lens=[2], refs=[0, 1, 0])
+    c["k"][1, 1, 0, 0] = -1.0
+    c["v"][1, 0, 0, :64], c["v"][1, 1, 0, :64] = a, -b
+    q = np.zeros((64 // M, M, 1, 128))
+    q[..., 0, 0] = t.reshape(64 // M, M)
+    o, lse = attend(c, q, "bf16", slots=[0] * (64 // M), scale=1.0)
+    got = host(o).reshape(64, 128)[np.arange(64), np.arange(64)]
+    ref, spread = (a - p * b) / (1 + p), (a + p * b) / (1 + p)
+    far = np.abs(got - ref) - 2.0 ** -8 * np.abs(ref)
+    assert (far <= 10 * U * spread).all(), (far / spread / U).max()
+    assert np.abs(host(lse).reshape(64) - np.log1p(p)).max() <= 16 * U
