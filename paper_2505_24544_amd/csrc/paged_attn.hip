@@ -142,7 +142,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
 #pragma unroll
     for (int c = 0; c < S::NA; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // scale * log2(e): float storage takes it as two numbers, since its rounding moves every score alike (2^-24 of scores of 20 is 1e-6)
+  // scale * log2(e) as two numbers: its rounding would move every score alike, and lse with them
   const float c2 = a.c2, c2_low = a.c2_low;
 
   // ---- the steps of this wave: KROWS rows each, of every WAVES-th block
@@ -175,10 +175,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
       }
     }
   };
-  auto scaled = [&](float x, float less) BEAGLE_INLINE_LAMBDA {
-    if constexpr (BF16) return fmaf(x, c2, -less);
-    else return fmaf(x, c2_low, fmaf(x, c2, -less));
-  };
+  auto scaled = [&](float x, float less) BEAGLE_INLINE_LAMBDA { return fmaf(x, c2_low, fmaf(x, c2, -less)); };
   // running maximum and sum, probabilities
   auto probabilities = [&]() BEAGLE_INLINE_LAMBDA {
 #pragma unroll

@@ -39,3 +39,24 @@ def test_probabilities_have_all_their_bits(M, W):
     far = np.abs(got - ref) - 2.0 ** -8 * np.abs(ref)
     assert (far <= 10 * U * spread).all(), (far / spread / U).max()
     assert np.abs(host(lse).reshape(64) - np.log1p(p)).max() <= 16 * U
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("W", [1, 40])
+def test_scale_has_all_its_bits(dtype, d, W):
+    """A sequence of one row: lse is the score, scale * <q, k> with <q, k> = 1024, whose products are exact.  The scales (0.6932 .. 0.697) are
+    those at which scale * log2(e) is a fifth of a float's step (2 u) or less below a float: the score in log2 units rounds by 0.4 u,
+    its product with ln 2 by half of a step, 0.73 u, and the float ln 2 is off by 0.05 u: 1.2 u in all.  The float below would be
+    1.6 u or more off."""
+    scales = np.float32(0.6932) + np.arange(1 << 16) * 2.0 ** -24
+    c2 = scales * 1.44269504088896340736
+    step = (c2 - 1) * 2.0 ** 23 % 1
+    scales = scales[step > 0.8][::800]
+    assert len(scales) >= 12 and c2.min() > 1 and (np.float32(scales) == scales).all()
+    c = dict(k=np.zeros((3, 16, 1, d)), v=np.zeros((3, 16, 1, d)), table=[[1] + [-1] * (W - 1)], lens=[1], refs=[0, 1, 0])
+    c["k"][1, 0, 0, 0] = 32.0
+    q = np.zeros((1, 1, 1, d))
+    q[..., 0] = 32.0
+    for scale in scales:
+        lse = attend(c, q, dtype, scale=float(scale))[1]
+        assert abs(host(lse).item() / (1024 * scale) - 1) <= 1.2 * U, scale
