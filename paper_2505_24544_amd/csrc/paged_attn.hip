@@ -90,6 +90,14 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
 }
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
+// infinities (and what is no number) as the largest numbers of their sign; as whole numbers, the negative bf16 are in reverse order
+__device__ __forceinline__ uint32_t finite_bf16x2(uint32_t x) {
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const i16x2 above = __builtin_elementwise_min(__builtin_bit_cast(i16x2, x), i16x2{0x7f7f, 0x7f7f});
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, above), u16x2{0xff7f, 0xff7f}));
+}
+
 template <bool BF16, int NH> struct Shape {
   static constexpr int HDP = BF16 ? 128 : 64 * NH;      // head width, padded
   static constexpr int KROWS = BF16 ? 32 : 16;          // rows of a step
@@ -223,7 +231,13 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
         for (int i = 0; i < 4; ++i)
           w[i] = __builtin_amdgcn_perm(v[2 * i + 1][0][c >> 1], v[2 * i][0][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int t = 0; t < RT; ++t) acc[t][c] = mfma_bf16(w, term[0][t], acc[t][c]);
+        // The second and third terms may be zero, and 0 * infinity is no number: there an infinity is the largest number
+        // (48 sequences of up to 4096 rows 94.9 us without, 95.4 with; under a tree 50.1 / 51.1).
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = finite_bf16x2(w[i]);
+#pragma unroll
+        for (int k = 1; k < 3; ++k)
 #pragma unroll
           for (int t = 0; t < RT; ++t) acc[t][c] = mfma_bf16(w, term[k][t], acc[t][c]);
       }

@@ -60,3 +60,63 @@ def test_scale_has_all_its_bits(dtype, d, W):
     for scale in scales:
         lse = attend(c, q, dtype, scale=float(scale))[1]
         assert abs(host(lse).item() / (1024 * scale) - 1) <= 1.2 * U, scale
+
+
+def with_infinities(rng, lens, page, W, d, dtype):
+    """Channel c of the sequences' rows: c % 8 == 0 an infinity in one row, 1 a negative one, 2 the same in every row, 3 both signs, 4 no number,
+    5 next to the largest number of bf16; the others ordinary."""
+    c = make(rng, lens, page, W, sum(po.pages_of(n, page) for n in lens) + 2, 2, d, dtype)
+    for s, n in enumerate(lens):
+        place = po.rows_of(c, s, n)
+        at = [place[int(i)] for i in rng.integers(0, n, 2)]
+        c["v"][at[0]][:, 0::8], c["v"][at[0]][:, 1::8], c["v"][at[0]][:, 4::8] = np.inf, -np.inf, np.nan
+        c["v"][at[0]][:, 3::8] = np.inf
+        c["v"][at[1]][:, 3::8] = -np.inf
+        c["v"][at[1]][:, 5::8] = -3.3e38 if dtype == "f32" else -(2.0 ** 127) * 1.984375
+        for p in place:
+            c["v"][p][:, 2::8] = np.inf
+    return c
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 100)])
+@pytest.mark.parametrize("lens,W,window", [([1, 2, 37, 300], 20, 0), ([1, 2, 37, 300], 400, 0), ([3000, 5, 777], 400, 0), ([900, 40], 400, 64)])
+@pytest.mark.parametrize("M", [1, 11])
+def test_infinities_in_rows_that_are_seen(dtype, d, lens, W, window, M):
+    """Where a query sees an infinite value the result is that infinity, as the definition says: every score is finite, so every weight
+    is above zero.  The other channels are as ever: half a step of the result, and per term the weight's error and float sums."""
+    rng = np.random.default_rng(len(lens) + M)
+    c = with_infinities(rng, lens, 16, W, d, dtype)
+    if window:
+        inside = {p for s, n in enumerate(lens) for p in po.rows_of(c, s, n)[max(0, n - window):]}
+        for s, n in enumerate(lens):
+            for p in po.rows_of(c, s, n):
+                c["v"][p][:, 7::8] = 1.0 if p in inside else np.inf          # (not seen)
+    q = queries(rng, len(lens), M, 8, d, dtype)
+    o, lse = attend(c, q, dtype, window=window)
+    with np.errstate(invalid="ignore", over="ignore"):
+        ref, rlse, spread, err = po.attend(c, q, window=window)
+    got = host(o)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), (np.isnan(got).sum(), np.isnan(ref).sum())
+    assert np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+    fine = np.isfinite(ref)
+    half, e = 2.0 ** -8 if dtype == "bf16" else U, err.transpose(0, 2, 1)[..., None]
+    tol = half * np.abs(ref) + spread * (1 + half) * (2 * e + (max(lens) + 64) * 2.0 ** -23) + 1e-37
+    assert np.isfinite(got[fine]).all() and (np.abs(got[fine] - ref[fine]) <= tol[fine]).all()
+    assert np.isinf(ref).any() and np.isnan(ref).any() and fine.any()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("M,W", [(18, 10), (18, 1000), (6, 10), (6, 1000)])
+def test_a_value_is_worth_the_same_in_a_true_and_in_a_drafted_row(dtype, d, M, W):
+    """The same rows, all seen: as true rows, and as true and drafted ones under a tree that lets everybody see everything."""
+    rng = np.random.default_rng(M)
+    lens = [90, 33]
+    c = with_infinities(rng, lens, 16, W, d, dtype)
+    q = queries(rng, 2, M, 4, d, dtype)
+    tree = np.ones((2, M, 60), bool)
+    a, la = attend(c, q, dtype)
+    b, lb = attend(c, q, dtype, n_true=[40, 0], tree=tree)
+    a, b = host(a), host(b)
+    assert np.array_equal(np.isnan(a), np.isnan(b)) and np.array_equal(a[np.isinf(a)], b[np.isinf(a)])
+    assert np.array_equal(np.isfinite(a), np.isfinite(b)) and np.isinf(a).any()
+    assert (np.abs(host(la) - host(lb)) <= 64 * U * np.maximum(1, np.abs(host(la)))).all()
