@@ -15,10 +15,11 @@ constexpr int PLAN_WAVES = PLAN / 64;
 
 __device__ __forceinline__ void add_count(int32_t* p, int v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool is_page(const PagedCache& c, int p) { return (unsigned)p < (unsigned)c.P; }
-// every thread's earlier stores and atomics are seen by the workgroup's later loads: a barrier, which waits for them, and vector
-// caches without what they held before (nobody else reads on, so nothing has to be written back for other dies: that fence
-// cost 2 us)
+// every thread's earlier stores and atomics are seen by the workgroup's later loads and atomics: all of them have reached the second-level cache
+// (the barrier alone waits for none), and the vector cache is without what it held before (nobody else reads on, so nothing
+// has to be written back for other dies: that fence cost 2 us)
 __device__ __forceinline__ void settle() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 }
