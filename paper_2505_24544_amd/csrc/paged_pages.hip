@@ -15,12 +15,16 @@ constexpr int PLAN_WAVES = PLAN / 64;
 
 __device__ __forceinline__ void add_count(int32_t* p, int v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool is_page(const PagedCache& c, int p) { return (unsigned)p < (unsigned)c.P; }
-// every thread's earlier stores and atomics are seen by the workgroup's later loads and atomics: all of them have reached the second-level cache
-// (the barrier alone waits for none), and the vector cache is without what it held before (nobody else reads on, so nothing
-// has to be written back for other dies: that fence cost 2 us)
-__device__ __forceinline__ void settle() {
+// a barrier behind which every thread's earlier loads are back, and its stores and atomics have reached the second-level cache (the barrier
+// alone waits for none)
+__device__ __forceinline__ void all_done() {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
+}
+// every thread's earlier stores and atomics are seen by the workgroup's later loads and atomics: they are done, and the vector cache is without what
+// it held before (nobody else reads on, so nothing has to be written back for other dies: that fence cost 2 us)
+__device__ __forceinline__ void settle() {
+  all_done();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 }
 
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(PLAN) void paged_fork_kernel(PagedCache c, const in
     if (i >= has[b]) now[e] = -1;
     if (i >= had[b]) old[e] = -1;
   }
-  __syncthreads();                         // (everything has been read)
+  all_done();                              // (everything has been read)
   if (tid < B) to[tid] = mine;
   __syncthreads();
 #pragma unroll
