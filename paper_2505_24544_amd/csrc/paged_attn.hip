@@ -474,7 +474,7 @@ __device__ __forceinline__ void attend_entry(const PagedAttnArgs& a, Shared<Shap
 // TREE: rows from n_true on are seen as the tree's bits say.
 // WHOLE: a workgroup of eight waves takes an entry (`worker` is its number), for few and short ones: nothing to look up, to cut or to join.
 template <bool BF16, int NH, int RT, bool TREE, bool WHOLE>
-__global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int heads8, int rowblocks) {
+__global__ __launch_bounds__(WHOLE ? 512 : 256, WHOLE ? 1 : RESIDENT) void paged_attn_kernel(PagedAttnArgs a, int rowblocks) {
   constexpr int WAVES = WHOLE ? 8 : 4;
   __shared__ Shared<Shape<BF16, NH>, RT, WAVES> shared;
   const int lane = threadIdx.x & 63;
@@ -632,16 +632,16 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
   a.parts = (int2*)(a.ml + rows * 2);
-  const int heads8 = (whole ? a.B : a.target) * a.G;
-  const dim3 grid((unsigned)((heads8 + 7) / 8 * 8 * tiles.blocks)), wg(whole ? 512 : 256);
+  const int heads = (whole ? a.B : a.target) * a.G;       // of all entries or workers
+  const dim3 grid((unsigned)((heads + 7) / 8 * 8 * tiles.blocks)), wg(whole ? 512 : 256);
   const bool tree = a.n_true != nullptr, narrow = !bf16 && a.d <= 64;
   {
     ProfScope ps("paged_attn", s);
     auto go = [&](auto bf_, auto nh_, auto rt_, auto whole_) {
       constexpr bool BF = decltype(bf_)::value != 0, WH = decltype(whole_)::value != 0;
       constexpr int NH = decltype(nh_)::value, RT = decltype(rt_)::value;
-      if (tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, true, WH>), grid, wg, 0, s, a, heads8, tiles.blocks);
-      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, false, WH>), grid, wg, 0, s, a, heads8, tiles.blocks);
+      if (tree) hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, true, WH>), grid, wg, 0, s, a, tiles.blocks);
+      else hipLaunchKernelGGL((paged_attn_kernel<BF, NH, RT, false, WH>), grid, wg, 0, s, a, tiles.blocks);
     };
     auto with = [&](auto bf_, auto nh_) {
       if (tiles.each == 1 && whole) go(bf_, nh_, int_c<1>{}, int_c<1>{});
