@@ -602,12 +602,17 @@ int workers_aimed(int R, int G) {
   return per < slots ? (int)(slots / per) : 1;
 }
 
+// rows of sums of parts: a worker has at most two entries in part (see paged_index.h), and one that is alone none
+int64_t part_rows(int R, int G) {
+  const int workers = workers_aimed(R, G);
+  return workers > 1 ? (int64_t)2 * workers * G * R : 0;
+}
+
 }  // namespace
 
-// Sums of parts: a worker has at most two (see paged_index.h).  And for each entry who has them.
+// The parts, and for each entry who has them.
 size_t paged_attn_ws_bytes(int32_t B, int32_t M, int32_t H, int32_t G) {
-  const int64_t R = (int64_t)M * (H / G);
-  return (size_t)2 * workers_aimed((int)R, G) * G * R * (128 + 2) * sizeof(float) + (size_t)B * sizeof(int2);
+  return (size_t)part_rows(M * (H / G), G) * (128 + 2) * sizeof(float) + (size_t)B * sizeof(int2);
 }
 
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
@@ -628,7 +633,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
   a.c2 = (float)c2;
   if ((double)a.c2 >= c2) a.c2 = nextafterf(a.c2, 0.f);
   a.c2_low = fmaxf((float)(c2 - a.c2), 1.1754944e-38f);
-  const int64_t rows = (int64_t)2 * a.target * a.G * R;
+  const int64_t rows = part_rows(R, a.G);
   a.part = (float*)ws;
   a.ml = a.part + rows * 128;
   a.parts = (int2*)(a.ml + rows * 2);
@@ -653,7 +658,7 @@ void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s) {
     else if (narrow) with(int_c<0>{}, int_c<1>{});
     else with(int_c<0>{}, int_c<2>{});
   }
-  if (whole || most <= 1 << PAGED_RUN) return;    // no entry is cut: nothing to join
+  if (whole || a.target == 1 || most <= 1 << PAGED_RUN) return;    // no entry is cut: nothing to join
   ProfScope ps("paged_join", s);
   auto join = [&](auto bf_, auto hdp_) {
     constexpr bool BF = decltype(bf_)::value != 0;
