@@ -697,10 +697,13 @@ beagle_status beagle_xattn_paged_compact(const beagle_xattn_desc* desc, const be
  *   beagle_xattn_draft_step_paged: q = x Wq, beagle_xattn_paged_attend, y = o Wo.
  *     With BEAGLE_FLAG_ROPE q is rotated at desc->rope_positions[b * M + m], or,
  *     if that is NULL, at the number of rows that the slot holds.  q and o are
- *     stored in io_dtype between the steps.
+ *     stored in io_dtype between the steps; a rotated q rounds once for up to
+ *     128 rows (B * M), and before and after the rotation for more.
  *       in : x_draft [B,M,D], wq [D,H*d], wo [H*d,D]    out: y [B,M,D], lse [B,H,M]
  *     Workspace: BEAGLE_WS_PAGED_DRAFT.
  *   beagle_xattn_kv_append_paged: K = x Wk, V = x Wv, beagle_xattn_paged_append.
+ *     (As in the appends to a contiguous cache, K rounds before the rotation
+ *     and behind it.)
  *       in : x_new [B,M,D], wk, wv [D,G*d]
  *     Workspace: BEAGLE_WS_PAGED_KV_APPEND.
  * desc->hidden is read; shapes and operand sizes as for beagle_xattn_draft_step

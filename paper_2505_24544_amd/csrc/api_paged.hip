@@ -65,10 +65,18 @@ beagle_status check_paged(const beagle_xattn_desc* desc, const beagle_paged_cach
 }
 
 // workspaces of the calls on states: the projected rows, then what the projections and the paged call themselves need
-struct StepWs { size_t a, b, pos, proj, call, total; };
-size_t proj_bytes(const Dims& d, int64_t N, int64_t K, bool pair) {
-  if (!d.bf16 || !kv_append_bf16_fits((int32_t)d.Tq, (int32_t)N, (int32_t)K)) return 0;
-  return align_up(kv_append_bf16_ws_bytes((int32_t)d.Tq, (int32_t)N, (int32_t)K)) / (pair ? 1 : 2);
+struct StepWs { size_t a, b, pos, angles, proj, call, total; };
+size_t proj_bytes(const Dims& d, int64_t n, int64_t N, int64_t K, bool pair) {
+  if (!d.bf16 || !kv_append_bf16_fits((int32_t)n, (int32_t)N, (int32_t)K)) return 0;
+  return align_up(kv_append_bf16_ws_bytes((int32_t)n, (int32_t)N, (int32_t)K)) / (pair ? 1 : 2);
+}
+// Rotated bf16 queries of up to this many rows are projected in passes of PROJ_ROWS, whose float sums are rotated; more are one tiled product that
+// is stored and rotated in place, as in the training forward, so they round twice.  A draft step at 4096 channels, us, in passes / by the
+// product: 65 rows 128 / 139, 120 87 / 84, 128 82 / 78, 192 96 / 78, 512 183 / 88.
+constexpr int64_t ROTATED_ROWS = 2 * PROJ_ROWS;
+int64_t pass_rows(const Dims& d) { return d.Tq < PROJ_ROWS ? d.Tq : PROJ_ROWS; }
+bool rotates_sums(const Dims& d) {
+  return d.rope && d.bf16 && d.Tq <= ROTATED_ROWS && kv_append_bf16_fits((int32_t)pass_rows(d), (int32_t)d.HD, (int32_t)d.D);
 }
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 StepWs draft_layout(const Dims& d) {
@@ -76,7 +84,8 @@ StepWs draft_layout(const Dims& d) {
   w.a = o; o += align_up((size_t)(d.Tq * d.HD) * d.esz);       // q
   w.b = o; o += align_up((size_t)(d.Tq * d.HD) * d.esz);       // o
   w.pos = o; o += align_up((size_t)d.Tq * sizeof(int32_t));
-  w.proj = o; o += align_up(larger(proj_bytes(d, d.HD, d.D, false), proj_bytes(d, d.D, d.HD, false)));
+  w.angles = o; if (rotates_sums(d)) o += align_up((size_t)pass_rows(d) * 64 * sizeof(float2));
+  w.proj = o; o += align_up(larger(proj_bytes(d, rotates_sums(d) ? pass_rows(d) : d.Tq, d.HD, d.D, false), proj_bytes(d, d.Tq, d.D, d.HD, false)));
   w.call = o; o += align_up(paged_attn_ws_bytes((int32_t)d.B, (int32_t)d.S, (int32_t)d.H, (int32_t)d.G));
   w.total = o;
   return w;
@@ -85,8 +94,8 @@ StepWs append_layout(const Dims& d, const PagedCache& c) {
   StepWs w; size_t o = 0;
   w.a = o; o += align_up((size_t)(d.Tq * d.GD) * d.esz);       // K rows
   w.b = o; o += align_up((size_t)(d.Tq * d.GD) * d.esz);       // V rows
-  w.pos = o;
-  w.proj = o; o += proj_bytes(d, d.GD, d.D, true);
+  w.pos = w.angles = o;
+  w.proj = o; o += proj_bytes(d, d.Tq, d.GD, d.D, true);
   w.call = o; o += align_up(paged_append_ws_bytes(c, (int32_t)d.B));
   w.total = o;
   return w;
@@ -251,16 +260,25 @@ beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const
   hipStream_t s = (hipStream_t)hip_stream;
   (void)hipGetLastError();
   char* base = (char*)workspace;
-  project(d, x_draft, wq, base + w.a, d.HD, d.D, base + w.proj, "draft_proj_q", s);
-  if (d.rope) {
-    const int32_t* at = d.rope_pos;
-    if (!at) {
-      launch_paged_positions(p.c, slots, (int32_t)d.B, (int32_t)d.S, (int32_t*)(base + w.pos), s);
-      at = (const int32_t*)(base + w.pos);
+  const int32_t* at = d.rope_pos;
+  if (d.rope && !at) {
+    launch_paged_positions(p.c, slots, (int32_t)d.B, (int32_t)d.S, (int32_t*)(base + w.pos), s);
+    at = (const int32_t*)(base + w.pos);
+  }
+  if (rotates_sums(d)) {
+    for (int64_t r = 0; r < d.Tq; r += PROJ_ROWS) {
+      const int64_t n = d.Tq - r < PROJ_ROWS ? d.Tq - r : PROJ_ROWS;
+      const RopeRows rope = {at + r, 0, log2((double)d.rope_base), (float2*)(base + w.angles), 1};
+      launch_proj_rope_rows_bf16((const bf16_t*)x_draft + r * d.D, wq, (bf16_t*)(base + w.a) + r * d.HD, (int32_t)n, (int32_t)d.HD, (int32_t)d.D,
+                                 base + w.proj, rope, "draft_proj_q", s);
     }
-    RopeArgs r = rope_args(d, false);
-    rope_add(r, base + w.a, d.Tq, d.Tq, d.H, 0, at);
-    launch_rope(d.bf16, r, s, "draft_rope_q");
+  } else {
+    project(d, x_draft, wq, base + w.a, d.HD, d.D, base + w.proj, "draft_proj_q", s);
+    if (d.rope) {
+      RopeArgs r = rope_args(d, false);
+      rope_add(r, base + w.a, d.Tq, d.Tq, d.H, 0, at);
+      launch_rope(d.bf16, r, s, "draft_rope_q");
+    }
   }
   PagedAttnArgs a = attn_of(p);
   set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);

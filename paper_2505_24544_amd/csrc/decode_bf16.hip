@@ -341,6 +341,35 @@ __global__ __launch_bounds__(256) void sum_slices_kernel(const float* __restrict
   *(uint2*)(y + i) = v;
 }
 
+// The same, rotated: a thread has channels c .. c + 3 and c + 64 .. of a row's head, tab[row][64] their angles.
+__global__ __launch_bounds__(256) void sum_slices_rope_kernel(const float* __restrict__ part, bf16_t* __restrict__ y, int64_t MN, int N, int KS,
+                                                              const float2* __restrict__ tab) {
+  asm volatile("" :: "s"(part), "s"(y), "s"(MN), "s"(N), "s"(KS), "s"(tab));
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, i = (t >> 4) * HD + 4 * (t & 15);
+  if (i >= MN) return;
+  const float4* angle = (const float4*)(tab + i / N * 64 + 4 * (t & 15));
+  const float4 cs0 = angle[0], cs1 = angle[1];
+  float4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+  for (int k0 = 0; k0 < KS; k0 += 8) {
+    float4 u[8], v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t o = (int64_t)min(k0 + k, KS - 1) * MN + i;
+      u[k] = *(const float4*)(part + o); v[k] = *(const float4*)(part + o + 64);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k0 + k < KS) {
+        a.x += u[k].x; a.y += u[k].y; a.z += u[k].z; a.w += u[k].w;
+        b.x += v[k].x; b.y += v[k].y; b.z += v[k].z; b.w += v[k].w;
+      }
+  }
+  const uint2 lo = {cvt_pk(a.x * cs0.x - b.x * cs0.y, a.y * cs0.z - b.y * cs0.w), cvt_pk(a.z * cs1.x - b.z * cs1.y, a.w * cs1.z - b.w * cs1.w)};
+  const uint2 hi = {cvt_pk(b.x * cs0.x + a.x * cs0.y, b.y * cs0.z + a.y * cs0.w), cvt_pk(b.z * cs1.x + a.z * cs1.y, b.w * cs1.z + a.w * cs1.w)};
+  *(uint2*)(y + i) = lo;
+  *(uint2*)(y + i + 64) = hi;
+}
+
 // m[i] = silu(sum_ks upart[ks][i]) * sum_ks wpart[ks][i]  -> bf16   (gate of the feed-forward layer, Eq. 1)
 __global__ __launch_bounds__(256) void sum_gate_kernel(const float* __restrict__ upart, const float* __restrict__ wpart,
                                                        bf16_t* __restrict__ m, int64_t MN, int KS) {
@@ -1928,6 +1957,18 @@ void launch_proj_rows_bf16(const void* x, const void* w, void* y, int32_t n, int
                      (const float*)nullptr, (bf16_t*)nullptr, (const bf16_t*)nullptr);
 }
 
+static_assert(PROJ_ROWS == dec::MAXM);
+void launch_proj_rope_rows_bf16(const void* x, const void* w, void* y, int32_t n, int32_t N, int32_t K, void* ws, const RopeRows& rope,
+                                const char* name, hipStream_t s) {
+  using namespace dec;
+  const int KS = (K + SG_K - 1) / SG_K;
+  const int64_t MN = (int64_t)n * N;
+  ProfScope ps(name, s);
+  hipLaunchKernelGGL(skinny_gemm_kernel<false>, dim3(N / SG_N + 1, KS), dim3(256), 0, s, (const bf16_t*)x, (const bf16_t*)w, (float*)ws, n, N,
+                     K, CombineArgs{}, (const bf16_t*)nullptr, (float*)nullptr, 0, rope);
+  hipLaunchKernelGGL(sum_slices_rope_kernel, dim3((unsigned)((MN / 8 + 255) / 256)), dim3(256), 0, s, (const float*)ws, (bf16_t*)y, MN, N, KS,
+                     (const float2*)rope.tab);
+}
 
 // ---- feed-forward layer of the draft block for a handful of rows (decode time): HBM-bound on the three weight
 // matrices, so the same split-k streaming projection: [z W_gate, z W_up] in one launch (z = 0 / 1), the gate fused
