@@ -629,8 +629,13 @@ size_t beagle_xattn_paged_workspace_bytes(const beagle_xattn_desc* desc, const b
  *   in : q [B,M,H,d] (rotated by the caller if its model rotates), slots,
  *        n_true [B] or NULL, tree_mask uint32 [B,M,mask_words] or NULL
  *   out: o [B,M,H,d], lse [B,H,M] float
- * The work is split by the lengths as they stand on the device: a batch of any
- * mix of lengths takes the time of its rows in all.
+ * All M queries of an entry see the same window.
+ * The work is split by the lengths as they stand on the device, so a batch of any
+ * mix of lengths takes about the time of its rows in all; each of thousands of
+ * short entries takes 0.08 us at least (8192 of up to 60 rows 680 us, their
+ * rows alone 190).  desc->seq_kv is a matter of speed, too: by it the call chooses
+ * how it is launched, and a bound far above the longest sequence costs batches of
+ * short ones up to 4 us (20 sequences of 400 rows: 10.4 us, with 32768 14.1).
  * Workspace: BEAGLE_WS_PAGED_ATTEND.
  */
 beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
@@ -644,7 +649,8 @@ beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const bea
  * [0, M]) rows at pos[b] .. pos[b] + n - 1: resetting a sequence to its true rows
  * and appending the next ones is one call, n = 0 alone drops rows.  A page that
  * the slot keeps a part of and shares with others is copied first, so other
- * slots never see the change.  (Where the table names no page for the kept part, the
+ * slots never see the change; where all that hold it append in one call, each of
+ * them copies it.  (Where the table names no page for the kept part, the
  * new rows go into a fresh one, whose rows before them hold what they held.)
  * With BEAGLE_FLAG_ROPE the K rows are rotated, at
  * desc->rope_positions[b * M + i] or, if that is NULL, at their row numbers.

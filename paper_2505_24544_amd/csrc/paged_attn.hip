@@ -12,10 +12,10 @@
 // the maximum and the weight of its part in the workspace, and a second launch joins them in the order of the rows.  Where workers suffice
 // for it, each entry is cut for itself instead, so that no worker has two, and few short entries go to a workgroup each, in one launch.
 //
-// Measured (MI355X; rows of 8 kv heads, 32 query heads unless said; a graph's replays): 48 sequences of up to 4096 rows 94 us
-// (462 MB, 4.9 TB/s), 4 of up to 32768 with 40 heads 355 (1974 MB, 5.6; a kernel that only reads reaches 6.0), 12 of up to 4096
-// with 10 queries each under a tree 43.6, one of 777 rows of 32 kv heads 10.0.  The counters have every visible row fetched once from HBM, and
-// vector and matrix instructions issue in a tenth of the waves' time: they wait for rows, or for room to ask for more.
+// Measured (MI355X; rows of 8 kv heads, 32 query heads unless said; a graph's replays): 48 sequences of up to 4096 rows 95 us
+// (462 MB, 4.9 TB/s), 4 of up to 32768 with 40 heads 357 (1974 MB, 5.5; a kernel that only reads reaches 6.0), 12 of up to 4096
+// with 10 queries each under a tree 47.4, one of 777 rows of 32 kv heads 10.3.  The counters have every visible row fetched once from HBM, and
+// vector and matrix instructions issue in a tenth of the waves' time (under the tree a fifth): they wait for rows, or for room to ask for more.
 //
 // Layout.  A wave keeps everything in registers and shares nothing until its end: S^T = K Q^T puts a query in a
 // column (lane % 16) and four keys in a lane, which is at once the layout that O^T = V^T P^T wants of P^T.  V rows are

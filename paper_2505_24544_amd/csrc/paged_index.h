@@ -47,8 +47,10 @@ PAGED_HD bool paged_all_seen(const PagedRows& r, int first, int count) {
 
 // Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs, one for each; an entry of up to
 // four blocks is not cut but goes whole to the worker that has its first block.  A worker so has at most two entries in part, its first
-// and its last.  Where each entry can be cut for itself into runs of four blocks (or of eight, if that is not much more than an equal share), with
+// and its last.  Where each entry can be cut for itself into runs of four blocks (or of eight, if an equal share is three blocks at least), with
 // a worker for each run, entries count as multiples of the run's length instead: then no worker has two, one behind the other.
+// Equal runs / runs of eight, us (8 kv heads of 128 bf16, 64 workers): 40 entries of 150 rows 14.2 / 10.8, 20 with 10 queries each 20.9 / 13.4; below the
+// limit the runs would be no slower either: 36 entries 13.9 / 10.7.
 constexpr int PAGED_RUN = 2, PAGED_LONG_RUN = 3;         // runs of 1 << PAGED_RUN or 1 << PAGED_LONG_RUN blocks
 struct PagedSplit { int64_t all; int workers, shift; bool apart; };
 PAGED_HD int paged_runs(int blocks, int shift) { return (blocks + (1 << shift) - 1) >> shift; }
