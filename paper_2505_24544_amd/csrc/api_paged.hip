@@ -1,6 +1,7 @@
 // C-ABI entry points of the paged cache: validation, workspace carving and launch order only.
 #include "api_internal.h"
 #include "paged.h"
+#include "proj_rows.h"
 
 #include <math.h>
 #include <string.h>

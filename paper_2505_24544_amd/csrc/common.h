@@ -249,14 +249,6 @@ void launch_read_probe(const void* buf, int64_t bytes, int wgs, uint32_t* sink, 
 void launch_clock_probe(uint64_t* out, hipStream_t s);
 size_t kv_append_bf16_ws_bytes(int32_t n, int32_t N, int32_t K);
 bool kv_append_bf16_fits(int32_t n, int32_t N, int32_t K);
-constexpr int PROJ_ROWS = 64;              // rows of a streaming projection, at most
-// y = x W for up to 64 rows (kv_append_bf16_fits), split over k; ws: half of kv_append_bf16_ws_bytes
-void launch_proj_rows_bf16(const void* x, const void* w, void* y, int32_t n, int32_t N, int32_t K, void* ws, const char* name, hipStream_t s);
-struct RopeRows;
-// The same with the rows of each head (128 wide) rotated: the finished float sums are, so a value rounds once.  rope.pos: of every row;
-// rope.tab: room for n rows
-void launch_proj_rope_rows_bf16(const void* x, const void* w, void* y, int32_t n, int32_t N, int32_t K, void* ws, const RopeRows& rope,
-                                const char* name, hipStream_t s);
 // feed-forward layer for a handful of rows: h = (silu(z W_gate) * (z W_up)) W_down + y_res
 size_t block_mlp_bf16_ws_bytes(int32_t M, int32_t D, int32_t F);
 bool block_mlp_bf16_fits(int32_t D, int32_t F);

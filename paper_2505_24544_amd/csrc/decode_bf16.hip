@@ -35,6 +35,7 @@
 #include <algorithm>
 #include <type_traits>
 #include "attn_tiles.h"
+#include "proj_rows.h"
 
 namespace beagle {
 using namespace tiles;
