@@ -604,7 +604,8 @@ typedef struct {
 } beagle_paged_cache;
 
 enum { BEAGLE_WS_PAGED_ATTEND = 0, BEAGLE_WS_PAGED_APPEND = 1, BEAGLE_WS_PAGED_FORK = 2, BEAGLE_WS_PAGED_COMPACT = 3,
-       BEAGLE_WS_PAGED_DRAFT = 4, BEAGLE_WS_PAGED_KV_APPEND = 5 };
+       BEAGLE_WS_PAGED_DRAFT = 4, BEAGLE_WS_PAGED_KV_APPEND = 5, BEAGLE_WS_PAGED_SHARED = 8, BEAGLE_WS_PAGED_SELECT = 9,
+       BEAGLE_WS_PAGED_BLOCKS = 10, BEAGLE_WS_PAGED_DRAFT_SHARED = 11, BEAGLE_WS_PAGED_DRAFT_BLOCKS = 12 };   /* (6, 7: none) */
 
 /* Workspace bytes of a paged call (`which` is BEAGLE_WS_PAGED_*); 0 for an
  * invalid descriptor or cache. */
@@ -720,6 +721,99 @@ beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const
     int32_t window, int32_t sinks, void* y, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 beagle_status beagle_xattn_kv_append_paged(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_new,
     const void* wk, const void* wv, const int32_t* slots, const int32_t* pos, const int32_t* n_new, int32_t* short_pages,
+    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * beagle_xattn_paged_attend for entries whose sequences begin with the same
+ * rows (branches of one sequence, as beagle_xattn_paged_fork makes them; users
+ * under one prompt): the common rows are fetched once for all of a group.
+ * Group g is the entries group_first[g] .. group_first[g + 1] - 1 (an element
+ * below the one before it counts as that one; entries outside all groups have
+ * no common rows).  With nt as in beagle_xattn_paged_attend, a true row j < nt
+ * of an entry is
+ *   j < n_shared[g]: row j of the slot of the group's FIRST entry (not seen if
+ *                    that slot does not hold it, or it is not below seq_kv),
+ *   otherwise      : row j of the entry's own slot;
+ * drafted rows are its own, seen as the tree says.  Where the sequences do
+ * begin with the same rows this is beagle_xattn_paged_attend without a window, but
+ * for the order of the sums.  Entries of any lengths go together, empty ones too.
+ *   in : as beagle_xattn_paged_attend; group_first [n_groups + 1], n_shared
+ *        [n_groups], DEVICE; 1 <= n_groups <= B
+ *   out: o [B,M,H,d], lse [B,H,M] float
+ * B * M * H / G at most 2^28.
+ * Workspace: BEAGLE_WS_PAGED_SHARED.
+ */
+beagle_status beagle_xattn_paged_attend_shared(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* group_first, const int32_t* n_shared, int32_t n_groups, const int32_t* n_true,
+    const uint32_t* tree_mask, int32_t mask_words, void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Attention to a few pages of a long context, in three calls.
+ *
+ * beagle_xattn_paged_bounds keeps, next to the cache, the least and the greatest
+ * value of every channel of a page's keys: bounds [P,G,2,d] in io_dtype,
+ *   bounds[p,g,0,c] = min_j k_pages[p,j,g,c],  bounds[p,g,1,c] = max_j.
+ * It writes those of the pages of slot slots[b] that are whole (all of their
+ * rows are held) and hold a row from first[b] on (first NULL: all whole pages);
+ * all others keep theirs.  After an append at pos it is called with first = pos,
+ * after a compaction on the new pool with NULL; a fork needs no call.  What is
+ * no number is passed over (a channel of nothing else: +infinity, -infinity).
+ *   in    : slots, first [B] or NULL    in/out: bounds
+ *
+ * beagle_xattn_paged_select picks pages by them.  Pages are counted along the
+ * sequence: page p holds its rows p * page_rows ...  With n, nt as in
+ * beagle_xattn_paged_attend, the pages from lead = ceil(sinks / page_rows) up to
+ * tail = max(nt - window, 0) / page_rows (rounded down, not counted in) are there
+ * to be picked, all of them whole; those before and behind are always seen.
+ * For a kv head with the query rows r of its H / G heads and M queries,
+ *   score(p) = max_r sum_c (q_rc > 0 ? q_rc hi_pc : q_rc < 0 ? q_rc lo_pc : 0)
+ * in 64 bits, rounded to float once per r (a sum that is no number is passed over; with none left,
+ * or a page number outside the pool, -infinity): no key of the page has a larger
+ * product with any of the queries.  The n_select pages with the highest scores,
+ * of equal ones the first, go to pages [B,G,n_select] in ascending order, -1
+ * behind them where there are fewer.
+ *   in : q, slots, n_true as in beagle_xattn_paged_attend (the queries that will
+ *        attend), bounds    out: pages
+ * Workspace: BEAGLE_WS_PAGED_SELECT.
+ *
+ * beagle_xattn_paged_attend_blocks is beagle_xattn_paged_attend over those rows: the
+ * queries of a kv head see a true row j < nt iff its page is before lead, from
+ * tail on, or listed for the head; drafted rows as the tree says.  (window and
+ * sinks so count in whole pages here, and window = 0 is none: only the page that
+ * the true rows end in.)  A list is ascending; its first min(n_select, max(tail -
+ * lead, 0)) numbers are read, and one that is not above the number before it, or not a page that
+ * is there to be picked, lists nothing.  It may come from beagle_xattn_paged_select, of this or of
+ * an earlier set of queries, or from the caller.
+ *   in : as beagle_xattn_paged_attend; pages [B,G,n_select] DEVICE
+ *   out: o [B,M,H,d], lse [B,H,M] float
+ * Workspace: BEAGLE_WS_PAGED_BLOCKS.
+ * 1 <= n_select <= 2^26.
+ */
+beagle_status beagle_xattn_paged_bounds(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const int32_t* slots,
+    const int32_t* first, void* bounds, void* hip_stream);
+beagle_status beagle_xattn_paged_select(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* n_true, const void* bounds, int32_t window, int32_t sinks, int32_t n_select, int32_t* pages,
+    void* workspace, size_t workspace_bytes, void* hip_stream);
+beagle_status beagle_xattn_paged_attend_blocks(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words, int32_t window, int32_t sinks,
+    const int32_t* pages, int32_t n_select, void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * beagle_xattn_draft_step_paged with these attentions in the place of
+ * beagle_xattn_paged_attend:
+ *   beagle_xattn_draft_step_paged_shared: beagle_xattn_paged_attend_shared.
+ *     Workspace: BEAGLE_WS_PAGED_DRAFT_SHARED.
+ *   beagle_xattn_draft_step_paged_blocks: beagle_xattn_paged_select with the
+ *     step's projected (and rotated) queries, then beagle_xattn_paged_attend_blocks;
+ *     pages [B,G,n_select] is an output.  Workspace: BEAGLE_WS_PAGED_DRAFT_BLOCKS.
+ */
+beagle_status beagle_xattn_draft_step_paged_shared(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* group_first, const int32_t* n_shared, int32_t n_groups,
+    const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words, void* y, float* lse, void* workspace, size_t workspace_bytes,
+    void* hip_stream);
+beagle_status beagle_xattn_draft_step_paged_blocks(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words,
+    const void* bounds, int32_t window, int32_t sinks, int32_t n_select, int32_t* pages, void* y, float* lse,
     void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---- mask / index inspection (HOST memory, integers only, no GPU needed) --

@@ -25,6 +25,8 @@ BEAGLE_WS_FWD, BEAGLE_WS_BWD, BEAGLE_WS_DRAFT, BEAGLE_WS_APPEND, BEAGLE_WS_BWD_S
 BEAGLE_WS_BLOCK_FWD, BEAGLE_WS_BLOCK_BWD, BEAGLE_WS_BLOCK_DRAFT, BEAGLE_WS_BLOCK_BWD_SIM = 0, 1, 2, 3
 (BEAGLE_WS_PAGED_ATTEND, BEAGLE_WS_PAGED_APPEND, BEAGLE_WS_PAGED_FORK, BEAGLE_WS_PAGED_COMPACT, BEAGLE_WS_PAGED_DRAFT,
  BEAGLE_WS_PAGED_KV_APPEND) = range(6)
+(BEAGLE_WS_PAGED_SHARED, BEAGLE_WS_PAGED_SELECT, BEAGLE_WS_PAGED_BLOCKS, BEAGLE_WS_PAGED_DRAFT_SHARED,
+ BEAGLE_WS_PAGED_DRAFT_BLOCKS) = range(8, 13)
 STATUS_NAMES = {0: "BEAGLE_OK", 1: "BEAGLE_ERR_NULL", 2: "BEAGLE_ERR_SHAPE", 3: "BEAGLE_ERR_UNSUPPORTED",
                 4: "BEAGLE_ERR_WORKSPACE", 5: "BEAGLE_ERR_ALIGN", 6: "BEAGLE_ERR_HIP"}
 
@@ -39,6 +41,8 @@ EXPORTS = (
     "beagle_xattn_block_kv_append",
     "beagle_xattn_paged_workspace_bytes", "beagle_xattn_paged_attend", "beagle_xattn_paged_append", "beagle_xattn_paged_fork",
     "beagle_xattn_paged_compact", "beagle_xattn_draft_step_paged", "beagle_xattn_kv_append_paged",
+    "beagle_xattn_paged_attend_shared", "beagle_xattn_paged_bounds", "beagle_xattn_paged_select", "beagle_xattn_paged_attend_blocks",
+    "beagle_xattn_draft_step_paged_shared", "beagle_xattn_draft_step_paged_blocks",
     "beagle_xattn_mask_row_limit", "beagle_xattn_mask_dense", "beagle_xattn_tile_map",
     "beagle_xattn_profile_begin", "beagle_xattn_profile_end", "beagle_xattn_profile_get",
     "beagle_xattn_probe_read", "beagle_xattn_probe_clock", "beagle_xattn_status_string", "beagle_xattn_version",
@@ -234,6 +238,14 @@ def lib() -> C.CDLL:
     L.beagle_xattn_paged_compact.argtypes = [dp, cp, cp, vp] + [vp, C.c_size_t, vp]
     L.beagle_xattn_draft_step_paged.restype = C.c_int
     L.beagle_xattn_draft_step_paged.argtypes = [dp, cp, vp, vp, vp] + view + [vp, vp] + [vp, C.c_size_t, vp]
+    i32, ws = C.c_int32, [vp, C.c_size_t, vp]
+    for name, args in (("paged_attend_shared", [vp] * 4 + [i32, vp, vp, i32, vp, vp] + ws), ("paged_bounds", [vp] * 4),
+                       ("paged_select", [vp] * 4 + [i32, i32, i32, vp] + ws),
+                       ("paged_attend_blocks", [vp] + view + [vp, i32, vp, vp] + ws),
+                       ("draft_step_paged_shared", [vp] * 6 + [i32, vp, vp, i32, vp, vp] + ws),
+                       ("draft_step_paged_blocks", [vp] * 6 + [i32, vp, i32, i32, i32, vp, vp, vp] + ws)):
+        fn = getattr(L, "beagle_xattn_" + name)
+        fn.restype, fn.argtypes = C.c_int, [dp, cp] + args
     L.beagle_xattn_kv_append_paged.restype = C.c_int
     L.beagle_xattn_kv_append_paged.argtypes = [dp, cp] + [vp] * 7 + [vp, C.c_size_t, vp]
     L.beagle_xattn_mask_row_limit.restype = C.c_int
@@ -434,6 +446,7 @@ def beagle_xattn_kv_append(desc, x_new, wk, wv, k_cache, v_cache, pos, workspace
 
 
 _torch = _WHOLE = _FLOAT = _BF16 = None
+_NO_WORKSPACE = object()                                  # in the place of a workspace: the call takes none
 
 
 class _Paged:
@@ -492,8 +505,19 @@ class _Paged:
         B = self.desc.batch
         return (self.ints(slots, B), self.ints(n_true, B), self.ints(tree_mask, self.n * mask_words), mask_words, window, sinks)
 
+    def groups(self, group_first, n_shared, n_groups):
+        return self.ints(group_first, n_groups + 1), self.ints(n_shared, n_groups), n_groups
+
+    def bounds(self, t, cache):
+        return self._at(t, cache.n_pages * self.desc.n_kv_heads * 2 * self.desc.head_dim, self.dtypes)
+
+    def pages(self, t, n_select):
+        return self.ints(t, self.desc.batch * self.desc.n_kv_heads * n_select)
+
     def call(self, name, cache, args, workspace, workspace_bytes, stream, check):
         """By default on the current stream of the cache's device, which is made the current one meanwhile."""
+        if workspace is _NO_WORKSPACE:
+            return self._call(name, cache, args, stream, check)
         if workspace is not None and not isinstance(workspace, int):
             if workspace.get_device() != self.index:
                 self._on_device(workspace)
@@ -502,13 +526,16 @@ class _Paged:
             if workspace_bytes is None:
                 workspace_bytes = workspace.nbytes
             workspace = workspace.data_ptr()
+        return self._call(name, cache, (*args, workspace, workspace_bytes or 0), stream, check)
+
+    def _call(self, name, cache, args, stream, check):
         fn = getattr(_lib or lib(), name)
         if self.dev is not None and self.dev.type != "cuda":
             raise ValueError("the cache is on %s, not on a GPU" % self.dev)
         if self.dev is not None and not cache.alone and self.index != _torch.cuda.current_device():
             with _torch.cuda.device(self.dev):
-                return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
-        return _check(fn(self.desc, cache, *args, workspace, workspace_bytes or 0, _stream(stream)), name, check)
+                return _check(fn(self.desc, cache, *args, _stream(stream)), name, check)
+        return _check(fn(self.desc, cache, *args, _stream(stream)), name, check)
 
 
 def beagle_xattn_paged_workspace_bytes(desc, cache, which) -> int:
@@ -521,6 +548,38 @@ def beagle_xattn_paged_attend(desc, cache, q, slots, n_true, tree_mask, mask_wor
     width = desc.n_q_heads * desc.head_dim
     args = (c.rows(q, width), *c.view(slots, n_true, tree_mask, mask_words, window, sinks), c.rows(o, width), c.lse(lse))
     return c.call("beagle_xattn_paged_attend", cache, args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_attend_shared(desc, cache, q, slots, group_first, n_shared, n_groups, n_true, tree_mask, mask_words, o, lse,
+                                     workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    c = _Paged(desc, cache)
+    width = desc.n_q_heads * desc.head_dim
+    slots, n_true, tree_mask, mask_words, _, _ = c.view(slots, n_true, tree_mask, mask_words, 0, 0)
+    args = (c.rows(q, width), slots, *c.groups(group_first, n_shared, n_groups), n_true, tree_mask, mask_words, c.rows(o, width), c.lse(lse))
+    return c.call("beagle_xattn_paged_attend_shared", cache, args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_bounds(desc, cache, slots, first, bounds, stream=None, *, check=True) -> int:
+    c = _Paged(desc, cache)
+    args = (c.ints(slots, desc.batch), c.ints(first, desc.batch), c.bounds(bounds, cache))
+    return c.call("beagle_xattn_paged_bounds", cache, args, _NO_WORKSPACE, None, stream, check)
+
+
+def beagle_xattn_paged_select(desc, cache, q, slots, n_true, bounds, window, sinks, n_select, pages, workspace, stream=None, *,
+                              workspace_bytes=None, check=True) -> int:
+    c = _Paged(desc, cache)
+    args = (c.rows(q, desc.n_q_heads * desc.head_dim), c.ints(slots, desc.batch), c.ints(n_true, desc.batch), c.bounds(bounds, cache),
+            window, sinks, n_select, c.pages(pages, n_select))
+    return c.call("beagle_xattn_paged_select", cache, args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_paged_attend_blocks(desc, cache, q, slots, n_true, tree_mask, mask_words, window, sinks, pages, n_select, o, lse,
+                                     workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    c = _Paged(desc, cache)
+    width = desc.n_q_heads * desc.head_dim
+    args = (c.rows(q, width), *c.view(slots, n_true, tree_mask, mask_words, window, sinks), c.pages(pages, n_select), n_select,
+            c.rows(o, width), c.lse(lse))
+    return c.call("beagle_xattn_paged_attend_blocks", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_paged_append(desc, cache, slots, pos, n_new, k_new, v_new, short_pages, workspace, stream=None, *,
@@ -552,6 +611,26 @@ def beagle_xattn_draft_step_paged(desc, cache, x_draft, wq, wo, slots, n_true, t
     args = (c.rows(x_draft, D), c.weight(wq, D * HD), c.weight(wo, D * HD),
             *c.view(slots, n_true, tree_mask, mask_words, window, sinks), c.rows(y, D), c.lse(lse))
     return c.call("beagle_xattn_draft_step_paged", cache, args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_draft_step_paged_shared(desc, cache, x_draft, wq, wo, slots, group_first, n_shared, n_groups, n_true, tree_mask,
+                                         mask_words, y, lse, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    c = _Paged(desc, cache)
+    D, HD = desc.hidden, desc.n_q_heads * desc.head_dim
+    slots, n_true, tree_mask, mask_words, _, _ = c.view(slots, n_true, tree_mask, mask_words, 0, 0)
+    args = (c.rows(x_draft, D), c.weight(wq, D * HD), c.weight(wo, D * HD), slots, *c.groups(group_first, n_shared, n_groups), n_true,
+            tree_mask, mask_words, c.rows(y, D), c.lse(lse))
+    return c.call("beagle_xattn_draft_step_paged_shared", cache, args, workspace, workspace_bytes, stream, check)
+
+
+def beagle_xattn_draft_step_paged_blocks(desc, cache, x_draft, wq, wo, slots, n_true, tree_mask, mask_words, bounds, window, sinks,
+                                         n_select, pages, y, lse, workspace, stream=None, *, workspace_bytes=None, check=True) -> int:
+    c = _Paged(desc, cache)
+    D, HD = desc.hidden, desc.n_q_heads * desc.head_dim
+    slots, n_true, tree_mask, mask_words, window, sinks = c.view(slots, n_true, tree_mask, mask_words, window, sinks)
+    args = (c.rows(x_draft, D), c.weight(wq, D * HD), c.weight(wo, D * HD), slots, n_true, tree_mask, mask_words, c.bounds(bounds, cache),
+            window, sinks, n_select, c.pages(pages, n_select), c.rows(y, D), c.lse(lse))
+    return c.call("beagle_xattn_draft_step_paged_blocks", cache, args, workspace, workspace_bytes, stream, check)
 
 
 def beagle_xattn_kv_append_paged(desc, cache, x_new, wk, wv, slots, pos, n_new, short_pages, workspace, stream=None, *,

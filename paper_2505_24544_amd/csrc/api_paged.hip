@@ -80,14 +80,15 @@ bool rotates_sums(const Dims& d) {
   return d.rope && d.bf16 && d.Tq <= ROTATED_ROWS && kv_append_bf16_fits((int32_t)pass_rows(d), (int32_t)d.HD, (int32_t)d.D);
 }
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
-StepWs draft_layout(const Dims& d) {
+size_t attend_bytes(const Dims& d) { return align_up(paged_attn_ws_bytes((int32_t)d.B, (int32_t)d.S, (int32_t)d.H, (int32_t)d.G)); }
+StepWs draft_layout(const Dims& d, size_t attention) {
   StepWs w; size_t o = 0;
   w.a = o; o += align_up((size_t)(d.Tq * d.HD) * d.esz);       // q
   w.b = o; o += align_up((size_t)(d.Tq * d.HD) * d.esz);       // o
   w.pos = o; o += align_up((size_t)d.Tq * sizeof(int32_t));
   w.angles = o; if (rotates_sums(d)) o += align_up((size_t)pass_rows(d) * 64 * sizeof(float2));
   w.proj = o; o += align_up(larger(proj_bytes(d, rotates_sums(d) ? pass_rows(d) : d.Tq, d.HD, d.D, false), proj_bytes(d, d.Tq, d.D, d.HD, false)));
-  w.call = o; o += align_up(paged_attn_ws_bytes((int32_t)d.B, (int32_t)d.S, (int32_t)d.H, (int32_t)d.G));
+  w.call = o; o += attention;
   w.total = o;
   return w;
 }
@@ -111,6 +112,11 @@ PagedAttnArgs attn_of(const Paged& p) {
   a.scale = p.scale;
   return a;
 }
+// shared prefixes: the query rows of all entries of a kv head are counted in 32 bits
+bool shared_fits(const Dims& d) { return d.Tq * (d.H / d.G) <= (1 << 28); }
+size_t shared_bytes(const Dims& d) { return align_up(paged_shared_ws_bytes((int32_t)d.B, (int32_t)d.S, (int32_t)d.H, (int32_t)d.G)); }
+size_t select_bytes(const Paged& p) { return align_up(paged_select_ws_bytes(p.c, (int32_t)p.d.B, (int32_t)p.d.G, attn_of(p).bound)); }
+size_t draft_blocks_bytes(const Paged& p) { return select_bytes(p) + attend_bytes(p.d); }
 PagedAppendArgs append_of(const Paged& p) {
   PagedAppendArgs a; memset(&a, 0, sizeof(a));
   a.c = p.c;
@@ -132,6 +138,26 @@ void set_view(PagedAttnArgs& a, const int32_t* slots, const int32_t* n_true, con
   a.tree = tree_mask; a.words = tree_mask ? mask_words : 0;
   a.window = window; a.sinks = sinks;
 }
+beagle_status check_groups(const Dims& d, const int32_t* group_first, const int32_t* n_shared, int32_t n_groups) {
+  if (!shared_fits(d)) return BEAGLE_ERR_UNSUPPORTED;
+  if (n_groups < 1 || n_groups > d.B) return BEAGLE_ERR_SHAPE;
+  if (!group_first || !n_shared) return BEAGLE_ERR_NULL;
+  return (((uintptr_t)group_first) | ((uintptr_t)n_shared)) & 3u ? BEAGLE_ERR_ALIGN : BEAGLE_OK;
+}
+beagle_status check_pages(const int32_t* pages, int32_t n_select) {
+  if (n_select < 1 || n_select > (1 << 26)) return BEAGLE_ERR_SHAPE;
+  if (!pages) return BEAGLE_ERR_NULL;
+  return (uintptr_t)pages & 3u ? BEAGLE_ERR_ALIGN : BEAGLE_OK;
+}
+PagedSelectArgs select_of(const Paged& p, const void* q, const int32_t* slots, const int32_t* n_true, const void* bounds, int32_t window,
+                          int32_t sinks, int32_t n_select, int32_t* pages) {
+  PagedSelectArgs a; memset(&a, 0, sizeof(a));
+  const PagedAttnArgs x = attn_of(p);
+  a.c = p.c; a.B = x.B; a.M = x.M; a.H = x.H; a.G = x.G; a.d = x.d; a.bound = x.bound;
+  a.q = q; a.bounds = bounds; a.slots = slots; a.n_true = n_true;
+  a.window = window; a.sinks = sinks; a.n_select = n_select; a.pages = pages;
+  return a;
+}
 bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
@@ -142,14 +168,21 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 
 size_t beagle_xattn_paged_workspace_bytes(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, int which) {
   Paged p;
-  if (check_paged(desc, cache, which == BEAGLE_WS_PAGED_DRAFT || which == BEAGLE_WS_PAGED_KV_APPEND, &p) != BEAGLE_OK) return 0;
+  const bool states = which == BEAGLE_WS_PAGED_DRAFT || which == BEAGLE_WS_PAGED_KV_APPEND || which == BEAGLE_WS_PAGED_DRAFT_SHARED ||
+                      which == BEAGLE_WS_PAGED_DRAFT_BLOCKS;
+  if (check_paged(desc, cache, states, &p) != BEAGLE_OK) return 0;
   switch (which) {
-    case BEAGLE_WS_PAGED_ATTEND: return align_up(paged_attn_ws_bytes((int32_t)p.d.B, (int32_t)p.d.S, (int32_t)p.d.H, (int32_t)p.d.G));
+    case BEAGLE_WS_PAGED_ATTEND: return attend_bytes(p.d);
     case BEAGLE_WS_PAGED_APPEND: return align_up(paged_append_ws_bytes(p.c, (int32_t)p.d.B));
     case BEAGLE_WS_PAGED_FORK: return align_up(paged_fork_ws_bytes(p.c, (int32_t)p.d.B));
     case BEAGLE_WS_PAGED_COMPACT: return align_up(paged_compact_ws_bytes(p.c));
-    case BEAGLE_WS_PAGED_DRAFT: return draft_layout(p.d).total;
+    case BEAGLE_WS_PAGED_DRAFT: return draft_layout(p.d, attend_bytes(p.d)).total;
     case BEAGLE_WS_PAGED_KV_APPEND: return append_layout(p.d, p.c).total;
+    case BEAGLE_WS_PAGED_SHARED: return shared_fits(p.d) ? shared_bytes(p.d) : 0;
+    case BEAGLE_WS_PAGED_SELECT: return select_bytes(p);
+    case BEAGLE_WS_PAGED_BLOCKS: return attend_bytes(p.d);
+    case BEAGLE_WS_PAGED_DRAFT_SHARED: return shared_fits(p.d) ? draft_layout(p.d, shared_bytes(p.d)).total : 0;
+    case BEAGLE_WS_PAGED_DRAFT_BLOCKS: return draft_layout(p.d, draft_blocks_bytes(p)).total;
     default: return 0;
   }
 }
@@ -178,6 +211,79 @@ beagle_status beagle_xattn_paged_attend(const beagle_xattn_desc* desc, const bea
   set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);
   a.q = q; a.o = o; a.lse = lse;
   launch_paged_attn(p.d.bf16, a, workspace, (hipStream_t)hip_stream);
+  return hip_status();
+}
+
+beagle_status beagle_xattn_paged_attend_shared(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* group_first, const int32_t* n_shared, int32_t n_groups, const int32_t* n_true,
+    const uint32_t* tree_mask, int32_t mask_words, void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, false, &p);
+  if (st != BEAGLE_OK) return st;
+  if (!q || !o || !lse) return BEAGLE_ERR_NULL;
+  if (!aligned16(q) || !aligned16(o) || !aligned16(lse)) return BEAGLE_ERR_ALIGN;
+  st = check_groups(p.d, group_first, n_shared, n_groups);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, tree_mask, mask_words, 0, 0);
+  if (st != BEAGLE_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, shared_bytes(p.d));
+  if (st != BEAGLE_OK) return st;
+  (void)hipGetLastError();
+  PagedSharedArgs a = {attn_of(p), group_first, n_shared, n_groups};
+  set_view(a.a, slots, n_true, tree_mask, mask_words, 0, 0);
+  a.a.q = q; a.a.o = o; a.a.lse = lse;
+  launch_paged_shared(p.d.bf16, a, workspace, (hipStream_t)hip_stream);
+  return hip_status();
+}
+
+beagle_status beagle_xattn_paged_bounds(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const int32_t* slots,
+    const int32_t* first, void* bounds, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, false, &p);
+  if (st != BEAGLE_OK) return st;
+  if (!bounds) return BEAGLE_ERR_NULL;
+  if (!aligned16(bounds)) return BEAGLE_ERR_ALIGN;
+  if ((((uintptr_t)slots) | ((uintptr_t)first)) & 3u) return BEAGLE_ERR_ALIGN;
+  (void)hipGetLastError();
+  launch_paged_bounds(p.d.bf16, p.c, (int32_t)p.d.B, (int32_t)p.d.G, (int32_t)p.d.d, attn_of(p).bound, slots, first, bounds, (hipStream_t)hip_stream);
+  return hip_status();
+}
+
+beagle_status beagle_xattn_paged_select(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* n_true, const void* bounds, int32_t window, int32_t sinks, int32_t n_select, int32_t* pages,
+    void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, false, &p);
+  if (st != BEAGLE_OK) return st;
+  if (!q || !bounds) return BEAGLE_ERR_NULL;
+  if (!aligned16(q) || !aligned16(bounds)) return BEAGLE_ERR_ALIGN;
+  st = check_pages(pages, n_select);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, nullptr, 0, window, sinks);
+  if (st != BEAGLE_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, select_bytes(p));
+  if (st != BEAGLE_OK) return st;
+  (void)hipGetLastError();
+  launch_paged_select(p.d.bf16, select_of(p, q, slots, n_true, bounds, window, sinks, n_select, pages), workspace, (hipStream_t)hip_stream);
+  return hip_status();
+}
+
+beagle_status beagle_xattn_paged_attend_blocks(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* q,
+    const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words, int32_t window, int32_t sinks,
+    const int32_t* pages, int32_t n_select, void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, false, &p);
+  if (st != BEAGLE_OK) return st;
+  if (!q || !o || !lse) return BEAGLE_ERR_NULL;
+  if (!aligned16(q) || !aligned16(o) || !aligned16(lse)) return BEAGLE_ERR_ALIGN;
+  st = check_pages(pages, n_select);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, tree_mask, mask_words, window, sinks);
+  if (st != BEAGLE_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, attend_bytes(p.d));
+  if (st != BEAGLE_OK) return st;
+  (void)hipGetLastError();
+  PagedAttnArgs a = attn_of(p);
+  set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);
+  a.lists = pages; a.listed = n_select;
+  a.q = q; a.o = o; a.lse = lse;
+  launch_paged_blocks(p.d.bf16, a, workspace, (hipStream_t)hip_stream);
   return hip_status();
 }
 
@@ -244,23 +350,12 @@ void project(const Dims& d, const void* x, const void* w, void* y, int64_t N, in
 }
 }  // namespace
 
-beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
-    const void* wq, const void* wo, const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words,
-    int32_t window, int32_t sinks, void* y, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  Paged p; beagle_status st = check_paged(desc, cache, true, &p);
-  if (st != BEAGLE_OK) return st;
-  const void* ptrs[] = {x_draft, wq, wo, y, lse};
-  for (const void* q : ptrs) if (!q) return BEAGLE_ERR_NULL;
-  for (const void* q : ptrs) if (!aligned16(q)) return BEAGLE_ERR_ALIGN;
-  st = check_view(slots, n_true, tree_mask, mask_words, window, sinks);
-  if (st != BEAGLE_OK) return st;
+namespace {
+// q = x Wq, attend(q, o), y = o Wo.  `attend` enqueues the attention on a workspace of its own, which stands at w.call.
+template <class Attend>
+void draft_step_run(const Paged& p, const StepWs& w, const void* x_draft, const void* wq, const void* wo, const int32_t* slots, void* y,
+                    char* base, hipStream_t s, Attend attend) {
   const Dims& d = p.d;
-  const StepWs w = draft_layout(d);
-  st = check_workspace(workspace, workspace_bytes, w.total);
-  if (st != BEAGLE_OK) return st;
-  hipStream_t s = (hipStream_t)hip_stream;
-  (void)hipGetLastError();
-  char* base = (char*)workspace;
   const int32_t* at = d.rope_pos;
   if (d.rope && !at) {
     launch_paged_positions(p.c, slots, (int32_t)d.B, (int32_t)d.S, (int32_t*)(base + w.pos), s);
@@ -281,11 +376,96 @@ beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const
       launch_rope(d.bf16, r, s, "draft_rope_q");
     }
   }
-  PagedAttnArgs a = attn_of(p);
-  set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);
-  a.q = base + w.a; a.o = base + w.b; a.lse = lse;
-  launch_paged_attn(d.bf16, a, base + w.call, s);
+  attend(base + w.a, base + w.b);
   project(d, base + w.b, wo, y, d.D, d.HD, base + w.proj, "draft_proj_out", s);
+}
+beagle_status check_states(const void* x_draft, const void* wq, const void* wo, const void* y, const float* lse) {
+  const void* ptrs[] = {x_draft, wq, wo, y, lse};
+  for (const void* q : ptrs) if (!q) return BEAGLE_ERR_NULL;
+  for (const void* q : ptrs) if (!aligned16(q)) return BEAGLE_ERR_ALIGN;
+  return BEAGLE_OK;
+}
+}  // namespace
+
+beagle_status beagle_xattn_draft_step_paged(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words,
+    int32_t window, int32_t sinks, void* y, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, true, &p);
+  if (st != BEAGLE_OK) return st;
+  st = check_states(x_draft, wq, wo, y, lse);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, tree_mask, mask_words, window, sinks);
+  if (st != BEAGLE_OK) return st;
+  const StepWs w = draft_layout(p.d, attend_bytes(p.d));
+  st = check_workspace(workspace, workspace_bytes, w.total);
+  if (st != BEAGLE_OK) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  (void)hipGetLastError();
+  char* base = (char*)workspace;
+  draft_step_run(p, w, x_draft, wq, wo, slots, y, base, s, [&](const void* q, void* o) {
+    PagedAttnArgs a = attn_of(p);
+    set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);
+    a.q = q; a.o = o; a.lse = lse;
+    launch_paged_attn(p.d.bf16, a, base + w.call, s);
+  });
+  return hip_status();
+}
+
+beagle_status beagle_xattn_draft_step_paged_shared(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* group_first, const int32_t* n_shared, int32_t n_groups,
+    const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words, void* y, float* lse, void* workspace, size_t workspace_bytes,
+    void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, true, &p);
+  if (st != BEAGLE_OK) return st;
+  st = check_states(x_draft, wq, wo, y, lse);
+  if (st != BEAGLE_OK) return st;
+  st = check_groups(p.d, group_first, n_shared, n_groups);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, tree_mask, mask_words, 0, 0);
+  if (st != BEAGLE_OK) return st;
+  const StepWs w = draft_layout(p.d, shared_bytes(p.d));
+  st = check_workspace(workspace, workspace_bytes, w.total);
+  if (st != BEAGLE_OK) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  (void)hipGetLastError();
+  char* base = (char*)workspace;
+  draft_step_run(p, w, x_draft, wq, wo, slots, y, base, s, [&](const void* q, void* o) {
+    PagedSharedArgs a = {attn_of(p), group_first, n_shared, n_groups};
+    set_view(a.a, slots, n_true, tree_mask, mask_words, 0, 0);
+    a.a.q = q; a.a.o = o; a.a.lse = lse;
+    launch_paged_shared(p.d.bf16, a, base + w.call, s);
+  });
+  return hip_status();
+}
+
+beagle_status beagle_xattn_draft_step_paged_blocks(const beagle_xattn_desc* desc, const beagle_paged_cache* cache, const void* x_draft,
+    const void* wq, const void* wo, const int32_t* slots, const int32_t* n_true, const uint32_t* tree_mask, int32_t mask_words,
+    const void* bounds, int32_t window, int32_t sinks, int32_t n_select, int32_t* pages, void* y, float* lse,
+    void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Paged p; beagle_status st = check_paged(desc, cache, true, &p);
+  if (st != BEAGLE_OK) return st;
+  st = check_states(x_draft, wq, wo, y, lse);
+  if (st != BEAGLE_OK) return st;
+  if (!bounds) return BEAGLE_ERR_NULL;
+  if (!aligned16(bounds)) return BEAGLE_ERR_ALIGN;
+  st = check_pages(pages, n_select);
+  if (st != BEAGLE_OK) return st;
+  st = check_view(slots, n_true, tree_mask, mask_words, window, sinks);
+  if (st != BEAGLE_OK) return st;
+  const StepWs w = draft_layout(p.d, draft_blocks_bytes(p));
+  st = check_workspace(workspace, workspace_bytes, w.total);
+  if (st != BEAGLE_OK) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  (void)hipGetLastError();
+  char* base = (char*)workspace;
+  draft_step_run(p, w, x_draft, wq, wo, slots, y, base, s, [&](const void* q, void* o) {
+    launch_paged_select(p.d.bf16, select_of(p, q, slots, n_true, bounds, window, sinks, n_select, pages), base + w.call + attend_bytes(p.d), s);
+    PagedAttnArgs a = attn_of(p);
+    set_view(a, slots, n_true, tree_mask, mask_words, window, sinks);
+    a.lists = pages; a.listed = n_select;
+    a.q = q; a.o = o; a.lse = lse;
+    launch_paged_blocks(p.d.bf16, a, base + w.call, s);
+  });
   return hip_status();
 }
 

@@ -27,6 +27,7 @@ struct PagedAttnArgs {
   const int32_t* n_true;                   // [B] or null: every row is a true one
   const uint32_t* tree; int32_t words;     // [B, M, words]
   int32_t window, sinks;                   // window 0: none
+  const int32_t* lists; int32_t listed;    // [B, G, listed]: pages that a kv head sees besides (launch_paged_blocks)
   float* part; float* ml;                  // sums of the parts of entries that several workers share
   int2* parts;                             // [B] first worker of an entry, how many have a part of it
   int32_t target;                          // workers, at most
@@ -34,6 +35,33 @@ struct PagedAttnArgs {
 };
 size_t paged_attn_ws_bytes(int32_t B, int32_t M, int32_t H, int32_t G);
 void launch_paged_attn(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s);
+
+void launch_paged_blocks(bool bf16, PagedAttnArgs a, void* ws, hipStream_t s);     // a.lists; workspace as launch_paged_attn's
+
+// least and greatest value of every channel over the rows of a page
+void launch_paged_bounds(bool bf16, const PagedCache& c, int32_t B, int32_t G, int32_t d, int32_t bound, const int32_t* slots,
+                         const int32_t* first, void* bounds, hipStream_t s);
+
+struct PagedSelectArgs {
+  PagedCache c;
+  int32_t B, M, H, G, d, bound;
+  const void *q, *bounds;                  // [B, M, H, d], [P, G, 2, d]
+  const int32_t *slots, *n_true;           // [B] or null
+  int32_t window, sinks, n_select;
+  int32_t* pages;                          // [B, G, n_select]
+  float* scores; int32_t width;            // [B, G, width]
+};
+size_t paged_select_ws_bytes(const PagedCache& c, int32_t B, int32_t G, int32_t bound);
+void launch_paged_select(bool bf16, PagedSelectArgs a, void* ws, hipStream_t s);
+
+// Entries group_first[g] .. group_first[g + 1] - 1 see the first n_shared[g] rows of the first of them
+struct PagedSharedArgs {
+  PagedAttnArgs a;                         // window 0
+  const int32_t *group_first, *n_shared;   // [groups + 1], [groups]
+  int32_t groups;
+};
+size_t paged_shared_ws_bytes(int32_t B, int32_t M, int32_t H, int32_t G);
+void launch_paged_shared(bool bf16, PagedSharedArgs a, void* ws, hipStream_t s);
 
 struct PagedAppendArgs {
   PagedCache c;

@@ -45,6 +45,48 @@ PAGED_HD bool paged_all_seen(const PagedRows& r, int first, int count) {
   return first + count <= r.nt && (r.window == 0 || first + count <= r.sinks || first >= r.nt - r.window);
 }
 
+// Only some pages of the true rows are seen: those that hold a row below `sinks`, from the one that holds row nt - window on (or where
+// the true rows end), and of those between them the listed ones.  The pages seen count as one sequence: `lead` first ones, `listed` from
+// the list, and the rest, whose numbers are `gap` higher than their places.  n - gap * page rows in all.
+struct PagedPick { int lead, listed, gap; };
+PAGED_HD PagedPick paged_pick(int n, int nt, int window, int sinks, int n_list, int shift) {
+  PagedPick p;
+  const int true_rows = paged_min(paged_max(nt, 0), n);
+  p.lead = (int)(((int64_t)sinks + (1 << shift) - 1) >> shift);
+  const int between = paged_max((paged_max(true_rows - window, 0) >> shift) - p.lead, 0);
+  p.listed = paged_min(between, n_list);
+  p.gap = between - p.listed;
+  return p;
+}
+PAGED_HD PagedRows paged_picked_rows(const PagedPick& p, int n, int nt, int shift) {
+  const int hidden = p.gap << shift;
+  return paged_rows(n - hidden, paged_max(paged_min(paged_max(nt, 0), n) - hidden, 0), 0, 0);
+}
+// page number at place i of the pages seen; -1 where the list names no page that stands between the others and behind the one before it
+PAGED_HD int paged_picked_page(const PagedPick& p, const int32_t* list, const int32_t* table, int i, int n_pages) {
+  const int at = i - p.lead;
+  const bool from_list = at >= 0 && at < p.listed;
+  int col = i + (at >= p.listed ? p.gap : 0);
+  if (from_list) {
+    col = list[at];
+    const int before = at > 0 ? list[at - 1] : -1;
+    if (col <= before || col < p.lead || col >= p.lead + p.listed + p.gap) return -1;
+  }
+  const int number = table[col];
+  return (unsigned)number < (unsigned)n_pages ? number : -1;
+}
+
+// The rows of an entry from row `from` of its true ones on
+PAGED_HD PagedRows paged_rows_from(int n, int nt, int from) {
+  PagedRows r;
+  r.n = n; r.nt = paged_min(paged_max(nt, 0), n); r.sinks = r.lead = 0;
+  from = paged_min(paged_max(from, 0), r.nt);
+  r.window = from < r.nt ? r.nt - from : -1;             // (-1: none of the true ones)
+  r.skip = from / PAGED_BLOCK;
+  r.blocks = paged_max((n + PAGED_BLOCK - 1) / PAGED_BLOCK - r.skip, 0);
+  return r;
+}
+
 // Workers: the blocks of all entries in a row (`all` of them, every entry at least one), cut into equal runs, one for each; an entry of up to
 // four blocks is not cut but goes whole to the worker that has its first block.  A worker so has at most two entries in part, its first
 // and its last.  Where each entry can be cut for itself into runs of four blocks (or of eight, if an equal share is three blocks at least), with
