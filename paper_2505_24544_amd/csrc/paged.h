@@ -49,7 +49,8 @@ struct PagedSelectArgs {
   const int32_t *slots, *n_true;           // [B] or null
   int32_t window, sinks, n_select;
   int32_t* pages;                          // [B, G, n_select]
-  float* scores; int32_t width;            // [B, G, width]
+  uint32_t* scores; int32_t width;         // [B, G, width]: floats, then keys
+  void* extents;                           // what they may be off by, the least and the greatest, chunk by chunk and wave by wave
 };
 size_t paged_select_ws_bytes(const PagedCache& c, int32_t B, int32_t G, int32_t bound);
 void launch_paged_select(bool bf16, PagedSelectArgs a, void* ws, hipStream_t s);

@@ -59,6 +59,17 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedCache c, int G, 
 }
 
 // ------------------------------------------------------------------ selection
+// The order of the pages is that of sums in 64 bits, rounded to float; but those are needed only where a page's place is in doubt.  The scores
+// are first taken from matrix instructions, sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c, and are then off by at most E:
+//   32 additions of a piece's products, each off by at most 2^-23 of the magnitudes |q_c x_c| of the piece, and 4 of pieces, by 2^-24 of all,
+//   less than 1.25 * 2^-18 of sum_c |q_c x_c| <= |q|_1 max_c |x_c| together; inputs and sums below 2^-126 may count as zero.
+// With t the n_select-th largest of them, the true one is within E of t: a page above t + 2 E is picked, one below t - 2 E is not, and of those
+// between (most often only the one that t comes from) the true scores are taken where they are more than are still to be picked.
+// Infinities and what is no number make E infinite, and all scores true ones.
+constexpr int SELECT_THREADS = 512, SELECT_WAVES = SELECT_THREADS / 64;
+constexpr int SELECT_HELD = 8192;          // scores that a workgroup holds
+constexpr int SELECT_LISTED = 240;         // pages in doubt that are kept in a list (times 2^24 query rows: 32 bits)
+
 struct Span { int lead, count; const int32_t* table; };
 // the pages that an entry's selection is made of: `count` of them from `lead` on
 __device__ __forceinline__ Span span_of(const PagedSelectArgs& a, int b) {
@@ -68,139 +79,460 @@ __device__ __forceinline__ Span span_of(const PagedSelectArgs& a, int b) {
   return {p.lead, p.listed + p.gap, a.c.table + (int64_t)max(slot, 0) * a.c.W};
 }
 
-// Scores.  Sixteen lanes take a page; what they add up is exact in 64 bits but for the last of them (a product of two bf16 has 16 bits, of two
-// floats 48), so that the order of the pages is that of the definition.  It is rounded to float once.
-constexpr int SELECT_PAGES = 64, SELECT_ROWS = 16;           // pages of a workgroup, query rows that are held at a time
+template <bool BF16> struct Rows {         // sixteen rows as the matrix instructions take them: lane % 16 is the row, lane / 16 the piece of 16 bytes
+  static constexpr int E = BF16 ? 2 : 4, NJ = BF16 ? 4 : 8;
+  u32x4 x[NJ];
+  __device__ __forceinline__ void load(addr_t row, int d, bool there) {
+    const int g4 = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) x[j] = load16(there && (BF16 || (4 * j + g4) * 16 < d * E) ? row + (4 * j + g4) * 16 : (addr_t)zero_row);
+  }
+  // the positive, or the negative, values; the others as zero
+  __device__ __forceinline__ Rows part(bool negative) const {
+    Rows r;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t v = x[j][i];          // (a bit cast of the element itself takes the first one's bits)
+        uint32_t sign;
+        if constexpr (BF16) {
+          typedef short i16x2 __attribute__((ext_vector_type(2)));
+          sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, v) >> 15);
+        } else {
+          sign = (uint32_t)((int)v >> 31);
+        }
+        r.x[j][i] = v & (negative ? sign : ~sign);
+      }
+    return r;
+  }
+  // the largest magnitude of this lane's values, as bits: infinities are above all numbers, what is no number above those
+  __device__ __forceinline__ uint32_t most() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, x[j][i] & 0x7fff7fffu)));
+        else m = max(m, x[j][i] & 0x7fffffffu);
+      }
+    return BF16 ? max(m >> 16, m & 0xffffu) << 16 : m;
+  }
+  // the sum of their magnitudes, as bits
+  __device__ __forceinline__ uint32_t sum() const {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) s += fabsf(__uint_as_float(x[j][i] << 16)) + fabsf(__uint_as_float(x[j][i] & 0xffff0000u));
+        else s += fabsf(__uint_as_float(x[j][i]));
+      }
+    return __float_as_uint(s) & 0x7fffffffu;
+  }
+};
+// (pieces of 32 channels, floats of 16, add up by themselves: less rounding, and no instruction waits for another's sum)
+template <bool BF16> __device__ __forceinline__ f32x4 product(const Rows<BF16>& a, const Rows<BF16>& b) {
+  f32x4 s[Rows<BF16>::NJ];
+#pragma unroll
+  for (int j = 0; j < Rows<BF16>::NJ; ++j) {
+    s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (BF16) s[j] = mfma_bf16(a.x[j], b.x[j], s[j]);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j] = mfma_f32(__uint_as_float(a.x[j][e]), __uint_as_float(b.x[j][e]), s[j]);
+  }
+#pragma unroll
+  for (int n = Rows<BF16>::NJ / 2; n > 0; n /= 2)
+#pragma unroll
+    for (int j = 0; j < n; ++j) s[j] += s[j + n];
+  return s[0];
+}
+__device__ __forceinline__ float as_float(uint32_t v) { return __uint_as_float(v); }
+template <int CONTROL> __device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xf, 0xf, false);
+}
+// over the first n of the sixteen lanes of a row, the four rows, all lanes (in registers: steps through LDS take 60 ns each)
+template <class F> __device__ __forceinline__ uint32_t over_row(uint32_t v, F f, int n = 16) {
+  if (n > 1) v = f(v, moved<0xb1>(v));     // neighbours
+  if (n > 2) v = f(v, moved<0x4e>(v));     // pairs
+  if (n > 4) {
+    v = f(v, moved<0x124>(v));             // turned by 4, by 8
+    v = f(v, moved<0x128>(v));
+  }
+  return v;
+}
+template <class F> __device__ __forceinline__ uint32_t over_rows(uint32_t v, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(b[0], b[1]);
+}
+template <class F> __device__ __forceinline__ uint32_t over_all(uint32_t v, F f) { return over_rows(over_row(v, f), f); }
+struct MaxBits { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
+struct MaxOf { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return __float_as_uint(fmaxf(as_float(a), as_float(b))); } };
+struct MinOf { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return __float_as_uint(fminf(as_float(a), as_float(b))); } };
+struct SumOf { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return __float_as_uint(as_float(a) + as_float(b)); } };
+
+// what the scores of some pages may be off by, and the least (but -infinity) and the greatest of them
+struct Extent { float off, least, most; };
+
+// Scores of pages [from, to) of the span by matrix instructions, sixteen at a time to each wave.  Returns the wave's share of their extent.
+// (Loops that are not unrolled: all of this runs once or a few times, and instructions that come from memory take longer than they run.)
 template <bool BF16>
-__global__ __launch_bounds__(256) void paged_score_kernel(PagedSelectArgs a, int64_t units, int chunks) {
-  constexpr int E = BF16 ? 2 : 4, N = 8;
-  __shared__ float sq[SELECT_ROWS][128];
+__device__ __forceinline__ Extent score_pages(const PagedSelectArgs& a, const int32_t* table, int b, int g, int from, int to, uint32_t* out) {
+  constexpr int E = BF16 ? 2 : 4, STEP = SELECT_WAVES * 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int rep = a.H / a.G, R = a.M * rep;
-  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int chunk = (int)(u % chunks);
-    const int64_t bg = u / chunks;
-    const int b = (int)(bg / a.G), g = (int)(bg % a.G);
-    const Span span = span_of(a, b);
-    if (span.count <= a.n_select || chunk * SELECT_PAGES >= span.count) continue;      // (the same in all lanes)
-    constexpr int EACH = SELECT_PAGES / 16;
-    float lo[EACH][N], hi[EACH][N], best[EACH];
+  auto query = [&](int first) {
+    const int r = first + l16;
+    Rows<BF16> q;
+    q.load((addr_t)a.q + (((int64_t)b * a.M + r / rep) * a.H + g * rep + r % rep) * a.d * E, a.d, r < R);
+    return q;
+  };
+  const int first = from + wave * 16;
+  auto number_of = [&](int i0) { return i0 + l16 < to ? table[i0 + l16] : -1; };
+  int page = number_of(first);
+  Rows<BF16> q = query(0), plus = q.part(false), minus = q.part(true);
+  uint32_t most = 0, sum = 0;
+  Extent x = {0.f, INFINITY, -INFINITY};
+  struct Pages { Rows<BF16> lo, hi; bool there; };
+  auto request = [&](Pages& p, int i0) BEAGLE_INLINE_LAMBDA {
+    p.there = (unsigned)page < (unsigned)a.c.P;
+    const addr_t at = (addr_t)a.bounds + ((int64_t)(p.there ? page : 0) * a.G + g) * 2 * a.d * E;
+    page = number_of(i0 + STEP);
+    p.lo.load(at, a.d, p.there);
+    p.hi.load(at + a.d * E, a.d, p.there);
+  };
+  auto score = [&](const Pages& p, int i0) BEAGLE_INLINE_LAMBDA {
+    uint32_t best[4];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int i = chunk * SELECT_PAGES + e * 16 + group;
-      const int page = i < span.count ? span.table[span.lead + i] : -1;
-      const bool there = (unsigned)page < (unsigned)a.c.P;
-      best[e] = -INFINITY;
-      const addr_t src = (addr_t)a.bounds + ((int64_t)(there ? page : 0) * a.G + g) * 2 * a.d * E;
+    for (int e = 0; e < 4; ++e) best[e] = __float_as_uint(-INFINITY);
+#pragma unroll 1
+    for (int t = 0; t < R; t += 16) {
+      if (R > 16) { q = query(t); plus = q.part(false); minus = q.part(true); }
+      if (i0 == first) sum = max(sum, q.sum());              // (while the bounds are on their way)
+      const f32x4 s = product(p.lo, minus) + product(p.hi, plus);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int ch = lane * N + i;
-          float v = 0.f;
-          if (ch < a.d) {
-            if constexpr (BF16) v = bf16_to_f32(((const bf16_t*)src)[h * a.d + ch]);
-            else v = ((const float*)src)[h * a.d + ch];
-          }
-          (h ? hi : lo)[e][i] = v;
-        }
-      if (!there) best[e] = NAN;
+      for (int e = 0; e < 4; ++e)                            // page 4 g4 + e, query row l16
+        if (t + l16 < R) best[e] = MaxOf()(best[e], __float_as_uint(s[e]));
     }
-    for (int r0 = 0; r0 < R; r0 += SELECT_ROWS) {
+    most = max(most, max(p.lo.most(), p.hi.most()));
+    const unsigned long long here = __ballot(p.there);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * g4 + e;
+      const float v = here >> i & 1 ? as_float(over_row(best[e], MaxOf(), R)) : -INFINITY;
+      if (l16 == 0 && i0 + i < to) out[i0 + i] = __float_as_uint(v);
+      x.most = fmaxf(x.most, v);
+      x.least = fminf(x.least, v == -INFINITY ? INFINITY : v);
+    }
+  };
+  // (the next sixteen pages travel meanwhile; of floats there is no room for them)
+  Pages now, next;
+  if (BF16 && first < to) request(now, first);
+#pragma unroll 1
+  for (int i0 = first; i0 < to; i0 += STEP) {
+    if constexpr (BF16) {
+      if (i0 + STEP < to) request(next, i0 + STEP);
+    } else {
+      request(now, i0);
+    }
+    score(now, i0);
+    if constexpr (BF16) now = next;
+  }
+  // (a row's lanes have their largest parts of all tiles: together no less than any query's)
+  const float total = as_float(over_row(over_rows(sum, SumOf()), MaxBits())), magnitude = as_float(over_all(most, MaxBits()));
+  const float size = 4.f * total * magnitude;                // (finite: and so is every sum on the way)
+  x.off = 1.01f * (0x1.4p-20f * size + 0x1p-117f * (total + magnitude + 1.f));
+  if (!(size < INFINITY && x.off < INFINITY)) x.off = INFINITY;
+  x.least = as_float(over_rows(__float_as_uint(x.least), MinOf()));
+  x.most = as_float(over_rows(__float_as_uint(x.most), MaxOf()));
+  return x;
+}
+
+// What this workgroup has written to memory, its waves read behind this: a barrier alone does not wait for stores, nor empty the vector cache of
+// what it held before.
+__device__ __forceinline__ void hand_over() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+}
+
+// larger scores have larger keys; 0 is no score's, and neither is the largest key
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+
+struct PickShared {
+  uint32_t count[256], state[2];
+  int sure, listed, list[SELECT_LISTED];
+  uint32_t best[SELECT_LISTED];
+  int found[SELECT_WAVES];
+  Extent x[SELECT_WAVES];
+};
+
+// Counts of a value from 0 to 255 of each of n elements (above: not counted), and which value the want-th largest has: state[0]; state[1] of the
+// elements with it are among the want largest.
+template <class Value>
+__device__ __forceinline__ void value_of(PickShared& sh, int n, uint32_t want, Value value) {
+  const int tid = threadIdx.x;
+  if (tid < 256) sh.count[tid] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int i = tid; i < n; i += SELECT_THREADS) {
+    const uint32_t v = value(i);
+    if (v < 256) atomicAdd(&sh.count[v], 1u);
+  }
+  __syncthreads();
+  if (tid < 64) {                                            // from the largest down: four to a lane
+    const u32x4 c = *(const u32x4*)&sh.count[252 - 4 * tid];
+    const uint32_t sum = c[0] + c[1] + c[2] + c[3];
+    uint32_t before = (uint32_t)sum_upto((int)sum) - sum;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      if (before < want && want <= before + c[i]) { sh.state[0] = 252 - 4 * tid + i; sh.state[1] = want - before; }
+      before += c[i];
+    }
+  }
+  __syncthreads();
+}
+
+// The want-th largest key, eight bits at a time.  `want` becomes how many of the keys equal to it are among them.
+__device__ __forceinline__ uint32_t largest_key(PickShared& sh, const uint32_t* keys, int n, uint32_t& want) {
+  uint32_t prefix = 0;
+#pragma unroll 1
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    value_of(sh, n, want, [&](int i) {
+      const uint32_t k = keys[i];
+      return shift == 24 || k >> (shift + 8) == prefix ? k >> shift & 255 : 256u;
+    });
+    prefix = prefix << 8 | sh.state[0];
+    want = sh.state[1];
+    __syncthreads();
+  }
+  return prefix;
+}
+
+// <q_r, the bounds> for page i of the span and one query row in 64 bits, by sixteen lanes; -infinity where there is no such page
+template <bool BF16>
+__device__ __forceinline__ float true_score(const PagedSelectArgs& a, const int32_t* table, int b, int g, int i, int r) {
+  constexpr int E = BF16 ? 2 : 4;
+  const int lane = threadIdx.x & 15, rep = a.H / a.G;
+  const int page = table[i];
+  const bool there = (unsigned)page < (unsigned)a.c.P;
+  const addr_t at_q = (addr_t)a.q + (((int64_t)b * a.M + r / rep) * a.H + g * rep + r % rep) * a.d * E;
+  const addr_t at_lo = (addr_t)a.bounds + ((int64_t)(there ? page : 0) * a.G + g) * 2 * a.d * E, at_hi = at_lo + a.d * E;
+  double s = 0.0;
+#pragma unroll
+  for (int h = 0; h < (BF16 ? 1 : 2); ++h) {                 // channels 8 lane .., floats 4 lane + 64 h ..
+    const int byte = 16 * lane + 256 * h;
+    const bool in = byte < a.d * E;
+    const u32x4 q = load16(in ? at_q + byte : (addr_t)zero_row), lo = load16(in ? at_lo + byte : (addr_t)zero_row),
+                hi = load16(in ? at_hi + byte : (addr_t)zero_row);
+#pragma unroll
+    for (int e = 0; e < 16 / E; ++e) {
+      auto value = [&](const u32x4& x) { return BF16 ? as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16) : as_float(x[e % 4]); };
+      const float v = value(q);
+      if (v > 0.f) s = fma((double)v, (double)value(hi), s);
+      else if (v < 0.f) s = fma((double)v, (double)value(lo), s);
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < 16; k *= 2) s += __shfl_xor(s, k);
+  return there ? (float)s : -INFINITY;
+}
+
+// An entry's and head's pages from their scores, whose extent the waves (or, in memory, the chunks' waves) have left; the scores are overwritten.
+template <bool BF16, bool MEMORY>
+__device__ __forceinline__ void pick_pages(const PagedSelectArgs& a, PickShared& sh, const Span& span, int b, int g, uint32_t* scores, Extent x,
+                                           int32_t* out) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = span.count, R = a.M * (a.H / a.G);
+  const int32_t* table = span.table + span.lead;
+  if (lane == 0) sh.x[wave] = x;
+  if (tid == 0) sh.sure = sh.listed = 0;
+  if constexpr (MEMORY) hand_over();
+  else __syncthreads();
+  x = sh.x[lane % SELECT_WAVES];
+  const float off = as_float(over_all(__float_as_uint(x.off), MaxBits()));
+  // Where the n_select-th largest score is: in one of 256 parts between the least and the greatest, and of that part in one of 256.  (What
+  // rounds here is far below off / 8.  -infinity counts to the lowest part; where all are alike, nothing is known.)
+  const float least = as_float(over_all(__float_as_uint(x.least), MinOf())), most = as_float(over_all(__float_as_uint(x.most), MaxOf()));
+  float low = -INFINITY, top = most;
+  if (most - least > off && most - least < INFINITY) {
+    auto part_of = [](float v, float base, float per) { return (uint32_t)(int)fminf(fmaxf((v - base) * per, 0.f), 255.f); };
+    const float width = (most - least) * 0x1p-8f, per = 1.f / width;
+    value_of(sh, n, a.n_select, [&](int i) { return part_of(as_float(scores[i]), least, per); });
+    const uint32_t part = sh.state[0], want = sh.state[1];
+    const float base = least + part * width;
+    if (part > 0) low = base;
+    if (part < 255) top = base + width;
+    __syncthreads();
+    if (width > off) {
+      const float narrow = width * 0x1p-8f, finer = 1.f / narrow;
+      value_of(sh, n, want, [&](int i) {
+        const float v = as_float(scores[i]);
+        return part_of(v, least, per) == part ? part_of(v, base, finer) : 256u;
+      });
+      const uint32_t k = sh.state[0];
+      if (k > 0) low = base + k * narrow;
+      if (k < 255) top = base + (k + 1) * narrow;
+    }
+  }
+  top += 2.125f * off; low -= 2.125f * off;
+
+  constexpr uint32_t PICKED = 0xffffffffu;
+  auto meet = [&] { if constexpr (MEMORY) hand_over(); else __syncthreads(); };
+  auto doubtful = [&](float v) { return !(v > top) && !(v < low); };
+  auto list = [&](int i) {
+    const int at = atomicAdd(&sh.listed, 1);
+    if (at < SELECT_LISTED) { sh.list[at] = i; sh.best[at] = key_of(-INFINITY); }
+  };
+  auto take_true_scores = [&](int listed) {                  // a page of the list and a query row to sixteen lanes
+#pragma unroll 1
+    for (uint32_t t = tid >> 4; t < (uint32_t)listed * R; t += SELECT_THREADS / 16) {
+      const int l = (int)(t / (uint32_t)R);
+      const float v = true_score<BF16>(a, table, b, g, sh.list[l], (int)(t - (uint32_t)l * R));
+      if ((tid & 15) == 0 && v == v) atomicMax(&sh.best[l], key_of(v));
+    }
+    __syncthreads();
+  };
+#pragma unroll 1
+  for (int i = tid; i < n; i += SELECT_THREADS) {
+    const float v = as_float(scores[i]);
+    if (v > top) atomicAdd(&sh.sure, 1);
+    if (doubtful(v)) list(i);
+  }
+  __syncthreads();
+  const int listed = sh.listed, wanted = a.n_select - sh.sure;      // in doubt, and how many of them are picked
+  const bool all = listed == wanted;
+  uint32_t last = PICKED - 1, ties = 0;                      // what is above `last` is picked, and the first `ties` of what equals it
+  if (all || listed <= SELECT_LISTED) {
+    if (!all) take_true_scores(listed);
+#pragma unroll 1
+    for (int i = tid; i < n; i += SELECT_THREADS) {
+      const float v = as_float(scores[i]);
+      if (all || !doubtful(v)) scores[i] = v > top || doubtful(v) ? PICKED : 0u;
+    }
+    if (!all && tid < listed) {                              // how many of the others come before it
+      const uint32_t mine = sh.best[tid];
+      const int at = sh.list[tid];
+      int before = 0;
+#pragma unroll 1
+      for (int l = 0; l < listed; ++l) before += sh.best[l] > mine || (sh.best[l] == mine && sh.list[l] < at);
+      scores[at] = before < wanted ? PICKED : 0u;
+    }
+    meet();
+  } else {
+    // too many for a list: piece by piece they take their true scores, and the last key is looked for among all
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += SELECT_LISTED) {
+      const int i = i0 + tid;
+      if (tid == 0) sh.listed = 0;
       __syncthreads();
-      for (int i = threadIdx.x; i < SELECT_ROWS * 128; i += 256) {
-        const int r = r0 + i / 128, ch = i % 128;
-        float v = 0.f;
-        if (r < R && ch < a.d) {
-          const int64_t at = (((int64_t)b * a.M + r / rep) * a.H + g * rep + r % rep) * a.d + ch;
-          v = BF16 ? bf16_to_f32(((const bf16_t*)a.q)[at]) : ((const float*)a.q)[at];
-        }
-        sq[i / 128][ch] = v;
+      if (tid < SELECT_LISTED && i < n) {
+        const float v = as_float(scores[i]);
+        if (doubtful(v)) list(i);
+        else scores[i] = v > top ? PICKED : 0u;
       }
       __syncthreads();
-      for (int r = 0; r < min(SELECT_ROWS, R - r0); ++r) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-          double s = 0.0;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float q = sq[r][lane * N + i], x = q > 0.f ? hi[e][i] : q < 0.f ? lo[e][i] : 0.f;
-            s = fma((double)(q == q ? q : 0.f), (double)x, s);
-          }
-#pragma unroll
-          for (int i = 1; i < 16; i *= 2) s += __shfl_xor(s, i);
-          best[e] = isnan(best[e]) ? best[e] : fmaxf(best[e], (float)s);
-        }
-      }
+      const int here = sh.listed;
+      take_true_scores(here);
+      if (tid < here) scores[sh.list[tid]] = sh.best[tid];
     }
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int i = chunk * SELECT_PAGES + e * 16 + group;
-      if (lane == 0 && i < span.count) a.scores[bg * a.width + i] = isnan(best[e]) ? -INFINITY : best[e] + 0.f;
-    }
+    meet();
+    ties = a.n_select;
+    last = largest_key(sh, scores, n, ties);
+  }
+  int written = 0, taken = 0;                                // of the pages before: picked, and those with the last key
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += SELECT_THREADS) {
+    const bool here = i0 + tid < n;
+    const uint32_t k = here ? scores[i0 + tid] : 0;
+    const unsigned long long gt = __ballot(here && k > last), eq = __ballot(here && k == last), lower = (1ull << lane) - 1;
+    if (lane == 0) sh.found[wave] = __popcll(gt) | __popcll(eq) << 16;
+    __syncthreads();
+    const int found = lane < SELECT_WAVES ? sh.found[lane] : 0, level = found >> 16, upto = sum_upto(level);       // a wave to a lane
+    const int more = (found & 0xffff) + min(level, max((int)ties - taken - (upto - level), 0)), sum = sum_upto(more);
+    auto of = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+    const int before = taken + of(upto - level, wave), tie = before + __popcll(eq & lower);
+    const int at = written + of(sum - more, wave) + __popcll(gt & lower) + max(min(tie, (int)ties) - min(before, (int)ties), 0);
+    if (here && (k > last || (k == last && tie < (int)ties))) out[at] = span.lead + i0 + tid;
+    written += of(sum, SELECT_WAVES - 1);
+    taken += of(upto, SELECT_WAVES - 1);
     __syncthreads();
   }
 }
 
-// larger scores have larger keys
-__device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+// every page is picked
+__device__ __forceinline__ bool picks_all(const PagedSelectArgs& a, const Span& span, int32_t* out) {
+  if (span.count > a.n_select) return false;
+  for (int i = threadIdx.x; i < a.n_select; i += SELECT_THREADS) out[i] = i < span.count ? span.lead + i : -1;
+  return true;
 }
 
-// The n_select largest of an entry's and head's scores: the key of the last of them is found eight bits at a time, then the pages are
-// written in order, of those with that key the first ones.
-__global__ __launch_bounds__(256) void paged_pick_kernel(PagedSelectArgs a) {
-  __shared__ uint32_t count[256], state[2];
-  __shared__ int above[4], level[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int64_t bg = blockIdx.x; bg < (int64_t)a.B * a.G; bg += gridDim.x) {
-    const Span span = span_of(a, (int)(bg / a.G));
+// One workgroup for an entry and head: scores in LDS, and the pages from them.
+template <bool BF16>
+__global__ __launch_bounds__(SELECT_THREADS) void paged_select_kernel(PagedSelectArgs a) {
+  __shared__ PickShared sh;
+  __shared__ uint32_t scores[SELECT_HELD];
+  // Workgroups go round the chip's eight dies.  Heads g, g + 8, .. of one entry on one die would ask for addresses that are alike in their
+  // lowest 4 KB, two of the sixteen channels of the die's cache; so each has its heads one behind the other.
+  const uint32_t all = (uint32_t)a.B * a.G, each = (all + 7) / 8;
+  for (uint32_t i = blockIdx.x; i < 8 * each; i += gridDim.x) {
+    const uint32_t bg = i % 8 * each + i / 8;
+    if (bg >= all) continue;
+    const int b = (int)(bg / (uint32_t)a.G), g = (int)(bg % (uint32_t)a.G);
+    const Span span = span_of(a, b);
+    int32_t* out = a.pages + (int64_t)bg * a.n_select;
+    if (picks_all(a, span, out)) continue;
+    const Extent x = score_pages<BF16>(a, span.table + span.lead, b, g, 0, span.count, scores);
+    pick_pages<BF16, false>(a, sh, span, b, g, scores, x, out);
+  }
+}
+
+// Few entries and heads of many pages: scores by as many workgroups as fill the chip, in memory, then the pages.
+constexpr int SELECT_CHUNK = 16 * SELECT_WAVES;
+template <bool BF16>
+__global__ __launch_bounds__(SELECT_THREADS) void paged_score_kernel(PagedSelectArgs a, int chunks) {
+  const int b = blockIdx.z;
+  const Span span = span_of(a, b);
+  for (int g = blockIdx.y; g < a.G; g += gridDim.y)
+    for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+      const int64_t bg = (int64_t)b * a.G + g;
+      const int from = chunk * SELECT_CHUNK, to = min(from + SELECT_CHUNK, span.count);
+      Extent x = {0.f, INFINITY, -INFINITY};
+      if (span.count > a.n_select && from < to) x = score_pages<BF16>(a, span.table + span.lead, b, g, from, to, a.scores + bg * a.width);
+      if ((threadIdx.x & 63) == 0) ((Extent*)a.extents)[(bg * chunks + chunk) * SELECT_WAVES + (threadIdx.x >> 6)] = x;
+    }
+}
+template <bool BF16>
+__global__ __launch_bounds__(SELECT_THREADS) void paged_pick_kernel(PagedSelectArgs a, int chunks) {
+  __shared__ PickShared sh;
+  __shared__ uint32_t held[SELECT_HELD];
+  const int b = blockIdx.y;
+  const Span span = span_of(a, b);
+  for (int g = blockIdx.x; g < a.G; g += gridDim.x) {
+    const int64_t bg = (int64_t)b * a.G + g;
     int32_t* out = a.pages + bg * a.n_select;
-    if (span.count <= a.n_select) {
-      for (int i = tid; i < a.n_select; i += 256) out[i] = i < span.count ? span.lead + i : -1;
+    if (picks_all(a, span, out)) continue;
+    Extent x = {0.f, INFINITY, -INFINITY};
+    for (int i = threadIdx.x; i < chunks * SELECT_WAVES; i += SELECT_THREADS) {
+      const Extent y = ((const Extent*)a.extents)[bg * chunks * SELECT_WAVES + i];
+      x = Extent{fmaxf(x.off, y.off), fminf(x.least, y.least), fmaxf(x.most, y.most)};
+    }
+    x.off = as_float(over_all(__float_as_uint(x.off), MaxBits()));
+    x.least = as_float(over_all(__float_as_uint(x.least), MinOf()));
+    x.most = as_float(over_all(__float_as_uint(x.most), MaxOf()));
+    uint32_t* scores = a.scores + bg * a.width;
+    if (span.count > SELECT_HELD) {
+      pick_pages<BF16, true>(a, sh, span, b, g, scores, x, out);
       continue;
     }
-    const float* scores = a.scores + bg * a.width;
-    uint32_t prefix = 0, want = a.n_select;                  // keys with these leading bits; how many of them are picked
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      count[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < span.count; i += 256) {
-        const uint32_t k = key_of(scores[i]);
-        if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&count[k >> shift & 255], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {                                       // from the largest bin down: four bins to a lane
-        uint32_t c[4], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { c[i] = count[255 - 4 * lane - i]; sum += c[i]; }
-        uint32_t before = (uint32_t)sum_upto((int)sum) - sum;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < want && want <= before + c[i]) { state[0] = prefix << 8 | (uint32_t)(255 - 4 * lane - i); state[1] = want - before; }
-          before += c[i];
-        }
-      }
-      __syncthreads();
-      prefix = state[0]; want = state[1];
-      __syncthreads();
-    }
-    int written = 0, taken = 0;                              // of the pages before: picked, and those of them with the last key
-    for (int i0 = 0; i0 < span.count; i0 += 256) {
-      const uint32_t k = i0 + tid < span.count ? key_of(scores[i0 + tid]) : 0;
-      const bool in = i0 + tid < span.count;
-      const unsigned long long gt = __ballot(in && k > prefix), eq = __ballot(in && k == prefix), lower = (1ull << lane) - 1;
-      if (lane == 0) { above[wave] = __popcll(gt); level[wave] = __popcll(eq); }
-      __syncthreads();
-      int ties = taken, at = written;
-      for (int w = 0; w < wave; ++w) { at += above[w] + min(level[w], max((int)want - ties, 0)); ties += level[w]; }
-      const int tie = ties + __popcll(eq & lower);
-      at += __popcll(gt & lower) + max(min(tie, (int)want) - min(ties, (int)want), 0);
-      if (in && (k > prefix || (k == prefix && tie < (int)want))) out[at] = span.lead + i0 + tid;
-      for (int w = 0; w < 4; ++w) { written += above[w] + min(level[w], max((int)want - taken, 0)); taken += level[w]; }
-      __syncthreads();
-    }
+    for (int i = threadIdx.x; i < span.count; i += SELECT_THREADS) held[i] = scores[i];
+    pick_pages<BF16, false>(a, sh, span, b, g, held, x, out);
   }
 }
 
@@ -223,24 +555,38 @@ static int32_t select_width(const PagedCache& c, int32_t bound) {
   const int32_t pages = bound >> c.shift;
   return pages < 1 ? 1 : pages < c.W ? pages : c.W;
 }
+static int select_chunks(int32_t width) { return (width + SELECT_CHUNK - 1) / SELECT_CHUNK; }
 size_t paged_select_ws_bytes(const PagedCache& c, int32_t B, int32_t G, int32_t bound) {
-  return (size_t)B * (size_t)G * (size_t)select_width(c, bound) * sizeof(float);
+  const int32_t width = select_width(c, bound);
+  return (size_t)B * (size_t)G * ((size_t)width * sizeof(uint32_t) + (size_t)select_chunks(width) * SELECT_WAVES * sizeof(Extent));
 }
 
 void launch_paged_select(bool bf16, PagedSelectArgs a, void* ws, hipStream_t s) {
-  a.scores = (float*)ws;
   a.width = select_width(a.c, a.bound);
-  if (a.width > a.n_select) {                                // (otherwise every page is picked)
+  a.scores = (uint32_t*)ws;
+  a.extents = a.scores + (size_t)a.B * a.G * a.width;
+  const int64_t heads = (int64_t)a.B * a.G;
+  const int chunks = select_chunks(a.width);
+  auto most = [](int64_t n, int64_t limit) { return (unsigned)(n < limit ? n : limit); };
+  const dim3 each(most(a.G, 4096), (unsigned)a.B), wg(SELECT_THREADS);
+  // One launch, a workgroup for each entry and head, or two, the first on the whole chip.  Us, one / two launches (1 query, 4 where said): 8 heads of
+  // 500 pages 14.7 / 11.8, of 2000 38.5 / 15.6, 32 heads of 187 pages 10.4 / 12.0, of 2000 38.9 / 22.6, 80 heads of 2000 (4 queries) 40.2 / 37.2, 96
+  // 40.2 / 44.1, 120 39.7 / 50.0, 256 of up to 304 14.4 / 24.0.
+  if (a.width <= SELECT_HELD && heads < (1 << 30) && (heads >= 96 || a.width <= 256)) {
+    ProfScope ps("paged_select", s);
+    if (bf16) hipLaunchKernelGGL((paged_select_kernel<true>), dim3(most((heads + 7) / 8 * 8, 65536)), wg, 0, s, a);
+    else hipLaunchKernelGGL((paged_select_kernel<false>), dim3(most((heads + 7) / 8 * 8, 65536)), wg, 0, s, a);
+    return;
+  }
+  {
     ProfScope ps("paged_score", s);
-    const int chunks = (a.width + SELECT_PAGES - 1) / SELECT_PAGES;
-    const int64_t units = (int64_t)a.B * a.G * chunks;
-    const dim3 grid((unsigned)(units < 8192 ? units : 8192));
-    if (bf16) hipLaunchKernelGGL((paged_score_kernel<true>), grid, dim3(256), 0, s, a, units, chunks);
-    else hipLaunchKernelGGL((paged_score_kernel<false>), grid, dim3(256), 0, s, a, units, chunks);
+    const dim3 all(most(chunks, 1024), most(a.G, 256), (unsigned)a.B);
+    if (bf16) hipLaunchKernelGGL((paged_score_kernel<true>), all, wg, 0, s, a, chunks);
+    else hipLaunchKernelGGL((paged_score_kernel<false>), all, wg, 0, s, a, chunks);
   }
   ProfScope ps("paged_pick", s);
-  const int64_t heads = (int64_t)a.B * a.G;
-  hipLaunchKernelGGL(paged_pick_kernel, dim3((unsigned)(heads < 65536 ? heads : 65536)), dim3(256), 0, s, a);
+  if (bf16) hipLaunchKernelGGL((paged_pick_kernel<true>), each, wg, 0, s, a, chunks);
+  else hipLaunchKernelGGL((paged_pick_kernel<false>), each, wg, 0, s, a, chunks);
 }
 
 }  // namespace beagle
