@@ -4,15 +4,18 @@
 //   over rows P (common) and T (own):  m = max(m_P, m_T),  l = l_P 2^(m_P - m) + l_T 2^(m_T - m),  o = (o_P 2^(m_P - m) + o_T 2^(m_T - m)) / l
 //
 // Three launches.  The first, one workgroup, divides the work into units: some blocks of 32 rows for a few tiles of 16 query rows, of a
-// group's common rows or of an entry's own.  The second computes units, the third joins every query row's parts in the order of the rows.
+// group's common rows or of an entry's own.  In the second as many workgroups as fit take units, those that are done take more; each unit
+// leaves its sums in the workspace, in a place of its own.  The third joins every query row's sums in the order of the rows.
 #include "paged_attend.h"
+#include "attn_tiles.h"
 
 namespace beagle {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-// What a block of 32 rows costs a workgroup: common rows for one block of query rows, own rows.
-constexpr int COST_COMMON = 1, COST_OWN = 2;
+// What a block of 32 rows takes a workgroup, in tenths of a microsecond: common rows for one block of query rows, own rows.
+constexpr int COST_COMMON = 5, COST_WIDE = 8, COST_OWN = 6;
+constexpr int LEAST = 4;                   // blocks of a unit at least: one for each of its waves
 
 struct Unit {
   int32_t own, b, slot, rb;                // own rows of entry b, or a group's that begins with entry b; which block of query rows
@@ -22,15 +25,17 @@ struct Unit {
 };
 // where the parts of an entry's query rows are: rows [common + i * stride + ..], i < n_common, [own + i * R + ..], i < n_own
 struct Where { int64_t common, own; int32_t stride, offset, n_common, n_own; };
+constexpr int QUEUE = 16;                  // words from one kv head's count of units taken to the next
 struct Plan { int32_t units, pad[63]; };
 
-struct SharedLayout { size_t units, where, ml, part, total; int64_t max_units, rows; };
+struct SharedLayout { size_t queue, units, where, ml, part, total; int64_t max_units, rows; };
 
 struct Shares {
   PagedAttnArgs a;
   const int32_t *group_first, *n_shared;
   int32_t groups, workers, common_cols, own_blocks;          // query rows of a unit of common rows; blocks of query rows of an entry
-  Plan* plan; Unit* units; Where* where;
+  int32_t wide;                            // groups of more query rows than that have units of WIDE_COLS (0: none has)
+  Plan* plan; int32_t* queue; Unit* units; Where* where;
 };
 
 // Sum of v over the threads before this one, and over all; `tmp` holds one value for each wave
@@ -48,6 +53,14 @@ __device__ __forceinline__ T sum_before(T v, T* tmp, T* all) {
   return before;
 }
 
+// groups of more query rows than that take blocks of WIDE_COLS of them
+constexpr int WIDE_COLS = 64;
+__device__ __forceinline__ bool is_wide(const Shares& s, int entries) { return s.wide && (int64_t)entries * s.a.M * (s.a.H / s.a.G) > s.wide; }
+__device__ __forceinline__ int cols_of(const Shares& s, int entries) {
+  const int each = is_wide(s, entries) ? WIDE_COLS : s.common_cols;
+  return (entries * s.a.M * (s.a.H / s.a.G) + each - 1) / each;
+}
+__device__ __forceinline__ int cost_of(const Shares& s, int entries) { return is_wide(s, entries) ? COST_WIDE : COST_COMMON; }
 struct Group { int lo, entries, slot, n, blocks, cols; };
 __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int g) {
   Group r = {};
@@ -58,9 +71,26 @@ __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int
   r.slot = paged_slot(s.a.c, s.a.slots, r.lo);
   r.n = min(min(max(s.n_shared[g], 0), paged_len(s.a.c, r.slot)), s.a.bound);
   r.blocks = (r.n + PAGED_BLOCK - 1) / PAGED_BLOCK;
-  r.cols = r.blocks ? (int)(((int64_t)r.entries * s.a.M * (s.a.H / s.a.G) + s.common_cols - 1) / s.common_cols) : 0;
+  r.cols = r.blocks ? cols_of(s, r.entries) : 0;
   return r;
 }
+// What a unit is to take.  An equal share of all (and a little more where there is one unit for each worker: cutting n items into equal lengths makes half a
+// unit more of each), but of long work half of that, so that those who are done early have something to take.
+constexpr int LONG = 240;
+__device__ __forceinline__ float aimed(float work, float items, int workers) {
+  const float share = work / (float)workers;
+  return share > LONG ? 0.5f * share : work / fmaxf((float)workers - 0.5f * items, 0.5f * (float)workers);
+}
+// units of up to `aim` that so many blocks are cut into
+__device__ __forceinline__ int cuts_of(int blocks, float aim, int cost) {
+  const int length = (int)fminf(fmaxf(aim / (float)cost, (float)LEAST), (float)(1 << 28));
+  return (int)((unsigned)(blocks + length - 1) / (unsigned)length);
+}
+// first block of cut i of n; common rows are cut between pairs of blocks, which the wide units take at a time
+__device__ __forceinline__ int cut_at(int blocks, int i, int n, bool own) {
+  return own ? (int)((int64_t)blocks * i / n) : min((int)((int64_t)((blocks + 1) / 2) * i / n) * 2, blocks);
+}
+
 // the group that entry b is in: -1 if it is in none
 __device__ __forceinline__ int group_with(const int* first, int groups, int b) {
   if (b < first[0] || b >= first[groups]) return -1;
@@ -101,19 +131,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     if (g0 + tid <= s.groups) first[g0 + tid] = v;
     __syncthreads();
   }
-  // what there is to do, and from it the blocks that a unit gets
-  int64_t common = 0, own = 0, sum;
-  for (int g = tid; g < s.groups; g += PLAN_THREADS) { const Group x = group_of(s, first, g); common += (int64_t)x.blocks * x.cols; }
-  for (int b = tid; b < s.a.B; b += PLAN_THREADS) own += (int64_t)own_of(s, first, b).blocks * s.own_blocks;
-  sum_before(common * COST_COMMON + own * COST_OWN, tmp, &sum);
-  const int64_t aim = (sum + s.workers - 1) / s.workers;
-  const int64_t long_common = max((aim + COST_COMMON - 1) / COST_COMMON, (int64_t)4), long_own = max((aim + COST_OWN - 1) / COST_OWN, (int64_t)4);
+  // what there is to do, and from it what a unit is to take
+  int64_t mine = 0, items = 0, work, sum;
+  for (int g = tid; g < s.groups; g += PLAN_THREADS) {
+    const Group x = group_of(s, first, g);
+    mine += (int64_t)x.blocks * x.cols * cost_of(s, x.entries);
+    items += x.cols;
+  }
+  for (int b = tid; b < s.a.B; b += PLAN_THREADS) {
+    const int n = own_of(s, first, b).blocks;
+    mine += (int64_t)n * s.own_blocks * COST_OWN;
+    items += n ? s.own_blocks : 0;
+  }
+  sum_before(mine, tmp, &work);
+  sum_before(items, tmp, &sum);
+  const float aim = aimed((float)work, (float)sum, s.workers);
+  for (int g = tid; g < s.a.G; g += PLAN_THREADS) s.queue[(int64_t)g * QUEUE] = s.workers;
 
   int units = 0;
   int64_t parts = 0;
   for (int g0 = 0; g0 < s.groups; g0 += PLAN_THREADS) {
     const Group x = group_of(s, first, g0 + tid);
-    const int cuts = x.blocks ? (int)((x.blocks + long_common - 1) / long_common) : 0;
+    const int cuts = cuts_of(x.blocks, aim, cost_of(s, x.entries));
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * x.cols, tmp, &all), row = sum_before(cuts * x.entries * R, tmp, &sum);
     base[tid] = (int)at; rows[tid] = parts + row;
@@ -123,8 +162,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
       const Group y = group_of(s, first, g0 + i);
-      const int n = (int)((y.blocks + long_common - 1) / long_common), cut = (u - base[i]) / y.cols;
-      s.units[units + u] = Unit{0, y.lo, y.slot, (u - base[i]) % y.cols, (int)((int64_t)y.blocks * cut / n), (int)((int64_t)y.blocks * (cut + 1) / n),
+      const int n = cuts_of(y.blocks, aim, cost_of(s, y.entries)), cut = (u - base[i]) / y.cols;
+      s.units[units + u] = Unit{0, y.lo, y.slot, (u - base[i]) % y.cols, cut_at(y.blocks, cut, n, false), cut_at(y.blocks, cut + 1, n, false),
                                 y.n, y.n, 0, y.entries, rows[i] + cut * y.entries * R};
     }
     const int last = min(g0 + PLAN_THREADS, s.groups);
@@ -133,7 +172,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
       const Group y = group_of(s, first, g);
       Where* w = s.where + b;
       w->common = rows[g - g0]; w->stride = (int)(y.entries * R); w->offset = (int)((b - y.lo) * R);
-      w->n_common = y.blocks ? (int)((y.blocks + long_common - 1) / long_common) : 0;
+      w->n_common = cuts_of(y.blocks, aim, cost_of(s, y.entries));
     }
     units += (int)all; parts += sum;
     __syncthreads();
@@ -141,7 +180,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   for (int b0 = 0; b0 < s.a.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
     const Own x = own_of(s, first, b);
-    const int cuts = (int)((x.blocks + long_own - 1) / long_own);
+    const int cuts = cuts_of(x.blocks, aim, COST_OWN);
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * s.own_blocks, tmp, &all), row = sum_before(cuts * R, tmp, &sum);
     base[tid] = (int)at; rows[tid] = parts + row;
@@ -150,9 +189,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
       const Own y = own_of(s, first, b0 + i);
-      const int n = (int)((y.blocks + long_own - 1) / long_own), cut = (u - base[i]) / s.own_blocks;
-      s.units[units + u] = Unit{1, b0 + i, y.slot, (u - base[i]) % s.own_blocks, (int)((int64_t)y.blocks * cut / n),
-                                (int)((int64_t)y.blocks * (cut + 1) / n), y.n, y.nt, y.from, 1, rows[i] + cut * R};
+      const int n = cuts_of(y.blocks, aim, COST_OWN), cut = (u - base[i]) / s.own_blocks;
+      s.units[units + u] = Unit{1, b0 + i, y.slot, (u - base[i]) % s.own_blocks, cut_at(y.blocks, cut, n, true), cut_at(y.blocks, cut + 1, n, true),
+                                y.n, y.nt, y.from, 1, rows[i] + cut * R};
     }
     if (b < s.a.B) {
       Where* w = s.where + b;
@@ -165,25 +204,312 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   if (tid == 0) s.plan->units = units;
 }
 
+// The same by one wave, where everything is counted in 32 bits: lane b has entry b, lane g group g.
+constexpr int WAVE_ENTRIES = 64, WAVE_ROWS = 1 << 15, WAVE_BOUND = 1 << 20;      // entries (and groups: one less), query rows of all, rows of a sequence
+__device__ __forceinline__ int max_upto(int v) {             // (of numbers from 0 on)
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+}
+// the last of the 64 numbers, in ascending order, that is not above v
+__device__ __forceinline__ int last_upto(const int* at, int v) {
+  int i = 0;
+#pragma unroll
+  for (int k = 32; k > 0; k /= 2)
+    if (at[i + k] <= v) i += k;
+  return i;
+}
+__global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
+  // of each lane's group and entry: units before, blocks, cuts, .. (of those without a unit, what comes next has the same number before it)
+  enum { GROUP_AT, GROUP_LO, GROUP_ENTRIES, GROUP_SLOT, GROUP_N, GROUP_BLOCKS, GROUP_COLS, GROUP_CUTS, GROUP_ROW,
+         OWN_AT, OWN_SLOT, OWN_N, OWN_NT, OWN_FROM, OWN_BLOCKS, OWN_CUTS, OWN_ROW, FIELDS };
+  __shared__ int f[FIELDS][64];
+  const int lane = threadIdx.x, at = min(lane, s.a.B - 1), g_at = min(lane, s.groups - 1), R = s.a.M * (s.a.H / s.a.G);
+  auto of = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+  const int first = s.group_first[g_at], next = s.group_first[g_at + 1], shared = max(s.n_shared[g_at], 0);
+  const int n_true = s.a.n_true ? s.a.n_true[at] : INT32_MAX, slot = paged_slot(s.a.c, s.a.slots, at);
+  for (int g = lane; g < s.a.G; g += 64) s.queue[(int64_t)g * QUEUE] = s.workers;
+  const int len = s.a.c.lens[max(slot, 0)];
+  const int n = lane < s.a.B && slot >= 0 ? min(paged_clamped(len, s.a.c.W, s.a.c.shift), s.a.bound) : 0, nt = min(max(n_true, 0), n);
+  const int lo = max_upto(lane < s.groups ? min(max(first, 0), s.a.B) : 0), hi = lane < s.groups ? max(lo, min(max(next, 0), s.a.B)) : lo;
+  int common = 0, in_group = -1;           // rows that this lane's entry has in common with others; its group
+#pragma unroll 1
+  for (int g = 0; g < s.groups; ++g)
+    if (lane >= of(lo, g) && lane < of(hi, g)) { common = of(shared, g); in_group = g; }
+  const int from = min(common, nt), own_blocks = n > from ? paged_rows_from(n, nt, from).blocks : 0;
+  const int lead = min(lo, s.a.B - 1), entries = hi - lo, group_n = min(shared, __shfl(n, lead)), group_slot = __shfl(slot, lead);
+  const int blocks = entries > 0 ? (group_n + PAGED_BLOCK - 1) / PAGED_BLOCK : 0, cols = blocks ? cols_of(s, entries) : 0, cost = cost_of(s, entries);
+  const int work = sum_upto(blocks * cols * cost + own_blocks * s.own_blocks * COST_OWN), items = sum_upto(cols + (own_blocks ? s.own_blocks : 0));
+  const float aim = aimed((float)of(work, 63), (float)of(items, 63), s.workers);
+  const int cuts = cuts_of(blocks, aim, cost), own_cuts = cuts_of(own_blocks, aim, COST_OWN);
+  const int uc = cuts * cols, uo = own_cuts * s.own_blocks, rc = cuts * entries * R, ro = own_cuts * R;
+  const int uc_upto = sum_upto(uc), uo_upto = sum_upto(uo), rc_upto = sum_upto(rc), common_units = of(uc_upto, 63), units = common_units + of(uo_upto, 63);
+  const int row = rc_upto - rc, own_row = of(rc_upto, 63) + sum_upto(ro) - ro;
+  f[GROUP_AT][lane] = uc_upto - uc; f[GROUP_LO][lane] = lo; f[GROUP_ENTRIES][lane] = entries; f[GROUP_SLOT][lane] = group_slot; f[GROUP_N][lane] = group_n;
+  f[GROUP_BLOCKS][lane] = blocks; f[GROUP_COLS][lane] = cols; f[GROUP_CUTS][lane] = cuts; f[GROUP_ROW][lane] = row;
+  f[OWN_AT][lane] = common_units + uo_upto - uo; f[OWN_SLOT][lane] = slot; f[OWN_N][lane] = n; f[OWN_NT][lane] = nt; f[OWN_FROM][lane] = from;
+  f[OWN_BLOCKS][lane] = own_blocks; f[OWN_CUTS][lane] = own_cuts; f[OWN_ROW][lane] = own_row;
+  __syncthreads();
+  if (lane == 0) s.plan->units = units;
+  if (lane < s.a.B) {
+    const int g = max(in_group, 0);
+    s.where[lane] = Where{f[GROUP_ROW][g], own_row, f[GROUP_ENTRIES][g] * R, (lane - f[GROUP_LO][g]) * R, in_group < 0 ? 0 : f[GROUP_CUTS][g], own_cuts};
+  }
+#pragma unroll 1
+  for (int u = lane; u < units; u += 64) {
+    const bool own = u >= common_units;
+    const int i = last_upto(f[own ? OWN_AT : GROUP_AT], u), each = own ? s.own_blocks : f[GROUP_COLS][i];
+    const int k = u - f[own ? OWN_AT : GROUP_AT][i], cut = (int)((unsigned)k / (unsigned)each), of_all = f[own ? OWN_CUTS : GROUP_CUTS][i];
+    const int all = f[own ? OWN_BLOCKS : GROUP_BLOCKS][i], es = own ? 1 : f[GROUP_ENTRIES][i];
+    s.units[u] = Unit{own, own ? i : f[GROUP_LO][i], f[own ? OWN_SLOT : GROUP_SLOT][i], k - cut * each, cut_at(all, cut, of_all, own),
+                      cut_at(all, cut + 1, of_all, own), f[own ? OWN_N : GROUP_N][i], f[own ? OWN_NT : GROUP_N][i], own ? f[OWN_FROM][i] : 0, es,
+                      (int64_t)f[own ? OWN_ROW : GROUP_ROW][i] + (int64_t)cut * es * R};
+  }
+}
+
+// Common rows for 64 query rows of a group that has more of them (bf16): a tile of 64 rows is staged in LDS for all, two waves take 32 query rows
+// each against its first half, two against its second.  As the training forward, but for the scale in two parts, rows that come from
+// pages, and probabilities in three terms that add up to them exactly (see attend_entry).  Infinite values, rows with what is no number that some queries do not
+// see, and pages that are none, are not looked for: where they show in the result (or a page's number was none), `false` comes back, and the caller
+// has the unit done row by row.
+constexpr int TILE_ROWS = 64;
+struct WideShared { bf16_t stage[2][2][TILE_ROWS * tiles::HD]; };
+__device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& sh, const Item& item, int b, int slot, int n, int first, int last,
+                                            int head, int cb) {
+  using namespace tiles;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));            // what is made of it belongs to this unit: kept for the next one it would take registers
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, ql = lane & 31;
+  const int qw = wave & 1, kw = (wave >> 1) * 32;              // this wave's query rows, and its first row of a tile
+  const int rep = a.H / a.G, R = item.R, r = cb * WIDE_COLS + qw * 32 + ql;
+  const uint32_t row_bytes = (uint32_t)a.G * HD * 2, page_bytes = row_bytes << a.c.shift;          // (the launcher sees to 32 bits)
+  const addr_t zero = (addr_t)zero_row;
+  const int32_t* table = a.c.table + (int64_t)max(slot, 0) * a.c.W;
+  const int shift = a.c.shift, in_page = (1 << shift) - 1;
+  // rows that this thread fetches of a tile: tid / 16 + 16 i; its chunk of them
+  int number[4];
+  bool bad = false;
+  const int row0 = first * PAGED_BLOCK, rows_end = min(last * PAGED_BLOCK, n), tiles_ = (rows_end - row0 + TILE_ROWS - 1) / TILE_ROWS;
+  auto look = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) number[i] = table[min(row0 + t * TILE_ROWS + (tid >> 4) + 16 * i, rows_end - 1) >> shift];
+  };
+  // (swz(at) does not depend on i; rows behind the end are the last one again)
+  const addr_t kbase = (addr_t)a.c.k + (int64_t)head * HD * 2 + ((tid & 15) ^ swz(tid >> 4)) * 16, to_v = (addr_t)a.c.v - (addr_t)a.c.k;
+  auto fetch = [&](int stage, int t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = min(row0 + t * TILE_ROWS + (tid >> 4) + 16 * i, rows_end - 1);
+      const bool none = (unsigned)number[i] >= (unsigned)a.c.P;
+      bad |= none;
+      const addr_t k = kbase + (uint64_t)(none ? 0u : (uint32_t)number[i]) * page_bytes + (uint32_t)(row & in_page) * row_bytes, v = k + to_v;
+      bf16_t* dst = sh.stage[stage][0] + (i * 4 + wave) * 512;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)k, (lds_void_ptr)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)v, (lds_void_ptr)(dst + TILE_ROWS * HD), 16, 0, 0);
+    }
+  };
+  look(0);
+  bf16x8_t qf[HD / 16];
+  {
+    const addr_t p = (addr_t)a.q + (((int64_t)b * a.M + r / rep) * a.H + head * rep + r % rep) * HD * 2;
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) qf[s] = __builtin_bit_cast(bf16x8_t, load16(r < R ? p + 32 * s + 16 * hf : zero));
+  }
+  const int at = b + min(r / (a.M * rep), item.entries - 1), nt = a.n_true ? a.n_true[at] : INT32_MAX;
+  fetch(0, 0);
+  look(1);
+  const int limit = min(min(max(nt, 0), rows_end), min(paged_len(a.c, paged_slot(a.c, a.slots, at)), a.bound));
+  // the least of the limits of this wave's query rows that see anything; the others are cleared at the end
+  int least = limit > 0 ? limit : INT32_MAX;
+#pragma unroll
+  for (int i = 1; i < 32; i *= 2) least = min(least, __shfl_xor(least, i));
+  least = __builtin_amdgcn_readfirstlane(least);
+  f32x16_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const FragOffs fo = make_frag_offs(lane);
+  auto scaled = [&](float x, float less) { return fmaf(x, a.c2_low, fmaf(x, a.c2, -less)); };
+  auto step = [&](int stage, int t) BEAGLE_INLINE_LAMBDA {
+    if (t + 1 < tiles_) {
+      fetch(stage ^ 1, t + 1);
+      look(t + 2);
+    }
+    const bf16_t *ks = sh.stage[stage][0] + kw * HD, *vs = sh.stage[stage][1] + kw * HD;
+    f32x16_t st;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st[e] = 0.f;
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag(ks, fo, 0, s), qf[s], st, 0, 0, 0);
+    pipeline_reads_mfma<HD / 16, 1>();
+    __builtin_amdgcn_sched_barrier(0);
+    const int j0 = row0 + t * TILE_ROWS + kw;                  // register e is row j0 + 8 (e / 4) + 4 hf + e % 4
+    if (j0 + 32 > least) {
+      const int rel = limit - j0 - 4 * hf;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (8 * (e >> 2) + (e & 3) >= rel) st[e] = -INFINITY;
+    }
+    float mx = st[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, st[e]);
+    mx = scaled(half_pair_max(mx), 0.f);
+    // (the reference moves where the maximum has grown by more than 2^8: float sums and terms have room for that)
+    const bool grow = mx - m > 8.f;
+    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+      const float now = grow ? mx : m, alpha = grow ? exp2_fast(m - now) : 1.f;
+      l *= alpha;
+      m = now;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+    }
+    const float safe = m == -INFINITY ? 0.f : m;
+    union Term { uint32_t u[4]; bf16x8_t v; } term[3][2];
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float p0 = exp2_fast(scaled(st[e], safe)), p1 = exp2_fast(scaled(st[e + 1], safe));
+      l += p0 + p1;
+      uint32_t x = __float_as_uint(p0), y = __float_as_uint(p1);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        term[k][e >> 3].u[(e & 7) >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        if (k == 2) break;
+        x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xffff0000u));
+        y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xffff0000u));
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8_t w[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) w[h][c] = tr_frag(vs, fo, 16 * h, c);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[h][c], term[k][h].v, o[c], 0, 0, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);         // the second half's reads behind the first MFMAs
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 16, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vmem();
+    __syncthreads();
+  };
+  wait_vmem();
+  __syncthreads();
+  int t = 0;
+#pragma unroll 1
+  for (; t + 2 <= tiles_; t += 2) {
+    step(0, t);
+    step(1, t + 1);
+  }
+  if (t < tiles_) step(0, t);
+
+  l = half_pair_sum(l);
+  if (limit <= 0) {
+    m = -INFINITY; l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  }
+  // the second half's result joins the first's
+  float4* po = (float4*)sh.stage[0][0] + qw * 64 + lane;       // [16][2 waves][64 lanes]: 32 KB
+  float2* pml = (float2*)sh.stage[1][0] + qw * 64 + lane;
+  int* flag = (int*)sh.stage[1][1];
+  if (tid == 0) *flag = 0;
+  __syncthreads();
+  if (kw) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) po[128 * i] = float4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+    *pml = float2{m, l};
+    if (bad) *flag = 1;
+  }
+  __syncthreads();
+  if (!kw) {
+    const float2 ml = *pml;
+    const float now = fmaxf(m, ml.x), safe = now == -INFINITY ? 0.f : now;
+    const float w0 = exp2_fast(m - safe), w1 = exp2_fast(ml.x - safe);
+    m = now;
+    l = l * w0 + ml.y * w1;
+    float sum = l;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float4 v = po[128 * i];
+      const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { o[i >> 2][4 * (i & 3) + e] = o[i >> 2][4 * (i & 3) + e] * w0 + w[e] * w1; sum += o[i >> 2][4 * (i & 3) + e]; }
+    }
+    if (bad || (r < R && !(sum == sum))) *flag = 1;            // (an infinite sum of both signs, too)
+  }
+  __syncthreads();
+  const bool whole = *flag == 0;
+  if (whole && !kw && r < R) {
+    float* row = a.part + (item.part_row + r) * HD;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)                               // channels 32 (i / 4) + 8 (i % 4) + 4 hf ..
+      *(f32x4*)(row + 32 * (i >> 2) + 8 * (i & 3) + 4 * hf) =
+          f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+    if (hf == 0) *(float2*)(a.ml + (item.part_row + r) * 2) = make_float2(m, l);
+  }
+  return whole;
+}
+
+// The workgroups that have the same number modulo eight share a die and its cache: those of one head, as far as heads go.
 template <bool BF16, int NH, int RTC, int RTO, bool TREE>
 __global__ __launch_bounds__(256, RESIDENT) void paged_shared_kernel(Shares s) {
   using S = Shape<BF16, NH>;
-  __shared__ union { Shared<S, RTC, 4, PREFIX> common; Shared<S, RTO, 4, SUFFIX> own; } shared;
+  __shared__ __attribute__((aligned(1024))) union { WideShared wide[BF16 ? 1 : 0]; Shared<S, RTC, 4, PREFIX> common; Shared<S, RTO, 4, SUFFIX> own; } shared;
   const int head = blockIdx.x % s.a.G;
   auto wave = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int units = wave(s.plan->units);
-  for (int u = blockIdx.x / s.a.G; u < units; u += s.workers) {
+#pragma unroll 1
+  for (int u = blockIdx.x / s.a.G; u < units;) {
     const Unit x = s.units[u];
+    // what comes next is asked for now, and known when this unit is done
+    int next = 0;
+    if (threadIdx.x == 0) next = __hip_atomic_fetch_add(s.queue + (int64_t)head * QUEUE, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const int R = s.a.M * (s.a.H / s.a.G) * wave(x.entries);
     Item item = {};
     item.R = R; item.entries = wave(x.entries);
     const int64_t part = (int64_t)wave((int)(x.part >> 32)) << 32 | (uint32_t)wave((int)x.part);
     item.part_row = part * s.a.G + (int64_t)head * R;
     const int b = wave(x.b), slot = wave(x.slot), rb = wave(x.rb), first = wave(x.first), last = wave(x.last), n = wave(x.n);
-    if (u >= s.workers) __syncthreads();   // (LDS holds the unit before)
-    if (wave(x.own)) attend_entry<BF16, NH, RTO, TREE, 4, SUFFIX>(s.a, shared.own, item, b, slot, paged_rows_from(n, wave(x.nt), wave(x.from)),
-                                                                first, last, false, 0, head, rb);
-    else attend_entry<BF16, NH, RTC, false, 4, PREFIX>(s.a, shared.common, item, b, slot, paged_rows(n, n, 0, 0), first, last, false, 0, head, rb);
+    if (wave(x.own)) {
+      attend_entry<BF16, NH, RTO, TREE, 4, SUFFIX>(s.a, shared.own, item, b, slot, paged_rows_from(n, wave(x.nt), wave(x.from)), first, last, false, 0,
+                                                   head, rb);
+    } else {
+      int block = rb, blocks = 1;
+      if constexpr (BF16)
+        if (is_wide(s, item.entries)) {
+          const bool done = attend_wide(s.a, shared.wide[0], item, b, slot, n, first, last, head, rb);
+          blocks = done ? 0 : WIDE_COLS / (16 * RTC);
+          block = rb * (WIDE_COLS / (16 * RTC));
+        }
+#pragma unroll 1
+      for (int i = 0; i < blocks; ++i) {
+        __syncthreads();
+        attend_entry<BF16, NH, RTC, false, 4, PREFIX>(s.a, shared.common, item, b, slot, paged_rows(n, n, 0, 0), first, last, false, 0, head, block + i);
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *(int*)&shared = next;
+    __syncthreads();
+    u = wave(*(const int*)&shared);
+    __syncthreads();
   }
 }
 
@@ -244,20 +570,21 @@ __global__ __launch_bounds__(256) void paged_shared_join_kernel(Shares s) {
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
+constexpr int WIDE_FROM = 64;
 constexpr int COMMON_TILES = 2;            // of 16 query rows in a unit of common rows
 int shared_workers(int G) { return G < 256 * RESIDENT ? 256 * RESIDENT / G : 1; }
 
-// A unit has at least an equal share of the blocks, so that cutting adds at most `workers` units to those that groups and entries
-// have uncut, and as many query rows to the parts.
+// A unit has at least 0.8 of what is aimed at (a length of four blocks or more is rounded down), which is at least half of an equal share: cutting adds at most
+// 2.5 units for each worker to those that groups and entries have uncut, and as many query rows to the parts.
 SharedLayout shared_layout(int32_t B, int32_t M, int32_t H, int32_t G) {
-  const int64_t R = (int64_t)M * (H / G), workers = shared_workers(G);
+  const int64_t R = (int64_t)M * (H / G), cut = (int64_t)shared_workers(G) * 5 / 2 + 1;
   const Tiles own = tiles_of((int)R);
-  const int64_t cols = 16 * COMMON_TILES;
   SharedLayout l;
-  l.max_units = workers + B + (B * R + cols - 1) / cols + workers + (int64_t)B * own.blocks;
-  l.rows = workers * cols + B * R + workers * 16 * own.each + B * R;
+  l.max_units = shared_workers(G) + cut + B + (B * R + 16 * COMMON_TILES - 1) / (16 * COMMON_TILES) + cut + (int64_t)B * own.blocks;
+  l.rows = cut * WIDE_COLS + B * R + cut * 16 * own.each + B * R;
   size_t at = sizeof(Plan);
   auto take = [&](size_t n) { const size_t o = at; at = (at + n + 255) / 256 * 256; return o; };
+  l.queue = take((size_t)G * QUEUE * sizeof(int32_t));
   l.units = take(l.max_units * sizeof(Unit));
   l.where = take(B * sizeof(Where));
   l.ml = take((size_t)l.rows * G * 2 * sizeof(float));
@@ -277,6 +604,7 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   const SharedLayout l = shared_layout(p.a.B, p.a.M, p.a.H, p.a.G);
   char* at = (char*)ws;
   x.plan = (Plan*)at;
+  x.queue = (int32_t*)(at + l.queue);
   x.units = (Unit*)(at + l.units);
   x.where = (Where*)(at + l.where);
   x.a.ml = (float*)(at + l.ml);
@@ -286,9 +614,12 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   x.workers = shared_workers(p.a.G);
   x.common_cols = 16 * COMMON_TILES;
   x.own_blocks = own.blocks;
+  x.wide = bf16 && ((int64_t)p.a.G * tiles::HD * 2 << p.a.c.shift) < (1ll << 32) ? WIDE_FROM : 0;
+  const bool by_wave = p.a.B <= WAVE_ENTRIES && p.groups < WAVE_ENTRIES && (int64_t)p.a.B * p.a.M * (p.a.H / p.a.G) <= WAVE_ROWS && p.a.bound <= WAVE_BOUND;
   {
     ProfScope ps("paged_shared_plan", s);
-    hipLaunchKernelGGL(paged_shared_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, x);
+    if (by_wave) hipLaunchKernelGGL(paged_shared_small_plan_kernel, dim3(1), dim3(64), 0, s, x);
+    else hipLaunchKernelGGL(paged_shared_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, x);
   }
   const bool narrow = !bf16 && p.a.d <= 64, tree = p.a.n_true != nullptr;
   {
