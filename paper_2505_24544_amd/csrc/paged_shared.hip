@@ -74,12 +74,12 @@ __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int
   r.cols = r.blocks ? cols_of(s, r.entries) : 0;
   return r;
 }
-// What a unit is to take.  An equal share of all (and a little more where there is one unit for each worker: cutting n items into equal lengths makes half a
-// unit more of each), but of long work half of that, so that those who are done early have something to take.
+// What a unit is to take: so much that each worker has one, or of long work two, so that those who are done early have something to take.  (Cutting n items
+// into equal lengths makes half a unit more of each.)
 constexpr int LONG = 240;
 __device__ __forceinline__ float aimed(float work, float items, int workers) {
-  const float share = work / (float)workers;
-  return share > LONG ? 0.5f * share : work / fmaxf((float)workers - 0.5f * items, 0.5f * (float)workers);
+  const float units = work > (float)LONG * (float)workers ? 2.f * (float)workers : (float)workers;
+  return work / fmaxf(units - 0.5f * items, 0.5f * (float)workers);
 }
 // units of up to `aim` that so many blocks are cut into
 __device__ __forceinline__ int cuts_of(int blocks, float aim, int cost) {
@@ -276,6 +276,11 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
 // see, and pages that are none, are not looked for: where they show in the result (or a page's number was none), `false` comes back, and the caller
 // has the unit done row by row.
 constexpr int TILE_ROWS = 64;
+// 16 bytes of each lane, in order, to a place in LDS.  Written out, since the compiler takes every later read of LDS for one of what is still on its
+// way and has it wait; who reads it here has waited for it by count, and met the others at a barrier.
+__device__ __forceinline__ void load_to_lds(addr_t from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+}
 struct WideShared { bf16_t stage[2][2][TILE_ROWS * tiles::HD]; };
 __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& sh, const Item& item, int b, int slot, int n, int first, int last,
                                             int head, int cb) {
@@ -297,6 +302,7 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
 #pragma unroll
     for (int i = 0; i < 4; ++i) number[i] = table[min(row0 + t * TILE_ROWS + (tid >> 4) + 16 * i, rows_end - 1) >> shift];
   };
+  const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(lds_void_ptr)sh.stage[0][0]);
   // (swz(at) does not depend on i; rows behind the end are the last one again)
   const addr_t kbase = (addr_t)a.c.k + (int64_t)head * HD * 2 + ((tid & 15) ^ swz(tid >> 4)) * 16, to_v = (addr_t)a.c.v - (addr_t)a.c.k;
   auto fetch = [&](int stage, int t) {
@@ -306,9 +312,9 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
       const bool none = (unsigned)number[i] >= (unsigned)a.c.P;
       bad |= none;
       const addr_t k = kbase + (uint64_t)(none ? 0u : (uint32_t)number[i]) * page_bytes + (uint32_t)(row & in_page) * row_bytes, v = k + to_v;
-      bf16_t* dst = sh.stage[stage][0] + (i * 4 + wave) * 512;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)k, (lds_void_ptr)dst, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)v, (lds_void_ptr)(dst + TILE_ROWS * HD), 16, 0, 0);
+      const uint32_t dst = lds0 + (uint32_t)((2 * stage * TILE_ROWS * HD + (i * 4 + wave) * 512) * 2);
+      load_to_lds(k, dst);
+      load_to_lds(v, dst + TILE_ROWS * HD * 2);
     }
   };
   look(0);
@@ -344,8 +350,12 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
     f32x16_t st;
 #pragma unroll
     for (int e = 0; e < 16; ++e) st[e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8_t kf[HD / 16];
 #pragma unroll
-    for (int s = 0; s < HD / 16; ++s) st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag(ks, fo, 0, s), qf[s], st, 0, 0, 0);
+    for (int s = 0; s < HD / 16; ++s) kf[s] = row_frag(ks, fo, 0, s);
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], st, 0, 0, 0);
     pipeline_reads_mfma<HD / 16, 1>();
     __builtin_amdgcn_sched_barrier(0);
     const int j0 = row0 + t * TILE_ROWS + kw;                  // register e is row j0 + 8 (e / 4) + 4 hf + e % 4
@@ -372,38 +382,45 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
     }
     const float safe = m == -INFINITY ? 0.f : m;
     union Term { uint32_t u[4]; bf16x8_t v; } term[3][2];
+    auto terms = [&](int h) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-      const float p0 = exp2_fast(scaled(st[e], safe)), p1 = exp2_fast(scaled(st[e + 1], safe));
-      l += p0 + p1;
-      uint32_t x = __float_as_uint(p0), y = __float_as_uint(p1);
+      for (int e = 8 * h; e < 8 * h + 8; e += 2) {
+        const float p0 = exp2_fast(scaled(st[e], safe)), p1 = exp2_fast(scaled(st[e + 1], safe));
+        l += p0 + p1;
+        uint32_t x = __float_as_uint(p0), y = __float_as_uint(p1);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        term[k][e >> 3].u[(e & 7) >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        if (k == 2) break;
-        x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xffff0000u));
-        y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xffff0000u));
+        for (int k = 0; k < 3; ++k) {
+          term[k][h].u[(e & 7) >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+          if (k == 2) break;
+          x = __float_as_uint(__uint_as_float(x) - __uint_as_float(x & 0xffff0000u));
+          y = __float_as_uint(__uint_as_float(y) - __uint_as_float(y & 0xffff0000u));
+        }
       }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    bf16x8_t w[2][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) w[h][c] = tr_frag(vs, fo, 16 * h, c);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
+    };
+    auto values = [&](int h, const bf16x8_t (&w)[4]) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
       for (int k = 0; k < 3; ++k)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[h][c], term[k][h].v, o[c], 0, 0, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);         // the second half's reads behind the first MFMAs
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[c], term[k][h].v, o[c], 0, 0, 0);
+    };
+    bf16x8_t w0[4], w1[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int c = 0; c < 4; ++c) w0[c] = tr_frag(vs, fo, 0, c);
+    terms(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // the first sixteen rows' products run behind the second's probabilities
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w1[c] = tr_frag(vs, fo, 16, c);
+    values(0, w0);
+    terms(1);
+#pragma unroll
+    for (int i = 0; i < 12; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (i < 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 7, 0);       // vector, transcendental
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 16, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    values(1, w1);
     __builtin_amdgcn_sched_barrier(0);
     wait_vmem();
     __syncthreads();
