@@ -13,9 +13,12 @@ namespace beagle {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-// What a block of 32 rows takes a workgroup, in tenths of a microsecond: common rows for one block of query rows, own rows.
-constexpr int COST_COMMON = 5, COST_WIDE = 8, COST_OWN = 6;
-constexpr int LEAST = 4;                   // blocks of a unit at least: one for each of its waves
+// The workgroups of the second launch: of four waves, two on a compute unit, or where groups have many query rows (bf16) of eight.  With `cols`
+// query rows in a wide unit, and what a block of 32 rows takes one of them, in tenths of a microsecond: common rows for one block of query rows, own rows.
+template <int WAVES> struct Work {
+  static constexpr int workgroups = 256 * 8 / WAVES, cols = 16 * WAVES, stages = WAVES / 2;
+  static constexpr int common = WAVES == 8 ? 3 : 5, wide = 8, own = WAVES == 8 ? 4 : 6;
+};
 
 struct Unit {
   int32_t own, b, slot, rb;                // own rows of entry b, or a group's that begins with entry b; which block of query rows
@@ -25,7 +28,7 @@ struct Unit {
 };
 // where the parts of an entry's query rows are: rows [common + i * stride + ..], i < n_common, [own + i * R + ..], i < n_own
 struct Where { int64_t common, own; int32_t stride, offset, n_common, n_own; };
-constexpr int QUEUE = 16;                  // words from one kv head's count of units taken to the next
+constexpr int QUEUE = 16;                  // words from one queue's count of units taken to the next
 struct Plan { int32_t units, pad[63]; };
 
 struct SharedLayout { size_t queue, units, where, ml, part, total; int64_t max_units, rows; };
@@ -33,8 +36,11 @@ struct SharedLayout { size_t queue, units, where, ml, part, total; int64_t max_u
 struct Shares {
   PagedAttnArgs a;
   const int32_t *group_first, *n_shared;
-  int32_t groups, workers, common_cols, own_blocks;          // query rows of a unit of common rows; blocks of query rows of an entry
-  int32_t wide;                            // groups of more query rows than that have units of WIDE_COLS (0: none has)
+  int32_t queues, workgroups, waves;       // queues of units; workgroups, and the waves of one, which a unit has blocks for at least
+  int32_t cost_common, cost_wide, cost_own;
+  float workers;                           // of a kv head
+  int32_t groups, common_cols, own_blocks;                   // query rows of a unit of common rows; blocks of query rows of an entry
+  int32_t wide;                            // query rows of a wide unit, which groups of more than common_cols have (0: none has)
   Plan* plan; int32_t* queue; Unit* units; Where* where;
 };
 
@@ -53,14 +59,12 @@ __device__ __forceinline__ T sum_before(T v, T* tmp, T* all) {
   return before;
 }
 
-// groups of more query rows than that take blocks of WIDE_COLS of them
-constexpr int WIDE_COLS = 64;
-__device__ __forceinline__ bool is_wide(const Shares& s, int entries) { return s.wide && (int64_t)entries * s.a.M * (s.a.H / s.a.G) > s.wide; }
+__device__ __forceinline__ bool is_wide(const Shares& s, int entries) { return s.wide && (int64_t)entries * s.a.M * (s.a.H / s.a.G) > s.common_cols; }
 __device__ __forceinline__ int cols_of(const Shares& s, int entries) {
-  const int each = is_wide(s, entries) ? WIDE_COLS : s.common_cols;
+  const int each = is_wide(s, entries) ? s.wide : s.common_cols;
   return (entries * s.a.M * (s.a.H / s.a.G) + each - 1) / each;
 }
-__device__ __forceinline__ int cost_of(const Shares& s, int entries) { return is_wide(s, entries) ? COST_WIDE : COST_COMMON; }
+__device__ __forceinline__ int cost_of(const Shares& s, int entries) { return is_wide(s, entries) ? s.cost_wide : s.cost_common; }
 struct Group { int lo, entries, slot, n, blocks, cols; };
 __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int g) {
   Group r = {};
@@ -76,14 +80,14 @@ __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int
 }
 // What a unit is to take: so much that each worker has one, or of long work two, so that those who are done early have something to take.  (Cutting n items
 // into equal lengths makes half a unit more of each.)
-constexpr int LONG = 240;
-__device__ __forceinline__ float aimed(float work, float items, int workers) {
-  const float units = work > (float)LONG * (float)workers ? 2.f * (float)workers : (float)workers;
-  return work / fmaxf(units - 0.5f * items, 0.5f * (float)workers);
+constexpr float LONG = 240.f;
+__device__ __forceinline__ float aimed(float work, float items, float workers) {
+  const float units = work > LONG * workers ? 2.f * workers : workers;
+  return work / fmaxf(units - 0.5f * items, 0.5f * workers);
 }
 // units of up to `aim` that so many blocks are cut into
-__device__ __forceinline__ int cuts_of(int blocks, float aim, int cost) {
-  const int length = (int)fminf(fmaxf(aim / (float)cost, (float)LEAST), (float)(1 << 28));
+__device__ __forceinline__ int cuts_of(int blocks, float aim, int cost, int least) {
+  const int length = (int)fminf(fmaxf(aim / (float)cost, (float)least), (float)(1 << 28));
   return (int)((unsigned)(blocks + length - 1) / (unsigned)length);
 }
 // first block of cut i of n; common rows are cut between pairs of blocks, which the wide units take at a time
@@ -140,19 +144,19 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   }
   for (int b = tid; b < s.a.B; b += PLAN_THREADS) {
     const int n = own_of(s, first, b).blocks;
-    mine += (int64_t)n * s.own_blocks * COST_OWN;
+    mine += (int64_t)n * s.own_blocks * s.cost_own;
     items += n ? s.own_blocks : 0;
   }
   sum_before(mine, tmp, &work);
   sum_before(items, tmp, &sum);
   const float aim = aimed((float)work, (float)sum, s.workers);
-  for (int g = tid; g < s.a.G; g += PLAN_THREADS) s.queue[(int64_t)g * QUEUE] = s.workers;
+  if (tid < s.queues) s.queue[tid * QUEUE] = s.workgroups / s.queues;
 
   int units = 0;
   int64_t parts = 0;
   for (int g0 = 0; g0 < s.groups; g0 += PLAN_THREADS) {
     const Group x = group_of(s, first, g0 + tid);
-    const int cuts = cuts_of(x.blocks, aim, cost_of(s, x.entries));
+    const int cuts = cuts_of(x.blocks, aim, cost_of(s, x.entries), s.waves);
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * x.cols, tmp, &all), row = sum_before(cuts * x.entries * R, tmp, &sum);
     base[tid] = (int)at; rows[tid] = parts + row;
@@ -162,7 +166,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
       const Group y = group_of(s, first, g0 + i);
-      const int n = cuts_of(y.blocks, aim, cost_of(s, y.entries)), cut = (u - base[i]) / y.cols;
+      const int n = cuts_of(y.blocks, aim, cost_of(s, y.entries), s.waves), cut = (u - base[i]) / y.cols;
       s.units[units + u] = Unit{0, y.lo, y.slot, (u - base[i]) % y.cols, cut_at(y.blocks, cut, n, false), cut_at(y.blocks, cut + 1, n, false),
                                 y.n, y.n, 0, y.entries, rows[i] + cut * y.entries * R};
     }
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
       const Group y = group_of(s, first, g);
       Where* w = s.where + b;
       w->common = rows[g - g0]; w->stride = (int)(y.entries * R); w->offset = (int)((b - y.lo) * R);
-      w->n_common = cuts_of(y.blocks, aim, cost_of(s, y.entries));
+      w->n_common = cuts_of(y.blocks, aim, cost_of(s, y.entries), s.waves);
     }
     units += (int)all; parts += sum;
     __syncthreads();
@@ -180,7 +184,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   for (int b0 = 0; b0 < s.a.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
     const Own x = own_of(s, first, b);
-    const int cuts = cuts_of(x.blocks, aim, COST_OWN);
+    const int cuts = cuts_of(x.blocks, aim, s.cost_own, s.waves);
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * s.own_blocks, tmp, &all), row = sum_before(cuts * R, tmp, &sum);
     base[tid] = (int)at; rows[tid] = parts + row;
@@ -189,7 +193,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
       const Own y = own_of(s, first, b0 + i);
-      const int n = cuts_of(y.blocks, aim, COST_OWN), cut = (u - base[i]) / s.own_blocks;
+      const int n = cuts_of(y.blocks, aim, s.cost_own, s.waves), cut = (u - base[i]) / s.own_blocks;
       s.units[units + u] = Unit{1, b0 + i, y.slot, (u - base[i]) % s.own_blocks, cut_at(y.blocks, cut, n, true), cut_at(y.blocks, cut + 1, n, true),
                                 y.n, y.nt, y.from, 1, rows[i] + cut * R};
     }
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
   auto of = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
   const int first = s.group_first[g_at], next = s.group_first[g_at + 1], shared = max(s.n_shared[g_at], 0);
   const int n_true = s.a.n_true ? s.a.n_true[at] : INT32_MAX, slot = paged_slot(s.a.c, s.a.slots, at);
-  for (int g = lane; g < s.a.G; g += 64) s.queue[(int64_t)g * QUEUE] = s.workers;
+  if (lane < s.queues) s.queue[lane * QUEUE] = s.workgroups / s.queues;
   const int len = s.a.c.lens[max(slot, 0)];
   const int n = lane < s.a.B && slot >= 0 ? min(paged_clamped(len, s.a.c.W, s.a.c.shift), s.a.bound) : 0, nt = min(max(n_true, 0), n);
   const int lo = max_upto(lane < s.groups ? min(max(first, 0), s.a.B) : 0), hi = lane < s.groups ? max(lo, min(max(next, 0), s.a.B)) : lo;
@@ -242,9 +246,9 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
   const int from = min(common, nt), own_blocks = n > from ? paged_rows_from(n, nt, from).blocks : 0;
   const int lead = min(lo, s.a.B - 1), entries = hi - lo, group_n = min(shared, __shfl(n, lead)), group_slot = __shfl(slot, lead);
   const int blocks = entries > 0 ? (group_n + PAGED_BLOCK - 1) / PAGED_BLOCK : 0, cols = blocks ? cols_of(s, entries) : 0, cost = cost_of(s, entries);
-  const int work = sum_upto(blocks * cols * cost + own_blocks * s.own_blocks * COST_OWN), items = sum_upto(cols + (own_blocks ? s.own_blocks : 0));
+  const int work = sum_upto(blocks * cols * cost + own_blocks * s.own_blocks * s.cost_own), items = sum_upto(cols + (own_blocks ? s.own_blocks : 0));
   const float aim = aimed((float)of(work, 63), (float)of(items, 63), s.workers);
-  const int cuts = cuts_of(blocks, aim, cost), own_cuts = cuts_of(own_blocks, aim, COST_OWN);
+  const int cuts = cuts_of(blocks, aim, cost, s.waves), own_cuts = cuts_of(own_blocks, aim, s.cost_own, s.waves);
   const int uc = cuts * cols, uo = own_cuts * s.own_blocks, rc = cuts * entries * R, ro = own_cuts * R;
   const int uc_upto = sum_upto(uc), uo_upto = sum_upto(uo), rc_upto = sum_upto(rc), common_units = of(uc_upto, 63), units = common_units + of(uo_upto, 63);
   const int row = rc_upto - rc, own_row = of(rc_upto, 63) + sum_upto(ro) - ro;
@@ -270,54 +274,61 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
   }
 }
 
-// Common rows for 64 query rows of a group that has more of them (bf16): a tile of 64 rows is staged in LDS for all, two waves take 32 query rows
-// each against its first half, two against its second.  As the training forward, but for the scale in two parts, rows that come from
-// pages, and probabilities in three terms that add up to them exactly (see attend_entry).  Infinite values, rows with what is no number that some queries do not
-// see, and pages that are none, are not looked for: where they show in the result (or a page's number was none), `false` comes back, and the caller
-// has the unit done row by row.
+// Common rows for 64 or 128 query rows of a group that has more of them (bf16): tiles of 64 rows go through a ring of LDS stages; half of the waves
+// take 32 query rows each against a tile's first half, half of them against its second.  As the training forward, but for the scale in two parts,
+// rows that come from pages, and probabilities in three terms that add up to them exactly (see attend_entry).  Infinite values, rows with what is no
+// number that some queries do not see, and pages that are none, are not looked for: where they show in the result (or a page's number was none),
+// `false` comes back, and the caller has the unit done row by row.
 constexpr int TILE_ROWS = 64;
 // 16 bytes of each lane, in order, to a place in LDS.  Written out, since the compiler takes every later read of LDS for one of what is still on its
 // way and has it wait; who reads it here has waited for it by count, and met the others at a barrier.
 __device__ __forceinline__ void load_to_lds(addr_t from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
 }
-struct WideShared { bf16_t stage[2][2][TILE_ROWS * tiles::HD]; };
-__device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& sh, const Item& item, int b, int slot, int n, int first, int last,
+constexpr int NUMBERS = 2048;              // page numbers that are held at a time
+template <int WAVES> struct WideShared { bf16_t stage[Work<WAVES>::stages][2][TILE_ROWS * tiles::HD]; int pages[NUMBERS]; };
+template <int WAVES>
+__device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared<WAVES>& sh, const Item& item, int b, int slot, int n, int first, int last,
                                             int head, int cb) {
   using namespace tiles;
+  constexpr int STAGES = Work<WAVES>::stages, COLS = Work<WAVES>::cols, HALF = WAVES / 2, CHUNKS = 16 / WAVES;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));            // what is made of it belongs to this unit: kept for the next one it would take registers
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, ql = lane & 31;
-  const int qw = wave & 1, kw = (wave >> 1) * 32;              // this wave's query rows, and its first row of a tile
-  const int rep = a.H / a.G, R = item.R, r = cb * WIDE_COLS + qw * 32 + ql;
+  const int qw = wave % HALF, kw = wave / HALF * 32;                // this wave's query rows, and its first row of a tile
+  const int rep = a.H / a.G, R = item.R, r = cb * COLS + qw * 32 + ql;
   const uint32_t row_bytes = (uint32_t)a.G * HD * 2, page_bytes = row_bytes << a.c.shift;          // (the launcher sees to 32 bits)
   const addr_t zero = (addr_t)zero_row;
   const int32_t* table = a.c.table + (int64_t)max(slot, 0) * a.c.W;
   const int shift = a.c.shift, in_page = (1 << shift) - 1;
-  // rows that this thread fetches of a tile: tid / 16 + 16 i; its chunk of them
-  int number[4];
-  bool bad = false;
   const int row0 = first * PAGED_BLOCK, rows_end = min(last * PAGED_BLOCK, n), tiles_ = (rows_end - row0 + TILE_ROWS - 1) / TILE_ROWS;
-  auto look = [&](int t) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) number[i] = table[min(row0 + t * TILE_ROWS + (tid >> 4) + 16 * i, rows_end - 1) >> shift];
+  // tiles whose page numbers are held: they begin with one of the numbers' first row at most a page before it
+  const int held = max(((NUMBERS - 1) << min(shift, 16)) / TILE_ROWS, 1);
+  bool bad = false;
+  int page0 = 0;
+  auto look = [&](int t0, int t1) {
+    page0 = (row0 + t0 * TILE_ROWS) >> shift;
+    const int end = t1 < tiles_ ? (row0 + t1 * TILE_ROWS - 1) >> shift : (rows_end - 1) >> shift;
+    for (int i = page0 + tid; i <= end; i += 64 * WAVES) {
+      const int number = table[i];
+      const bool none = (unsigned)number >= (unsigned)a.c.P;
+      bad |= none;
+      sh.pages[i - page0] = none ? 0 : number;
+    }
   };
   const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(lds_void_ptr)sh.stage[0][0]);
-  // (swz(at) does not depend on i; rows behind the end are the last one again)
+  // this thread fetches its chunk of rows tid / 16 + 4 WAVES i of a tile (swz is the same for all of them; rows behind the end are the last one again)
   const addr_t kbase = (addr_t)a.c.k + (int64_t)head * HD * 2 + ((tid & 15) ^ swz(tid >> 4)) * 16, to_v = (addr_t)a.c.v - (addr_t)a.c.k;
-  auto fetch = [&](int stage, int t) {
+  auto fetch = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = min(row0 + t * TILE_ROWS + (tid >> 4) + 16 * i, rows_end - 1);
-      const bool none = (unsigned)number[i] >= (unsigned)a.c.P;
-      bad |= none;
-      const addr_t k = kbase + (uint64_t)(none ? 0u : (uint32_t)number[i]) * page_bytes + (uint32_t)(row & in_page) * row_bytes, v = k + to_v;
-      const uint32_t dst = lds0 + (uint32_t)((2 * stage * TILE_ROWS * HD + (i * 4 + wave) * 512) * 2);
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int row = min(row0 + t * TILE_ROWS + (tid >> 4) + 4 * WAVES * i, rows_end - 1), number = sh.pages[(row >> shift) - page0];
+      const addr_t k = kbase + (uint64_t)(uint32_t)number * page_bytes + (uint32_t)(row & in_page) * row_bytes, v = k + to_v;
+      const uint32_t dst = lds0 + (uint32_t)((t % STAGES * 2 * TILE_ROWS * HD + (i * WAVES + wave) * 512) * 2);
       load_to_lds(k, dst);
       load_to_lds(v, dst + TILE_ROWS * HD * 2);
     }
   };
-  look(0);
   bf16x8_t qf[HD / 16];
   {
     const addr_t p = (addr_t)a.q + (((int64_t)b * a.M + r / rep) * a.H + head * rep + r % rep) * HD * 2;
@@ -325,8 +336,6 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
     for (int s = 0; s < HD / 16; ++s) qf[s] = __builtin_bit_cast(bf16x8_t, load16(r < R ? p + 32 * s + 16 * hf : zero));
   }
   const int at = b + min(r / (a.M * rep), item.entries - 1), nt = a.n_true ? a.n_true[at] : INT32_MAX;
-  fetch(0, 0);
-  look(1);
   const int limit = min(min(max(nt, 0), rows_end), min(paged_len(a.c, paged_slot(a.c, a.slots, at)), a.bound));
   // the least of the limits of this wave's query rows that see anything; the others are cleared at the end
   int least = limit > 0 ? limit : INT32_MAX;
@@ -341,12 +350,8 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
   float m = -INFINITY, l = 0.f;
   const FragOffs fo = make_frag_offs(lane);
   auto scaled = [&](float x, float less) { return fmaf(x, a.c2_low, fmaf(x, a.c2, -less)); };
-  auto step = [&](int stage, int t) BEAGLE_INLINE_LAMBDA {
-    if (t + 1 < tiles_) {
-      fetch(stage ^ 1, t + 1);
-      look(t + 2);
-    }
-    const bf16_t *ks = sh.stage[stage][0] + kw * HD, *vs = sh.stage[stage][1] + kw * HD;
+  auto step = [&](int t) BEAGLE_INLINE_LAMBDA {
+    const bf16_t *ks = sh.stage[t % STAGES][0] + kw * HD, *vs = ks + TILE_ROWS * HD;
     f32x16_t st;
 #pragma unroll
     for (int e = 0; e < 16; ++e) st[e] = 0.f;
@@ -422,18 +427,27 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
     __builtin_amdgcn_sched_barrier(0);
     values(1, w1);
     __builtin_amdgcn_sched_barrier(0);
-    wait_vmem();
-    __syncthreads();
   };
-  wait_vmem();
-  __syncthreads();
-  int t = 0;
 #pragma unroll 1
-  for (; t + 2 <= tiles_; t += 2) {
-    step(0, t);
-    step(1, t + 1);
+  for (int t0 = 0; t0 < tiles_; t0 += held) {
+    const int t1 = min(t0 + held, tiles_);
+    look(t0, t1);
+    __syncthreads();
+#pragma unroll 1
+    for (int t = t0; t < min(t0 + STAGES - 1, t1); ++t) fetch(t);
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      // tile t is there when all but the requests of the tiles behind it are back (2 CHUNKS for each), in all waves; then nobody reads tile t - 1
+      // any more, whose place the next one takes
+      if (STAGES > 3 && t + 2 < t1) wait_vmem_n<4 * CHUNKS>();
+      else if (STAGES > 2 && t + 1 < t1) wait_vmem_n<2 * CHUNKS>();
+      else wait_vmem_n<0>();
+      lds_barrier();
+      if (t + STAGES - 1 < t1) fetch(t + STAGES - 1);
+      step(t);
+    }
+    __syncthreads();
   }
-  if (t < tiles_) step(0, t);
 
   l = half_pair_sum(l);
   if (limit <= 0) {
@@ -444,14 +458,14 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   }
   // the second half's result joins the first's
-  float4* po = (float4*)sh.stage[0][0] + qw * 64 + lane;       // [16][2 waves][64 lanes]: 32 KB
-  float2* pml = (float2*)sh.stage[1][0] + qw * 64 + lane;
-  int* flag = (int*)sh.stage[1][1];
+  float4* po = (float4*)sh.stage[0][0] + qw * 64 + lane;       // [16][HALF][64 lanes]: half of the stages
+  float2* pml = (float2*)sh.stage[STAGES / 2][0] + qw * 64 + lane;
+  int* flag = sh.pages;
   if (tid == 0) *flag = 0;
   __syncthreads();
   if (kw) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) po[128 * i] = float4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+    for (int i = 0; i < 16; ++i) po[64 * HALF * i] = float4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
     *pml = float2{m, l};
     if (bad) *flag = 1;
   }
@@ -465,7 +479,7 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
     float sum = l;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float4 v = po[128 * i];
+      const float4 v = po[64 * HALF * i];
       const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) { o[i >> 2][4 * (i & 3) + e] = o[i >> 2][4 * (i & 3) + e] * w0 + w[e] * w1; sum += o[i >> 2][4 * (i & 3) + e]; }
@@ -486,19 +500,24 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared& 
 }
 
 // The workgroups that have the same number modulo eight share a die and its cache: those of one head, as far as heads go.
-template <bool BF16, int NH, int RTC, int RTO, bool TREE>
-__global__ __launch_bounds__(256, RESIDENT) void paged_shared_kernel(Shares s) {
+template <bool BF16, int NH, int RTC, int RTO, bool TREE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void paged_shared_kernel(Shares s) {
   using S = Shape<BF16, NH>;
-  __shared__ __attribute__((aligned(1024))) union { WideShared wide[BF16 ? 1 : 0]; Shared<S, RTC, 4, PREFIX> common; Shared<S, RTO, 4, SUFFIX> own; } shared;
-  const int head = blockIdx.x % s.a.G;
+  __shared__ __attribute__((aligned(1024))) union {
+    WideShared<WAVES> wide[BF16 ? 1 : 0];
+    Shared<S, RTC, WAVES, PREFIX> common;
+    Shared<S, RTO, WAVES, SUFFIX> own;
+  } shared;
   auto wave = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  const int units = wave(s.plan->units);
+  // one queue for each die that has heads of its own: of every unit, its heads
+  const int queue = blockIdx.x % s.queues, heads = s.a.G / s.queues, units = wave(s.plan->units);
 #pragma unroll 1
-  for (int u = blockIdx.x / s.a.G; u < units;) {
+  for (int64_t i = blockIdx.x / s.queues; i < (int64_t)units * heads;) {
+    const int u = (int)((uint32_t)i / (uint32_t)heads), head = (int)((uint32_t)i % (uint32_t)heads) * s.queues + queue;
     const Unit x = s.units[u];
     // what comes next is asked for now, and known when this unit is done
     int next = 0;
-    if (threadIdx.x == 0) next = __hip_atomic_fetch_add(s.queue + (int64_t)head * QUEUE, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) next = __hip_atomic_fetch_add(s.queue + queue * QUEUE, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const int R = s.a.M * (s.a.H / s.a.G) * wave(x.entries);
     Item item = {};
     item.R = R; item.entries = wave(x.entries);
@@ -506,26 +525,26 @@ __global__ __launch_bounds__(256, RESIDENT) void paged_shared_kernel(Shares s) {
     item.part_row = part * s.a.G + (int64_t)head * R;
     const int b = wave(x.b), slot = wave(x.slot), rb = wave(x.rb), first = wave(x.first), last = wave(x.last), n = wave(x.n);
     if (wave(x.own)) {
-      attend_entry<BF16, NH, RTO, TREE, 4, SUFFIX>(s.a, shared.own, item, b, slot, paged_rows_from(n, wave(x.nt), wave(x.from)), first, last, false, 0,
-                                                   head, rb);
+      attend_entry<BF16, NH, RTO, TREE, WAVES, SUFFIX>(s.a, shared.own, item, b, slot, paged_rows_from(n, wave(x.nt), wave(x.from)), first, last, false, 0,
+                                                       head, rb);
     } else {
       int block = rb, blocks = 1;
       if constexpr (BF16)
         if (is_wide(s, item.entries)) {
-          const bool done = attend_wide(s.a, shared.wide[0], item, b, slot, n, first, last, head, rb);
-          blocks = done ? 0 : WIDE_COLS / (16 * RTC);
-          block = rb * (WIDE_COLS / (16 * RTC));
+          const bool done = attend_wide<WAVES>(s.a, shared.wide[0], item, b, slot, n, first, last, head, rb);
+          blocks = done ? 0 : WAVES / RTC;
+          block = rb * (WAVES / RTC);
         }
 #pragma unroll 1
-      for (int i = 0; i < blocks; ++i) {
+      for (int k = 0; k < blocks; ++k) {
         __syncthreads();
-        attend_entry<BF16, NH, RTC, false, 4, PREFIX>(s.a, shared.common, item, b, slot, paged_rows(n, n, 0, 0), first, last, false, 0, head, block + i);
+        attend_entry<BF16, NH, RTC, false, WAVES, PREFIX>(s.a, shared.common, item, b, slot, paged_rows(n, n, 0, 0), first, last, false, 0, head, block + k);
       }
     }
     __syncthreads();
     if (threadIdx.x == 0) *(int*)&shared = next;
     __syncthreads();
-    u = wave(*(const int*)&shared);
+    i = (uint32_t)wave(*(const int*)&shared);
     __syncthreads();
   }
 }
@@ -587,21 +606,20 @@ __global__ __launch_bounds__(256) void paged_shared_join_kernel(Shares s) {
   else *(f32x4*)((float*)a.o + at) = o;
 }
 
-constexpr int WIDE_FROM = 64;
 constexpr int COMMON_TILES = 2;            // of 16 query rows in a unit of common rows
-int shared_workers(int G) { return G < 256 * RESIDENT ? 256 * RESIDENT / G : 1; }
 
 // A unit has at least 0.8 of what is aimed at (a length of four blocks or more is rounded down), which is at least half of an equal share: cutting adds at most
-// 2.5 units for each worker to those that groups and entries have uncut, and as many query rows to the parts.
+// 2.5 units for each worker to those that groups and entries have uncut, and as many query rows to the parts.  (Workgroups of eight waves are half as many,
+// with twice the query rows.)
 SharedLayout shared_layout(int32_t B, int32_t M, int32_t H, int32_t G) {
-  const int64_t R = (int64_t)M * (H / G), cut = (int64_t)shared_workers(G) * 5 / 2 + 1;
+  const int64_t R = (int64_t)M * (H / G), cut = (int64_t)Work<4>::workgroups * 5 / 2 / G + 4;
   const Tiles own = tiles_of((int)R);
   SharedLayout l;
-  l.max_units = shared_workers(G) + cut + B + (B * R + 16 * COMMON_TILES - 1) / (16 * COMMON_TILES) + cut + (int64_t)B * own.blocks;
-  l.rows = cut * WIDE_COLS + B * R + cut * 16 * own.each + B * R;
+  l.max_units = 2 * cut + B + (B * R + 16 * COMMON_TILES - 1) / (16 * COMMON_TILES) + (int64_t)B * own.blocks;
+  l.rows = cut * Work<4>::cols + B * R + cut * 16 * own.each + B * R;
   size_t at = sizeof(Plan);
   auto take = [&](size_t n) { const size_t o = at; at = (at + n + 255) / 256 * 256; return o; };
-  l.queue = take((size_t)G * QUEUE * sizeof(int32_t));
+  l.queue = take(8 * QUEUE * sizeof(int32_t));
   l.units = take(l.max_units * sizeof(Unit));
   l.where = take(B * sizeof(Where));
   l.ml = take((size_t)l.rows * G * 2 * sizeof(float));
@@ -628,11 +646,25 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   x.a.part = (float*)(at + l.part);
   x.group_first = p.group_first; x.n_shared = p.n_shared; x.groups = p.groups;
   const Tiles own = tiles_of(p.a.M * (p.a.H / p.a.G));
-  x.workers = shared_workers(p.a.G);
+  x.queues = p.a.G % 8 ? 1 : 8;
+  const int64_t in_groups = (int64_t)p.a.B * p.a.M * (p.a.H / p.a.G);
+  const bool stages = bf16 && ((int64_t)p.a.G * tiles::HD * 2 << p.a.c.shift) < (1ll << 32), many = stages && in_groups > (int64_t)Work<8>::cols * p.groups;
+  // Eight waves where a group has on average more query rows than one of their wide units: 64 entries of 1024 query rows in all over 16000 rows, 8 kv heads:
+  // 150 us, 4 waves 179; where they do not pay, 32 entries of 128 in all over 4000 common rows and 700 own: 44 us, 4 waves 37.  Wide units already from 33
+  // query rows on: groups of 40 over 6000 rows, 32 or 40 kv heads: 92 and 81 us, in units of 32 query rows, 113 and 86 (48: as fast).
+  auto work = [&](auto w_) {
+    using W = Work<decltype(w_)::value>;
+    x.waves = decltype(w_)::value;
+    x.workgroups = W::workgroups;
+    x.cost_common = W::common; x.cost_wide = W::wide; x.cost_own = W::own;
+    x.wide = stages ? W::cols : 0;
+  };
+  if (many) work(int_c<8>{});
+  else work(int_c<4>{});
+  x.workers = p.a.G < x.workgroups ? (float)(x.workgroups / p.a.G) : (float)x.workgroups / (float)p.a.G;
   x.common_cols = 16 * COMMON_TILES;
   x.own_blocks = own.blocks;
-  x.wide = bf16 && ((int64_t)p.a.G * tiles::HD * 2 << p.a.c.shift) < (1ll << 32) ? WIDE_FROM : 0;
-  const bool by_wave = p.a.B <= WAVE_ENTRIES && p.groups < WAVE_ENTRIES && (int64_t)p.a.B * p.a.M * (p.a.H / p.a.G) <= WAVE_ROWS && p.a.bound <= WAVE_BOUND;
+  const bool by_wave = p.a.B <= WAVE_ENTRIES && p.groups < WAVE_ENTRIES && in_groups <= WAVE_ROWS && p.a.bound <= WAVE_BOUND;
   {
     ProfScope ps("paged_shared_plan", s);
     if (by_wave) hipLaunchKernelGGL(paged_shared_small_plan_kernel, dim3(1), dim3(64), 0, s, x);
@@ -641,17 +673,18 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   const bool narrow = !bf16 && p.a.d <= 64, tree = p.a.n_true != nullptr;
   {
     ProfScope ps("paged_shared", s);
-    const dim3 grid((unsigned)(x.workers * p.a.G));
-    auto go = [&](auto bf_, auto nh_, auto rt_) {
+    const dim3 grid((unsigned)x.workgroups), wg((unsigned)(64 * x.waves));
+    auto go = [&](auto bf_, auto nh_, auto rt_, auto w_) {
       constexpr bool BF = decltype(bf_)::value != 0;
-      constexpr int NH = decltype(nh_)::value, RT = decltype(rt_)::value;
-      if (tree) hipLaunchKernelGGL((paged_shared_kernel<BF, NH, COMMON_TILES, RT, true>), grid, dim3(256), 0, s, x);
-      else hipLaunchKernelGGL((paged_shared_kernel<BF, NH, COMMON_TILES, RT, false>), grid, dim3(256), 0, s, x);
+      constexpr int NH = decltype(nh_)::value, RT = decltype(rt_)::value, W = decltype(w_)::value;
+      if (tree) hipLaunchKernelGGL((paged_shared_kernel<BF, NH, COMMON_TILES, RT, true, W>), grid, wg, 0, s, x);
+      else hipLaunchKernelGGL((paged_shared_kernel<BF, NH, COMMON_TILES, RT, false, W>), grid, wg, 0, s, x);
     };
-    auto with = [&](auto bf_, auto nh_) { own.each == 1 ? go(bf_, nh_, int_c<1>{}) : go(bf_, nh_, int_c<2>{}); };
-    if (bf16) with(int_c<1>{}, int_c<1>{});
-    else if (narrow) with(int_c<0>{}, int_c<1>{});
-    else with(int_c<0>{}, int_c<2>{});
+    auto with = [&](auto bf_, auto nh_, auto w_) { own.each == 1 ? go(bf_, nh_, int_c<1>{}, w_) : go(bf_, nh_, int_c<2>{}, w_); };
+    if (many) with(int_c<1>{}, int_c<1>{}, int_c<8>{});
+    else if (bf16) with(int_c<1>{}, int_c<1>{}, int_c<4>{});
+    else if (narrow) with(int_c<0>{}, int_c<1>{}, int_c<4>{});
+    else with(int_c<0>{}, int_c<2>{}, int_c<4>{});
   }
   ProfScope ps("paged_shared_join", s);
   auto join = [&](auto bf_, auto hdp_) {
