@@ -201,6 +201,111 @@ def test_page_numbers_outside_the_pool(dtype, H, G, d):
     check_shared(c, queries(rng, 3, 2, H, d, dtype), first, n, dtype)
 
 
+# Groups of many query rows: 4 heads a kv head, one query, so 9 entries have 36 query rows, 50 have 200.
+@pytest.mark.parametrize("entries", [8, 9, 16, 17, 32, 33, 50])
+@pytest.mark.parametrize("rows,page", [(1, 16), (31, 4), (64, 64), (65, 128), (200, 4), (333, 16), (1000, 32)])
+def test_groups_of_many_query_rows(entries, rows, page):
+    rng = np.random.default_rng(entries + rows)
+    c, first, n = branches(rng, [rows], [entries], [int(x) for x in rng.integers(0, 40, entries)], page, 2, 128, "bf16")
+    check_shared(c, queries(rng, entries, 1, 8, 128, "bf16"), first, n, "bf16")
+
+
+@pytest.mark.parametrize("sizes,M", [([40, 3, 0, 25, 1], 2), ([9, 1, 2], 5), ([70, 70], 1)])
+def test_common_rows_that_end_inside_a_tile_for_some(sizes, M):
+    """Few true rows, none, short and empty sequences among the many of a group."""
+    rng = np.random.default_rng(sum(sizes))
+    B = sum(sizes)
+    longest = [500, 70, 64, 130, 33][: len(sizes)]
+    c, first, n = branches(rng, [x for x, k in zip(longest, sizes) if k], [k for k in sizes if k], [int(x) for x in rng.integers(0, 40, B)], 8, 2, 128, "bf16")
+    first, n = [0] + list(np.cumsum(sizes)), longest
+    slots, n_true = list(range(B)), [int(x) for x in rng.integers(-5, 540, B)]
+    for b in range(1, B, 5):
+        slots[b] = int(rng.integers(-1, B + 2))
+    tree = rng.random((B, M, 40)) < 0.4
+    q = queries(rng, B, M, 8, 128, "bf16")
+    check_shared(c, q, first, n, "bf16", slots=slots, n_true=n_true, tree=tree)
+    check_shared(c, q, first, n, "bf16", slots=slots)
+    check_shared(c, q, first, n, "bf16", slots=slots, bound=65)
+
+
+@pytest.mark.parametrize("entries", [12, 40])
+@pytest.mark.parametrize("scale", [1e-30, 3.0, 40.0])
+def test_peaked_and_flat_scores_of_many_query_rows(entries, scale):
+    rng = np.random.default_rng(int(scale))
+    c, first, n = branches(rng, [700], [entries], [int(x) for x in rng.integers(0, 20, entries)], 16, 2, 128, "bf16")
+    check_shared(c, queries(rng, entries, 1, 8, 128, "bf16"), first, n, "bf16", scale=scale)
+
+
+@pytest.mark.parametrize("entries", [12, 40])
+def test_growing_scores_of_many_query_rows(entries):
+    """Every row's score is above all before it, by less and by more than the reference may lag behind."""
+    rng = np.random.default_rng(entries)
+    c, first, n = branches(rng, [600], [entries], [3] * entries, 16, 2, 128, "bf16")
+    q = queries(rng, entries, 1, 8, 128, "bf16")
+    q[:] = np.sign(q)
+    q[1:] = q[:1]
+    k = stored(np.arange(600)[:, None, None] / 150.0 * q[0, 0, ::4][None], "bf16")
+    for (p, r), row in zip(po.rows_of(c, 0, 600), k):
+        c["k"][p, r] = row
+    for scale in (0.02, 0.2, 2.0):
+        check_shared(c, q, first, n, "bf16", scale=scale)
+
+
+@pytest.mark.parametrize("entries", [12, 40])
+def test_what_some_of_many_query_rows_do_not_see(entries):
+    rng = np.random.default_rng(entries)
+    c, first, n = branches(rng, [300], [entries], [5] * entries, 16, 2, 128, "bf16")
+    clean = copy.deepcopy(c)
+    q, n_true = queries(rng, entries, 1, 8, 128, "bf16"), [290] + [int(x) for x in rng.integers(0, 250, entries - 1)]
+    poison(c, po.rows_of(c, 0, 300)[290:])
+    check_shared(c, q, first, n, "bf16", n_true=n_true)
+    poison(c, po.rows_of(c, 0, 300)[250:])
+    got = shared(c, q, first, n, "bf16", n_true=n_true)
+    want = pc.attend_shared(clean, q, first, n, n_true=n_true)
+    check([x[1:] for x in got], [x[1:] for x in want], "bf16", 305)
+    assert torch.isnan(got[0][0]).all()
+    # one infinite value that some see: theirs has no bound there, and nobody else's
+    c = copy.deepcopy(clean)
+    p, r = po.rows_of(c, 0, 300)[100]
+    c["v"][p, r, 1, 7] = -np.inf
+    got = shared(c, q, first, n, "bf16", n_true=n_true)
+    sees = torch.tensor([x > 100 for x in n_true], device=DEV)
+    assert torch.equal(~torch.isfinite(got[0][:, 0, 4:, 7]), sees[:, None].expand(entries, 4))
+    got[0][:, 0, 4:, 7] = 0
+    want[0][:, 0, 4:, 7] = 0
+    check(got, want, "bf16", 305)
+
+
+@pytest.mark.parametrize("entries", [12, 40])
+def test_page_numbers_outside_the_pool_of_many_query_rows(entries):
+    rng = np.random.default_rng(entries)
+    c, first, n = branches(rng, [300], [entries], [5] * entries, 16, 2, 128, "bf16")
+    c["table"][0][2], c["table"][0][5], c["table"][0][18], c["table"][3][17] = -1, len(c["refs"]), 1 << 30, -(1 << 31)
+    check_shared(c, queries(rng, entries, 1, 8, 128, "bf16"), first, n, "bf16")
+
+
+@pytest.mark.parametrize("M,groups", [(36, 700), (130, 300)])
+def test_units_of_more_pages_than_are_held_at_a_time(M, groups):
+    """More groups than workgroups: each takes its 9000 rows of pages of 4 at once.  All groups see the same: one is checked, the others are equal."""
+    rng = np.random.default_rng(M)
+    c = make(rng, [9100], 4, 2275, 2280, 1, 128, "bf16")
+    q = queries(rng, 1, M, 1, 128, "bf16")
+    n_true = [9050]
+    one = pc.attend_shared(c, q, [0, 1], [9000], n_true=n_true)
+    o, lse = shared(c, np.repeat(q, groups, 0), list(range(groups + 1)), [9000] * groups, "bf16", slots=[0] * groups, n_true=n_true * groups)
+    check((o[:1], lse[:1]), one, "bf16", 9100)
+    assert torch.equal(o, o[:1].expand_as(o)) and torch.equal(lse, lse[:1].expand_as(lse))
+
+
+@pytest.mark.parametrize("B,groups,M", [(63, 62, 1), (64, 63, 1), (64, 64, 1), (65, 3, 1), (64, 2, 512), (64, 2, 513), (7, 2, 6000)])
+def test_either_plan(B, groups, M):
+    """On both sides of what one wave plans for."""
+    rng = np.random.default_rng(B + M)
+    c = make(rng, [int(x) for x in rng.integers(0, 70, B)], 8, 10, 700, 1, 128, "bf16")
+    first = [0] + sorted(int(x) for x in rng.integers(0, B, groups - 1)) + [B]
+    check_shared(c, queries(rng, B, M, 1, 128, "bf16"), first, [int(x) for x in rng.integers(0, 90, groups)], "bf16")
+
+
 # ------------------------------------------------------------------ bounds
 def bounds(c, before, slots, dtype, first=None, bound=1 << 20):
     t, handle = on_gpu(c, dtype)
@@ -498,6 +603,29 @@ def test_a_captured_run_replays():
         torch.cuda.synchronize()
         for a, b in zip(results(s), results(eager)):
             assert torch.equal(a, b)
+
+
+def test_two_graphs_with_one_workspace_take_turns():
+    fixed, state, run, results, fill = _calls(np.random.default_rng(32))
+    both, eager = [state(), state()], state()
+    both[1]["ws"] = both[0]["ws"]
+    graphs = []
+    run(both[0])
+    torch.cuda.synchronize()
+    for s in both:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(s)
+    for seed in range(4):
+        for i, (s, graph) in enumerate(zip(both, graphs)):
+            fill(s, 2 * seed + i)
+            graph.replay()
+        for i, s in enumerate(both):
+            fill(eager, 2 * seed + i)
+            run(eager)
+            torch.cuda.synchronize()
+            for a, b in zip(results(s), results(eager)):
+                assert torch.equal(a, b)
 
 
 def test_two_streams_and_the_same_bits_every_time():
