@@ -5,6 +5,7 @@
 // which no <q_r, k_j> of the page exceeds.  An entry's first pages and its last ones are always seen; of those between them a kv
 // head sees the n_select with the highest scores.
 #include "paged_attend.h"
+#include "attn_tiles.h"
 
 namespace beagle {
 namespace {
@@ -61,8 +62,9 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedCache c, int G, 
 // ------------------------------------------------------------------ selection
 // The order of the pages is that of sums in 64 bits, rounded to float; but those are needed only where a page's place is in doubt.  The scores
 // are first taken from matrix instructions, sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c, and are then off by at most E:
-//   32 additions of a piece's products, each off by at most 2^-23 of the magnitudes |q_c x_c| of the piece, and 4 of pieces, by 2^-24 of all,
-//   less than 1.25 * 2^-18 of sum_c |q_c x_c| <= |q|_1 max_c |x_c| together; inputs and sums below 2^-126 may count as zero.
+//   64 additions of a piece's products, each off by at most 2^-23 of the magnitudes |q_c x_c| of the piece, and 4 of pieces, by 2^-24 of all,
+//   less than 1.0625 * 2^-17 of sum_c |q_c x_c| <= |q| |(lo, hi)| together; inputs and sums below 2^-126 may count as zero.
+// (The norms are summed from squares, of which those below 2^-126 may count as zero too, together a norm of less than 2^-58.)
 // With t the n_select-th largest of them, the true one is within E of t: a page above t + 2 E is picked, one below t - 2 E is not, and of those
 // between (most often only the one that t comes from) the true scores are taken where they are more than are still to be picked.
 // Infinities and what is no number make E infinite, and all scores true ones.
@@ -78,6 +80,10 @@ __device__ __forceinline__ Span span_of(const PagedSelectArgs& a, int b) {
   const PagedPick p = paged_pick(n, a.n_true ? a.n_true[b] : INT32_MAX, a.window, a.sinks, a.n_select, a.c.shift);
   return {p.lead, p.listed + p.gap, a.c.table + (int64_t)max(slot, 0) * a.c.W};
 }
+
+// Sixteen pages' bounds of each wave on their way (bf16): sixteen lanes ask for a whole row of 256 bytes.  (Asked for in the order that the matrix instructions
+// take, 64 bytes of each of sixteen rows at a time, 96 heads of 1992 pages took 39 us, not 28.)  Chunk c of row r is at c ^ swz(r).
+struct Staged { u32x4 x[2][SELECT_WAVES][2][16 * 16]; };
 
 template <bool BF16> struct Rows {         // sixteen rows as the matrix instructions take them: lane % 16 is the row, lane / 16 the piece of 16 bytes
   static constexpr int E = BF16 ? 2 : 4, NJ = BF16 ? 4 : 8;
@@ -106,45 +112,43 @@ template <bool BF16> struct Rows {         // sixteen rows as the matrix instruc
       }
     return r;
   }
-  // the largest magnitude of this lane's values, as bits: infinities are above all numbers, what is no number above those
-  __device__ __forceinline__ uint32_t most() const {
-    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-    uint32_t m = 0;
+  // the sum of their squares
+  __device__ __forceinline__ float squares() const {
+    float s[4] = {};
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, x[j][i] & 0x7fff7fffu)));
-        else m = max(m, x[j][i] & 0x7fffffffu);
+        const uint32_t v = x[j][i];
+        if constexpr (BF16) {
+          typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+          s[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v), __builtin_bit_cast(bf16x2, v), s[i], false);
+        } else {
+          s[i] = fmaf(__uint_as_float(v), __uint_as_float(v), s[i]);
+        }
       }
-    return BF16 ? max(m >> 16, m & 0xffffu) << 16 : m;
-  }
-  // the sum of their magnitudes, as bits
-  __device__ __forceinline__ uint32_t sum() const {
-    float s = 0.f;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) s += fabsf(__uint_as_float(x[j][i] << 16)) + fabsf(__uint_as_float(x[j][i] & 0xffff0000u));
-        else s += fabsf(__uint_as_float(x[j][i]));
-      }
-    return __float_as_uint(s) & 0x7fffffffu;
+    return (s[0] + s[1]) + (s[2] + s[3]);
   }
 };
-// (pieces of 32 channels, floats of 16, add up by themselves: less rounding, and no instruction waits for another's sum)
-template <bool BF16> __device__ __forceinline__ f32x4 product(const Rows<BF16>& a, const Rows<BF16>& b) {
-  f32x4 s[Rows<BF16>::NJ];
+// Register e: query row 4 (lane / 16) + e of sixteen, page lane % 16.  (Pieces of 32 channels, floats of 16, add up by themselves: less rounding, and
+// few instructions wait for another's sum.)
+template <bool BF16> __device__ __forceinline__ f32x4 product(const Rows<BF16>& minus, const Rows<BF16>& plus, const Rows<BF16>& lo, const Rows<BF16>& hi) {
+  constexpr int NJ = Rows<BF16>::NJ;
+  f32x4 s[NJ];
 #pragma unroll
-  for (int j = 0; j < Rows<BF16>::NJ; ++j) {
-    s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (BF16) s[j] = mfma_bf16(a.x[j], b.x[j], s[j]);
-    else
+  for (int j = 0; j < NJ; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const Rows<BF16>& q, const Rows<BF16>& x) BEAGLE_INLINE_LAMBDA {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[j] = mfma_f32(__uint_as_float(a.x[j][e]), __uint_as_float(b.x[j][e]), s[j]);
-  }
+    for (int j = 0; j < NJ; ++j)
+      if constexpr (BF16) s[j] = mfma_bf16(q.x[j], x.x[j], s[j]);
+      else
 #pragma unroll
-  for (int n = Rows<BF16>::NJ / 2; n > 0; n /= 2)
+        for (int e = 0; e < 4; ++e) s[j] = mfma_f32(__uint_as_float(q.x[j][e]), __uint_as_float(x.x[j][e]), s[j]);
+  };
+  add(minus, lo);
+  add(plus, hi);
+#pragma unroll
+  for (int n = NJ / 2; n > 0; n /= 2)
 #pragma unroll
     for (int j = 0; j < n; ++j) s[j] += s[j + n];
   return s[0];
@@ -181,7 +185,7 @@ struct Extent { float off, least, most; };
 // Scores of pages [from, to) of the span by matrix instructions, sixteen at a time to each wave.  Returns the wave's share of their extent.
 // (Loops that are not unrolled: all of this runs once or a few times, and instructions that come from memory take longer than they run.)
 template <bool BF16>
-__device__ __forceinline__ Extent score_pages(const PagedSelectArgs& a, const int32_t* table, int b, int g, int from, int to, uint32_t* out) {
+__device__ __forceinline__ Extent score_pages(const PagedSelectArgs& a, Staged* staged, const int32_t* table, int b, int g, int from, int to, uint32_t* out) {
   constexpr int E = BF16 ? 2 : 4, STEP = SELECT_WAVES * 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int rep = a.H / a.G, R = a.M * rep;
@@ -192,63 +196,94 @@ __device__ __forceinline__ Extent score_pages(const PagedSelectArgs& a, const in
     return q;
   };
   const int first = from + wave * 16;
-  auto number_of = [&](int i0) { return i0 + l16 < to ? table[i0 + l16] : -1; };
-  int page = number_of(first);
+  // a lane's number of the wave's next four turns: lane % 16 of turn lane / 16 (behind the end the last page again)
+  auto numbers_of = [&](int i0) { return table[min(i0 + g4 * STEP + l16, to - 1)]; };
+  int numbers = first < to ? numbers_of(first) : -1;
   Rows<BF16> q = query(0), plus = q.part(false), minus = q.part(true);
-  uint32_t most = 0, sum = 0;
+  // What is loaded into registers is waited for here, and where it is loaded: later the wait would be one for requests into LDS, too, that the
+  // compiler does not count.
+  if constexpr (BF16) {
+    asm volatile("" : "+v"(numbers));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(q.x[j]), "+v"(plus.x[j]), "+v"(minus.x[j]));
+  }
+  uint32_t of_pages = 0, of_queries = 0;                     // the largest sums of squares, as bits; what is no number is above all
   Extent x = {0.f, INFINITY, -INFINITY};
   struct Pages { Rows<BF16> lo, hi; bool there; };
-  auto request = [&](Pages& p, int i0) BEAGLE_INLINE_LAMBDA {
-    p.there = (unsigned)page < (unsigned)a.c.P;
-    const addr_t at = (addr_t)a.bounds + ((int64_t)(p.there ? page : 0) * a.G + g) * 2 * a.d * E;
-    page = number_of(i0 + STEP);
-    p.lo.load(at, a.d, p.there);
-    p.hi.load(at + a.d * E, a.d, p.there);
+  auto there = [&](int number) { return (unsigned)number < (unsigned)a.c.P; };
+  const int64_t row_bytes = (int64_t)2 * a.d * E;
+  auto request = [&](int turn, int stage) BEAGLE_INLINE_LAMBDA {                  // (bf16)
+    const uint32_t lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(tiles::lds_void_ptr)staged->x[stage][wave][0]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int number = __shfl(numbers, 16 * (turn & 3) + 4 * j + g4);
+      const addr_t at = (there(number) ? (addr_t)a.bounds + ((int64_t)number * a.G + g) * row_bytes : (addr_t)zero_row) + 16 * (l16 ^ tiles::swz(4 * j + g4));
+      load_to_lds(at, lds + 1024 * j);
+      load_to_lds(at + 256, lds + 4096 + 1024 * j);
+    }
+  };
+  auto take = [&](Pages& p, int page, int stage) BEAGLE_INLINE_LAMBDA {
+    p.there = there(page);
+    if constexpr (BF16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 16 * l16 + ((4 * j + g4) ^ tiles::swz(l16));
+        p.lo.x[j] = staged->x[stage][wave][0][at];
+        p.hi.x[j] = staged->x[stage][wave][1][at];
+      }
+    } else {
+      const addr_t at = (addr_t)a.bounds + ((int64_t)page * a.G + g) * row_bytes;
+      p.lo.load(at, a.d, p.there);
+      p.hi.load(at + a.d * E, a.d, p.there);
+    }
   };
   auto score = [&](const Pages& p, int i0) BEAGLE_INLINE_LAMBDA {
-    uint32_t best[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) best[e] = __float_as_uint(-INFINITY);
+    float best = -INFINITY;
 #pragma unroll 1
     for (int t = 0; t < R; t += 16) {
       if (R > 16) { q = query(t); plus = q.part(false); minus = q.part(true); }
-      if (i0 == first) sum = max(sum, q.sum());              // (while the bounds are on their way)
-      const f32x4 s = product(p.lo, minus) + product(p.hi, plus);
+      if (i0 == first) of_queries = max(of_queries, __float_as_uint(q.squares()) & 0x7fffffffu);   // (while the bounds are on their way)
+      const f32x4 s = product(minus, plus, p.lo, p.hi);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)                            // page 4 g4 + e, query row l16
-        if (t + l16 < R) best[e] = MaxOf()(best[e], __float_as_uint(s[e]));
+      for (int e = 0; e < 4; ++e) best = fmaxf(best, t + 4 * g4 + e < R ? s[e] : -INFINITY);
     }
-    most = max(most, max(p.lo.most(), p.hi.most()));
-    const unsigned long long here = __ballot(p.there);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * g4 + e;
-      const float v = here >> i & 1 ? as_float(over_row(best[e], MaxOf(), R)) : -INFINITY;
-      if (l16 == 0 && i0 + i < to) out[i0 + i] = __float_as_uint(v);
-      x.most = fmaxf(x.most, v);
-      x.least = fminf(x.least, v == -INFINITY ? INFINITY : v);
-    }
+    of_pages = max(of_pages, __float_as_uint(p.lo.squares() + p.hi.squares()) & 0x7fffffffu);
+    best = as_float(over_rows(__float_as_uint(best), MaxOf()));
+    const float v = p.there ? best : -INFINITY;
+    if (g4 == 0 && i0 + l16 < to) out[i0 + l16] = __float_as_uint(v);
+    x.most = fmaxf(x.most, v);
+    x.least = fminf(x.least, v == -INFINITY ? INFINITY : v);
   };
   // (the next sixteen pages travel meanwhile; of floats there is no room for them)
-  Pages now, next;
-  if (BF16 && first < to) request(now, first);
+  if (BF16 && first < to) request(0, 0);
+  int turn = 0;
 #pragma unroll 1
-  for (int i0 = first; i0 < to; i0 += STEP) {
-    if constexpr (BF16) {
-      if (i0 + STEP < to) request(next, i0 + STEP);
-    } else {
-      request(now, i0);
+  for (int i0 = first; i0 < to; i0 += STEP, ++turn) {
+    Pages p;
+    const int page = __shfl(numbers, 16 * (turn & 3) + l16);
+    if ((turn & 3) == 3) {
+      numbers = numbers_of(i0 + STEP);
+      if (BF16) asm volatile("" : "+v"(numbers));
     }
-    score(now, i0);
-    if constexpr (BF16) now = next;
+    if constexpr (BF16) {
+      if (i0 + STEP < to) {
+        request(turn + 1, (turn + 1) & 1);
+        tiles::wait_vmem_n<8>();
+      } else {
+        tiles::wait_vmem();
+      }
+      asm volatile("" ::: "memory");       // (nothing of LDS is read before)
+    }
+    take(p, page, turn & 1);
+    score(p, i0);
   }
-  // (a row's lanes have their largest parts of all tiles: together no less than any query's)
-  const float total = as_float(over_row(over_rows(sum, SumOf()), MaxBits())), magnitude = as_float(over_all(most, MaxBits()));
-  const float size = 4.f * total * magnitude;                // (finite: and so is every sum on the way)
-  x.off = 1.01f * (0x1.4p-20f * size + 0x1p-117f * (total + magnitude + 1.f));
+  // (a row's lanes have their largest parts of all tiles: together no less than any query's, or page's)
+  auto norm = [&](uint32_t squares) { return sqrtf(as_float(over_row(over_rows(squares, SumOf()), MaxBits()))); };
+  const float nq = norm(of_queries), nx = norm(of_pages), size = nq * nx;        // (finite: and so is every sum on the way)
+  x.off = 1.01f * 0x1.1p-17f * (size + 0x1p-58f * (nq + nx) + 0x1p-100f);
   if (!(size < INFINITY && x.off < INFINITY)) x.off = INFINITY;
-  x.least = as_float(over_rows(__float_as_uint(x.least), MinOf()));
-  x.most = as_float(over_rows(__float_as_uint(x.most), MaxOf()));
+  x.least = as_float(over_all(__float_as_uint(x.least), MinOf()));
+  x.most = as_float(over_all(__float_as_uint(x.most), MaxOf()));
   return x;
 }
 
@@ -476,7 +511,7 @@ __device__ __forceinline__ bool picks_all(const PagedSelectArgs& a, const Span& 
 // One workgroup for an entry and head: scores in LDS, and the pages from them.
 template <bool BF16>
 __global__ __launch_bounds__(SELECT_THREADS) void paged_select_kernel(PagedSelectArgs a) {
-  __shared__ PickShared sh;
+  __shared__ union { PickShared pick; Staged staged[BF16 ? 1 : 0]; } sh;
   __shared__ uint32_t scores[SELECT_HELD];
   // Workgroups go round the chip's eight dies.  Heads g, g + 8, .. of one entry on one die would ask for addresses that are alike in their
   // lowest 4 KB, two of the sixteen channels of the die's cache; so each has its heads one behind the other.
@@ -488,8 +523,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void paged_select_kernel(PagedSelec
     const Span span = span_of(a, b);
     int32_t* out = a.pages + (int64_t)bg * a.n_select;
     if (picks_all(a, span, out)) continue;
-    const Extent x = score_pages<BF16>(a, span.table + span.lead, b, g, 0, span.count, scores);
-    pick_pages<BF16, false>(a, sh, span, b, g, scores, x, out);
+    const Extent x = score_pages<BF16>(a, sh.staged, span.table + span.lead, b, g, 0, span.count, scores);
+    if (BF16) __syncthreads();
+    pick_pages<BF16, false>(a, sh.pick, span, b, g, scores, x, out);
   }
 }
 
@@ -497,6 +533,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void paged_select_kernel(PagedSelec
 constexpr int SELECT_CHUNK = 16 * SELECT_WAVES;
 template <bool BF16>
 __global__ __launch_bounds__(SELECT_THREADS) void paged_score_kernel(PagedSelectArgs a, int chunks) {
+  __shared__ u32x4 staged[BF16 ? sizeof(Staged) / 32 : 1];   // (the first half: no wave has a second turn)
   const int b = blockIdx.z;
   const Span span = span_of(a, b);
   for (int g = blockIdx.y; g < a.G; g += gridDim.y)
@@ -504,7 +541,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void paged_score_kernel(PagedSelect
       const int64_t bg = (int64_t)b * a.G + g;
       const int from = chunk * SELECT_CHUNK, to = min(from + SELECT_CHUNK, span.count);
       Extent x = {0.f, INFINITY, -INFINITY};
-      if (span.count > a.n_select && from < to) x = score_pages<BF16>(a, span.table + span.lead, b, g, from, to, a.scores + bg * a.width);
+      if (span.count > a.n_select && from < to) x = score_pages<BF16>(a, (Staged*)staged, span.table + span.lead, b, g, from, to, a.scores + bg * a.width);
       if ((threadIdx.x & 63) == 0) ((Extent*)a.extents)[(bg * chunks + chunk) * SELECT_WAVES + (threadIdx.x >> 6)] = x;
     }
 }
@@ -569,10 +606,10 @@ void launch_paged_select(bool bf16, PagedSelectArgs a, void* ws, hipStream_t s) 
   const int chunks = select_chunks(a.width);
   auto most = [](int64_t n, int64_t limit) { return (unsigned)(n < limit ? n : limit); };
   const dim3 each(most(a.G, 4096), (unsigned)a.B), wg(SELECT_THREADS);
-  // One launch, a workgroup for each entry and head, or two, the first on the whole chip.  Us, one / two launches (1 query, 4 where said): 8 heads of
-  // 500 pages 14.7 / 11.8, of 2000 38.5 / 15.6, 32 heads of 187 pages 10.4 / 12.0, of 2000 38.9 / 22.6, 80 heads of 2000 (4 queries) 40.2 / 37.2, 96
-  // 40.2 / 44.1, 120 39.7 / 50.0, 256 of up to 304 14.4 / 24.0.
-  if (a.width <= SELECT_HELD && heads < (1 << 30) && (heads >= 96 || a.width <= 256)) {
+  // One launch, a workgroup for each entry and head, or two, the first on the whole chip.  Us, one / two launches (1 query, from 64 heads on 4): 8 heads of
+  // 242 pages 9.8 / 10.6, of 492 11.5 / 10.2, of 1992 26.5 / 14.4; 32 heads of 367 pages 10.9 / 10.9, of 1992 27.9 / 21.1; 64 heads of 1992 28.4 / 27.8, 80
+  // 28.4 / 30.7, 96 28.6 / 32.9, 256 50.9 / 72.8, 264 72.6 / 74.3; 256 of up to 304 13.1 / 20.1.
+  if (a.width <= SELECT_HELD && heads < (1 << 30) && (heads >= 72 || a.width <= 256)) {
     ProfScope ps("paged_select", s);
     if (bf16) hipLaunchKernelGGL((paged_select_kernel<true>), dim3(most((heads + 7) / 8 * 8, 65536)), wg, 0, s, a);
     else hipLaunchKernelGGL((paged_select_kernel<false>), dim3(most((heads + 7) / 8 * 8, 65536)), wg, 0, s, a);

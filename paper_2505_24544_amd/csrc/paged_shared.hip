@@ -280,11 +280,6 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
 // number that some queries do not see, and pages that are none, are not looked for: where they show in the result (or a page's number was none),
 // `false` comes back, and the caller has the unit done row by row.
 constexpr int TILE_ROWS = 64;
-// 16 bytes of each lane, in order, to a place in LDS.  Written out, since the compiler takes every later read of LDS for one of what is still on its
-// way and has it wait; who reads it here has waited for it by count, and met the others at a barrier.
-__device__ __forceinline__ void load_to_lds(addr_t from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
-}
 constexpr int NUMBERS = 2048;              // page numbers that are held at a time
 template <int WAVES> struct WideShared { bf16_t stage[Work<WAVES>::stages][2][TILE_ROWS * tiles::HD]; int pages[NUMBERS]; };
 template <int WAVES>
