@@ -389,6 +389,30 @@ def test_equal_and_odd_scores(dtype):
         check_select(c, q, b, 16, 0, n, dtype)
 
 
+@pytest.mark.parametrize("dtype,H,G,d", [("bf16", 8, 2, 128), ("f32", 4, 2, 100)])
+@pytest.mark.parametrize("q_scale,b_scale", [(1e-15, 1e-12), (1e-30, 1e-5), (1e12, 1e15), (1e-10, 1e30), (1e18, 1e18), (1e-38, 1e36)])
+def test_scores_of_any_size(dtype, H, G, d, q_scale, b_scale):
+    """Squares and products that leave a float's range on either side; channels of very different size."""
+    rng = np.random.default_rng(7)
+    c = make(rng, [3000, 1200], 8, 380, 530, G, d, dtype)
+    q, b = queries(rng, 2, 2, H, d, dtype) * q_scale, bounds_of(c) * b_scale
+    q, b = stored(q, dtype), stored(b, dtype)
+    check_select(c, q, b, 16, 4, 60, dtype)
+    b[::2, :, :, ::9] *= 2.0 ** -20
+    q[:, :, 1] *= 2.0 ** -30
+    check_select(c, stored(q, dtype), stored(b, dtype), 16, 4, 60, dtype)
+
+
+@pytest.mark.parametrize("B,G,rows", [(9, 8, 530), (3, 2, 5000), (1, 1, 66000)])
+def test_either_way_of_selection(B, G, rows):
+    """A launch for all heads, or two, with fewer and more pages than a workgroup holds, whole and in part."""
+    rng = np.random.default_rng(B)
+    c = make(rng, [rows - 37 * b for b in range(B)], 8, rows // 8 + 2, B * rows // 8 + 8, G, 128, "bf16")
+    b = stored(np.abs(rng.standard_normal((len(c["refs"]), G, 2, 128))) * [[-1.0], [1.0]], "bf16")
+    for M, n in ((1, 3), (5, 33)):
+        check_select(c, queries(rng, B, M, 4 * G, 128, "bf16"), b, 64, 4, n, "bf16")
+
+
 def test_many_query_rows_and_pages():
     rng = np.random.default_rng(6)
     c = make(rng, [2600, 131], 4, 700, 720, 1, 128, "bf16")
