@@ -3,6 +3,11 @@
 //
 //   over rows P (common) and T (own):  m = max(m_P, m_T),  l = l_P 2^(m_P - m) + l_T 2^(m_T - m),  o = (o_P 2^(m_P - m) + o_T 2^(m_T - m)) / l
 //
+// Bound: the rows' bytes where groups have few query rows, their products where many (see attend_wide); of little work the three launches and their trips to
+// memory, some 14 us.  Measured (MI355X, bf16, a graph's replays): 12 entries of 10 queries under a tree, 40 heads, 3 groups of up to 6000 common rows, up to
+// 500 own (340 MB) 94 us, its second launch 81 at 4.2 TB/s; 32 entries of a query, 32 / 8 heads, 4000 common, up to 700 own (69 MB) 31.5 us, its second launch 21.
+// Each entry by itself they would read 1.0 and 0.6 GB.
+//
 // Three launches.  The first, one workgroup, divides the work into units: some blocks of 32 rows for a few tiles of 16 query rows, of a
 // group's common rows or of an entry's own.  In the second as many workgroups as fit take units, those that are done take more; each unit
 // leaves its sums in the workspace, in a place of its own.  The third joins every query row's sums in the order of the rows.
@@ -300,8 +305,12 @@ __global__ __launch_bounds__(64) void paged_shared_small_plan_kernel(Shares s) {
 // Common rows for 64 or 128 query rows of a group that has more of them (bf16): tiles of 64 rows go through a ring of LDS stages; half of the waves
 // take 32 query rows each against a tile's first half, half of them against its second.  As the training forward, but for the scale in two parts,
 // rows that come from pages, and probabilities in three terms that add up to them exactly (see attend_entry).  Infinite values, rows with what is no
-// number that some queries do not see, and pages that are none, are not looked for: where they show in the result (or a page's number was none),
-// `false` comes back, and the caller has the unit done row by row.
+// number that some queries do not see, values that leave a float's range times a probability above one, and pages that are none, are not looked for: where
+// they show in the result, which is not finite then (or a page's number was none), `false` comes back, and the caller has the unit done row by row.
+//
+// Bound by the matrix pipe: four products of d for a row and query, 134 G (multiplications and additions) for 64 entries of 4 queries of 32 heads over 16000
+// common rows of 8 kv heads.  These take 149 us with the other two launches' 13: 0.98 of the 1.20 PFLOP/s that a product of 8192^3 reaches.
+// (Four waves, 64 query rows, two stages: 179 us.)
 constexpr int TILE_ROWS = 64;
 constexpr int NUMBERS = 2048;              // page numbers that are held at a time
 template <int WAVES> struct WideShared { bf16_t stage[Work<WAVES>::stages][2][TILE_ROWS * tiles::HD]; int pages[NUMBERS]; };
@@ -502,7 +511,7 @@ __device__ __forceinline__ bool attend_wide(const PagedAttnArgs& a, WideShared<W
 #pragma unroll
       for (int e = 0; e < 4; ++e) { o[i >> 2][4 * (i & 3) + e] = o[i >> 2][4 * (i & 3) + e] * w0 + w[e] * w1; sum += o[i >> 2][4 * (i & 3) + e]; }
     }
-    if (bad || (r < R && !(sum == sum))) *flag = 1;            // (an infinite sum of both signs, too)
+    if (bad || (r < R && !(fabsf(sum) < INFINITY))) *flag = 1;
   }
   __syncthreads();
   const bool whole = *flag == 0;

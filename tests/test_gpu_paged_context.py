@@ -251,6 +251,21 @@ def test_growing_scores_of_many_query_rows(entries):
         check_shared(c, q, first, n, "bf16", scale=scale)
 
 
+@pytest.mark.parametrize("entries", [8, 12, 40])
+def test_the_largest_values_of_many_query_rows(entries):
+    """The row with the largest values is a hundred times as probable as those before it: times that they leave a float's range."""
+    rng = np.random.default_rng(entries)
+    c, first, n = branches(rng, [300], [entries], [5] * entries, 16, 2, 128, "bf16")
+    q = np.sign(queries(rng, 1, 1, 8, 128, "bf16"))
+    q[:, :, 1:4], q[:, :, 5:] = q[:, :, :1], q[:, :, 4:5]
+    for b in range(entries):
+        for p, r in po.rows_of(c, b, 305):
+            c["k"][p, r] = 0.0
+    p, r = po.rows_of(c, 0, 300)[200]
+    c["k"][p, r], c["v"][p, r] = stored(q[0, 0, ::4] * (4.8 / 128), "bf16"), stored(np.full((2, 128), 3e38), "bf16")
+    check_shared(c, np.repeat(q, entries, 0), first, n, "bf16", scale=1.0)
+
+
 @pytest.mark.parametrize("entries", [12, 40])
 def test_what_some_of_many_query_rows_do_not_see(entries):
     rng = np.random.default_rng(entries)
