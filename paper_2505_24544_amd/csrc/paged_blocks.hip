@@ -72,8 +72,8 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedCache c, int G, 
 // Infinities and what is no number make E infinite, and all scores true ones.
 //
 // Bound: the bounds' bytes, and of little work the chain of a launch, lengths, page numbers, bounds, and the picking (some 4 us).  Measured (MI355X, bf16, a graph's
-// replays): 160 heads of up to 1008 pages, 10 queries (61 MB) 22 us, 256 heads of up to 304 pages, 4 queries (23 MB) 13, 32 heads of 179 pages 9.5.  With all scores in 64 bits the
-// first of these took 120 us, the second 102: the vector pipe's double rate.
+// replays): 160 heads of up to 1008 pages, 10 queries (61 MB) 22 us, 256 heads of up to 304 pages, 4 queries (23 MB) 13, 32 heads of 179 pages 9.5.  With
+// all scores in 64 bits the first took 120 us, the second 102: the vector pipe's double rate.
 constexpr int SELECT_THREADS = 512, SELECT_WAVES = SELECT_THREADS / 64;
 constexpr int SELECT_HELD = 8192;          // scores that a workgroup holds
 constexpr int SELECT_LISTED = 240;         // pages in doubt that are kept in a list (times 2^24 query rows: 32 bits)
