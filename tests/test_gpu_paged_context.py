@@ -210,7 +210,7 @@ def test_groups_of_many_query_rows(entries, rows, page):
     check_shared(c, queries(rng, entries, 1, 8, 128, "bf16"), first, n, "bf16")
 
 
-@pytest.mark.parametrize("sizes,M", [([40, 3, 0, 25, 1], 2), ([9, 1, 2], 5), ([70, 70], 1)])
+@pytest.mark.parametrize("sizes,M", [([40, 3, 0, 25, 1], 2), ([9, 1, 2], 5), ([70, 70], 1), ([30, 12], 6), ([2, 1], 40)])
 def test_common_rows_that_end_inside_a_tile_for_some(sizes, M):
     """Few true rows, none, short and empty sequences among the many of a group."""
     rng = np.random.default_rng(sum(sizes))
