@@ -84,11 +84,12 @@ __device__ __forceinline__ Group group_of(const Shares& s, const int* first, int
   return r;
 }
 // What a unit is to take: so much that each worker has one, or of long work two, so that those who are done early have something to take.  (Cutting n items
-// into equal lengths makes half a unit more of each.)
+// into equal lengths makes half a unit more of each; but no unit takes a third more than an equal share: 64 entries of 700 own rows behind 4000 common ones
+// 57 us with twice a share, 52 so, 256 in 4 groups 149 / 137.)
 constexpr float LONG = 240.f;
 __device__ __forceinline__ float aimed(float work, float items, float workers) {
   const float units = work > LONG * workers ? 2.f * workers : workers;
-  return work / fmaxf(units - 0.5f * items, 0.5f * workers);
+  return work / fmaxf(units - 0.5f * items, 0.75f * workers);
 }
 // units of up to `aim` that so many blocks are cut into
 __device__ __forceinline__ int cuts_of(int blocks, float aim, int cost, int least) {
@@ -675,9 +676,11 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   const Tiles own = tiles_of(p.a.M * (p.a.H / p.a.G));
   x.queues = p.a.G % 8 ? 1 : 8;
   const int64_t in_groups = (int64_t)p.a.B * p.a.M * (p.a.H / p.a.G);
-  const bool stages = bf16 && ((int64_t)p.a.G * tiles::HD * 2 << p.a.c.shift) < (1ll << 32), many = stages && in_groups > (int64_t)Work<8>::cols * p.groups;
-  // Eight waves where a group has on average more query rows than one of their wide units: 64 entries of 1024 query rows in all over 16000 rows, 8 kv heads:
-  // 150 us, 4 waves 179; where they do not pay, 32 entries of 128 in all over 4000 common rows and 700 own: 44 us, 4 waves 37.  Wide units already from 33
+  const bool stages = bf16 && ((int64_t)p.a.G * tiles::HD * 2 << p.a.c.shift) < (1ll << 32);
+  const bool many = stages && in_groups > (int64_t)Work<8>::cols * p.groups && in_groups * p.a.bound > (int64_t)(3 << 20) * p.groups;
+  // Eight waves where a group has on average more query rows than one of their wide units, and those times the rows that a sequence can have pass 3 * 2^20 (8 kv
+  // heads, us with 8 / 4 waves): 1024 query rows over 16000 rows 150 / 179, over 4000 65 / 74, 256 over 16000 74 / 78; 512 over 4000 58 / 49, 1024 over
+  // 2000 52 / 45, 128 over 4000 44 / 37: there the entries' own rows are as much, whose units are better small and many.  Wide units already from 33
   // query rows on: groups of 40 over 6000 rows, 32 or 40 kv heads: 92 and 81 us, in units of 32 query rows, 113 and 86 (48: as fast).
   auto work = [&](auto w_) {
     using W = Work<decltype(w_)::value>;
