@@ -127,6 +127,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   __shared__ int tops[PLAN_THREADS / 64];
   __shared__ int base[PLAN_THREADS + 1];   // units before each of the groups, or entries, at hand
   __shared__ int64_t rows[PLAN_THREADS];
+  __shared__ union { Group group[PLAN_THREADS]; Own own[PLAN_THREADS]; } held;       // those at hand
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t R = (int64_t)s.a.M * (s.a.H / s.a.G);
   // the groups' first entries, each at least the one before
@@ -143,13 +144,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   }
   // what there is to do, and from it what a unit is to take
   int64_t mine = 0, items = 0, work, sum;
+  const Group group0 = group_of(s, first, tid);              // (in most calls all that there are)
+  const Own own0 = own_of(s, first, tid);
   for (int g = tid; g < s.groups; g += PLAN_THREADS) {
-    const Group x = group_of(s, first, g);
+    const Group x = g == tid ? group0 : group_of(s, first, g);
     mine += (int64_t)x.blocks * x.cols * cost_of(s, x.entries);
     items += x.cols;
   }
   for (int b = tid; b < s.a.B; b += PLAN_THREADS) {
-    const int n = own_of(s, first, b).blocks;
+    const int n = b == tid ? own0.blocks : own_of(s, first, b).blocks;
     mine += (int64_t)n * s.own_blocks * s.cost_own;
     items += n ? s.own_blocks : 0;
   }
@@ -161,7 +164,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   int units = 0;
   int64_t parts = 0;
   for (int g0 = 0; g0 < s.groups; g0 += PLAN_THREADS) {
-    const Group x = group_of(s, first, g0 + tid);
+    const Group x = g0 == 0 ? group0 : group_of(s, first, g0 + tid);
+    held.group[tid] = x;
     const int cuts = cuts_of(x.blocks, aim, cost_of(s, x.entries), s.waves);
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * x.cols, tmp, &all), row = sum_before(cuts * x.entries * R, tmp, &sum);
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     // units of each group: cut after cut of its rows, those of a cut one behind the other
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
-      const Group y = group_of(s, first, g0 + i);
+      const Group y = held.group[i];
       const int n = cuts_of(y.blocks, aim, cost_of(s, y.entries), s.waves), cut = (u - base[i]) / y.cols;
       s.units[units + u] = Unit{0, y.lo, y.slot, (u - base[i]) % y.cols, cut_at(y.blocks, cut, n, false), cut_at(y.blocks, cut + 1, n, false),
                                 y.n, y.n, 0, y.entries, rows[i] + cut * y.entries * R};
@@ -179,7 +183,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     const int last = min(g0 + PLAN_THREADS, s.groups);
     for (int b = first[g0] + tid; b < first[last]; b += PLAN_THREADS) {
       const int g = group_with(first, s.groups, b);
-      const Group y = group_of(s, first, g);
+      const Group y = held.group[g - g0];
       Where* w = s.where + b;
       w->common = rows[g - g0]; w->stride = (int)(y.entries * R); w->offset = (int)((b - y.lo) * R);
       w->n_common = cuts_of(y.blocks, aim, cost_of(s, y.entries), s.waves);
@@ -189,7 +193,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
   }
   for (int b0 = 0; b0 < s.a.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
-    const Own x = own_of(s, first, b);
+    const Own x = b0 == 0 ? own0 : own_of(s, first, b);
+    held.own[tid] = x;
     const int cuts = cuts_of(x.blocks, aim, s.cost_own, s.waves);
     int64_t all;
     const int64_t at = sum_before((int64_t)cuts * s.own_blocks, tmp, &all), row = sum_before(cuts * R, tmp, &sum);
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
     __syncthreads();
     for (int u = tid; u < (int)all; u += PLAN_THREADS) {
       const int i = group_with(base, PLAN_THREADS, u);
-      const Own y = own_of(s, first, b0 + i);
+      const Own y = held.own[i];
       const int n = cuts_of(y.blocks, aim, s.cost_own, s.waves), cut = (u - base[i]) / s.own_blocks;
       s.units[units + u] = Unit{1, b0 + i, y.slot, (u - base[i]) % s.own_blocks, cut_at(y.blocks, cut, n, true), cut_at(y.blocks, cut + 1, n, true),
                                 y.n, y.nt, y.from, 1, rows[i] + cut * R};
