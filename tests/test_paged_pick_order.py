@@ -1,0 +1,61 @@
+"""The picking of pages (CPU): its code in a host build, where a workgroup's waves run in any order between two barriers, against a
+plain ranking.  An order that changes the pages, waves that meet at different barriers and writes outside the list all show."""
+import os
+import random
+import shutil
+import struct
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ORDERS = (-1, -2, 1)                       # the first wave first, the last one, any
+
+
+@pytest.fixture(scope="module")
+def pick(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no host C++ compiler")
+    exe = str(tmp_path_factory.mktemp("pick") / "paged_pick_order_driver")
+    r = subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-Wno-unknown-pragmas",
+                        os.path.join(HERE, "paged_pick_order_driver.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+    def run(n_select, off, scores, truth, *, lead=3, rows=2, memory=0, order=-1):
+        text = "%d %d %d %d %d %d %r\n" % (len(scores), n_select, lead, rows, memory, order, off)
+        text += "\n".join("%r %r" % p for p in zip(scores, truth))
+        env = dict(os.environ)
+        env.pop("LD_PRELOAD", None)
+        r = subprocess.run([exe], input=text + "\n", capture_output=True, text=True, env=env, timeout=120)
+        assert r.returncode == 0, r.stderr[-4000:]
+        assert not r.stdout.startswith("wrong"), r.stdout
+        return [int(v) for v in r.stdout.split()]
+    return run
+
+
+def f32(x):
+    return struct.unpack("f", struct.pack("f", x))[0]
+
+
+def ranked(truth, n_select, lead=3):
+    return sorted(i + lead for i in sorted(range(len(truth)), key=lambda i: (-truth[i], i))[:n_select])
+
+
+def near(rng, truth, off):
+    """Scores that are off by less than `off`."""
+    return [f32(t + 0.9 * off * rng.uniform(-1, 1)) for t in truth]
+
+
+def check(pick, truth, scores, n_select, off, **kw):
+    for order in ORDERS:
+        assert pick(n_select, off, scores, truth, order=order, **kw) == ranked(truth, n_select), (n_select, off, kw, order)
+
+
+@pytest.mark.parametrize("memory", [0, 1])
+@pytest.mark.parametrize("n,n_select", [(2, 1), (65, 64), (513, 40), (3001, 700)])
+def test_the_largest_scores(pick, memory, n, n_select):
+    rng = random.Random(n)
+    truth = [f32(rng.uniform(1, 9)) for _ in range(n)]
+    check(pick, truth, near(rng, truth, 0.01), n_select, 0.01, memory=memory)
+    check(pick, truth, truth, n_select, 1e-6, memory=memory, rows=1)
