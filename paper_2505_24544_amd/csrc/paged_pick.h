@@ -175,6 +175,7 @@ __device__ __forceinline__ void pick_pages(PickShared& sh, int n, int n_select, 
       const float v = as_float(scores[i]);
       if (all || !doubtful(v)) scores[i] = v > top || doubtful(v) ? PICKED : 0u;
     }
+    if (!all) __syncthreads();                               // (every score has been read: a zero written now would pass for one)
     if (!all && tid < listed) {                              // how many of the others come before it
       const uint32_t mine = sh.best[tid];
       const int at = sh.list[tid];
@@ -218,7 +219,7 @@ __device__ __forceinline__ void pick_pages(PickShared& sh, int n, int n_select, 
     auto of = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
     const int before = taken + of(upto - level, wave), tie = before + __popcll(eq & lower);
     const int at = written + of(sum - more, wave) + __popcll(gt & lower) + max(min(tie, (int)ties) - min(before, (int)ties), 0);
-    if (here && (k > last || (k == last && tie < (int)ties))) out[at] = lead + i0 + tid;
+    if (here && (k > last || (k == last && tie < (int)ties)) && at < n_select) out[at] = lead + i0 + tid;     // (there are n_select of them)
     written += of(sum, SELECT_WAVES - 1);
     taken += of(upto, SELECT_WAVES - 1);
     __syncthreads();

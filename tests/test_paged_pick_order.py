@@ -59,3 +59,16 @@ def test_the_largest_scores(pick, memory, n, n_select):
     truth = [f32(rng.uniform(1, 9)) for _ in range(n)]
     check(pick, truth, near(rng, truth, 0.01), n_select, 0.01, memory=memory)
     check(pick, truth, truth, n_select, 1e-6, memory=memory, rows=1)
+
+
+@pytest.mark.parametrize("memory", [0, 1])
+@pytest.mark.parametrize("n,n_select,doubt", [(600, 100, 3), (2000, 333, 40), (9000, 700, 150), (700, 690, 8)])
+def test_scores_below_zero(pick, memory, n, n_select, doubt):
+    """The last page picked has a score below zero, and some before and behind it are in doubt."""
+    rng = random.Random(n + doubt)
+    truth = [f32(-100.0 + rng.uniform(0, 90)) for _ in range(n)]
+    order = sorted(range(n), key=lambda i: -truth[i])
+    for k in order[max(n_select - doubt // 2, 0): n_select + doubt - doubt // 2]:      # closer to each other than can be told
+        truth[k] = f32(truth[order[n_select]] + rng.uniform(-1e-3, 1e-3))
+    for off in (2e-3, 1e-6):
+        check(pick, truth, near(rng, truth, off), n_select, off, memory=memory)
