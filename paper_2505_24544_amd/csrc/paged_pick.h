@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 
 struct PickShared {
   uint32_t count[256], state[2];
-  int sure, listed, list[SELECT_LISTED];
+  int sure, listed, here, list[SELECT_LISTED];
   uint32_t best[SELECT_LISTED];
   int found[SELECT_WAVES];
   Extent x[SELECT_WAVES];
@@ -145,8 +145,8 @@ __device__ __forceinline__ void pick_pages(PickShared& sh, int n, int n_select, 
   constexpr uint32_t PICKED = 0xffffffffu;
   auto meet = [&] { if constexpr (MEMORY) hand_over(); else __syncthreads(); };
   auto doubtful = [&](float v) { return !(v > top) && !(v < low); };
-  auto list = [&](int i) {
-    const int at = atomicAdd(&sh.listed, 1);
+  auto list = [&](int* count, int i) {
+    const int at = atomicAdd(count, 1);
     if (at < SELECT_LISTED) { sh.list[at] = i; sh.best[at] = key_of(-INFINITY); }
   };
   auto take_true_scores = [&](int listed) {                  // a page of the list and a query row to sixteen lanes
@@ -162,7 +162,7 @@ __device__ __forceinline__ void pick_pages(PickShared& sh, int n, int n_select, 
   for (int i = tid; i < n; i += SELECT_THREADS) {
     const float v = as_float(scores[i]);
     if (v > top) atomicAdd(&sh.sure, 1);
-    if (doubtful(v)) list(i);
+    if (doubtful(v)) list(&sh.listed, i);
   }
   __syncthreads();
   const int listed = sh.listed, wanted = n_select - sh.sure;      // in doubt, and how many of them are picked
@@ -187,18 +187,19 @@ __device__ __forceinline__ void pick_pages(PickShared& sh, int n, int n_select, 
     meet();
   } else {
     // too many for a list: piece by piece they take their true scores, and the last key is looked for among all
+    // (each piece has a count of its own: a wave may still have to read the first one)
 #pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += SELECT_LISTED) {
       const int i = i0 + tid;
-      if (tid == 0) sh.listed = 0;
+      if (tid == 0) sh.here = 0;
       __syncthreads();
       if (tid < SELECT_LISTED && i < n) {
         const float v = as_float(scores[i]);
-        if (doubtful(v)) list(i);
+        if (doubtful(v)) list(&sh.here, i);
         else scores[i] = v > top ? PICKED : 0u;
       }
       __syncthreads();
-      const int here = sh.listed;
+      const int here = sh.here;
       take_true_scores(here);
       if (tid < here) scores[sh.list[tid]] = sh.best[tid];
     }

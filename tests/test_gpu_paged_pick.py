@@ -45,3 +45,24 @@ def test_scores_below_zero(B, G, pages, dtype, d):
         q2, b2 = q.copy(), b.copy()
         in_doubt(rng, c, q2, b2, n_select, many)
         check_select(c, stored(q2, dtype), stored(b2, dtype), 0, 0, n_select, dtype)
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("B,G,pages", SIZES[1:])
+def test_many_in_doubt(B, G, pages, dtype, d):
+    """More pages in doubt than a list holds: equal scores on both sides of the last one picked, and what takes the error's bound away."""
+    rng = np.random.default_rng(pages + 1)
+    c, q, b = leaning(rng, B, G, pages, d, dtype)
+    kinds = b[rng.integers(0, 17, len(b))]                   # seventeen scores below zero, hundreds of pages of each
+    for n_select in (1, pages // 17, pages // 2, pages - 3):
+        check_select(c, q, kinds, 0, 0, n_select, dtype)
+    check_select(c, q, np.zeros_like(b), 8, 4, pages // 3, dtype)
+    check_select(c, -q, kinds, 0, 0, pages // 2, dtype)
+    odd = b.copy()
+    odd[::401, :, 0, 3] = -np.inf                            # (a least value that no query above zero meets)
+    for n_select in (5, pages // 3):
+        check_select(c, q, odd, 0, 0, n_select, dtype)
+    odd[::7, :, 1, 2], odd[1::5, :, 1, 0], odd[2::9, :, 1] = np.nan, np.inf, np.nan
+    c["table"][0][11], c["table"][0][pages - 20] = -1, 1 << 20
+    for n_select in (pages // 9, pages - 30):
+        check_select(c, q, odd, 0, 0, n_select, dtype)

@@ -72,3 +72,29 @@ def test_scores_below_zero(pick, memory, n, n_select, doubt):
         truth[k] = f32(truth[order[n_select]] + rng.uniform(-1e-3, 1e-3))
     for off in (2e-3, 1e-6):
         check(pick, truth, near(rng, truth, off), n_select, off, memory=memory)
+
+
+@pytest.mark.parametrize("memory", [0, 1])
+@pytest.mark.parametrize("n,n_select,alike", [(300, 50, 241), (1000, 400, 1000), (1200, 700, 600), (9000, 300, 2500)])
+def test_many_in_doubt(pick, memory, n, n_select, alike):
+    """More pages in doubt than a list holds: equal scores, an error without a bound, scores below zero and of both signs."""
+    rng = random.Random(n + alike)
+    for low, high in ((1, 9), (-9, -1), (-5, 5)):
+        truth = [f32(rng.uniform(low, high)) for _ in range(n)]
+        check(pick, truth, near(rng, truth, 0.5), n_select, float("inf"), memory=memory, rows=1)
+        at = sorted(truth, reverse=True)[n_select - 1]
+        for i in rng.sample(range(n), alike):
+            truth[i] = at
+        check(pick, truth, near(rng, truth, 1e-4), n_select, 1e-4, memory=memory, rows=1)
+
+
+@pytest.mark.parametrize("memory", [0, 1])
+def test_no_scores_at_all(pick, memory):
+    none = [float("-inf")] * 700
+    check(pick, none, none, 300, 1e-3, memory=memory)
+    check(pick, none, none, 300, float("inf"), memory=memory)
+    some = none[:]
+    some[5], some[650], some[651] = -3.0, -2.0, float("inf")
+    check(pick, some, some, 2, float("inf"), memory=memory)
+    some[651] = -4.0
+    check(pick, some, some, 300, 1e-3, memory=memory)
