@@ -82,8 +82,9 @@ __device__ __forceinline__ float max_over_keys(float v) {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // 16 bytes of each lane, in order, to a place in LDS.  Written out, since the compiler takes every later read of LDS for one of what is still on its
 // way and has it wait; who reads it here has waited for it by count, and met the others at a barrier if it is another wave's.
+// (The place goes into m0 as an operand: the compiler's own requests keep theirs there, and have to know.)
 __device__ __forceinline__ void load_to_lds(addr_t from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
