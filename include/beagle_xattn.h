@@ -781,9 +781,10 @@ beagle_status beagle_xattn_paged_attend_shared(const beagle_xattn_desc* desc, co
  * tail on, or listed for the head; drafted rows as the tree says.  (window and
  * sinks so count in whole pages here, and window = 0 is none: only the page that
  * the true rows end in.)  A list is ascending; its first min(n_select, max(tail -
- * lead, 0)) numbers are read, and one that is not above the number before it, or not a page that
- * is there to be picked, lists nothing.  It may come from beagle_xattn_paged_select, of this or of
- * an earlier set of queries, or from the caller.
+ * lead, 0)) numbers are read, and one that is not above the number before it, not above every page
+ * before it that is there to be picked, or no such page itself, lists nothing; so no page counts
+ * twice.  It may come from beagle_xattn_paged_select, of this or of an earlier set of queries, or
+ * from the caller.
  *   in : as beagle_xattn_paged_attend; pages [B,G,n_select] DEVICE
  *   out: o [B,M,H,d], lse [B,H,M] float
  * Workspace: BEAGLE_WS_PAGED_BLOCKS.

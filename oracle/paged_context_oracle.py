@@ -150,11 +150,13 @@ def attend_blocks(cache, q, pages, window, sinks, *, slots=None, n_true=None, tr
             n = _held(cache, s, bound)
             nt = _true(n, n_true, b)
             lead, tail = span(nt, window, sinks, page)
-            cols, before = [i for i in range(po.pages_of(nt, page)) if i < lead or i >= tail], -1
+            cols, before, most = [i for i in range(po.pages_of(nt, page)) if i < lead or i >= tail], -1, -1
             for i in list(pages[b][g])[: tail - lead]:
-                if i > before and lead <= i < tail:
+                if i > before and lead <= i < tail and i > most:
                     cols.append(i)
                 before = i
+                if lead <= i < tail:
+                    most = max(most, i)
             mine = po.rows_of(cache, s, n) if n else []
             ids = [j for i in cols for j in range(i * page, min(nt, (i + 1) * page))] + _drafted(tree, b, m, nt, n)
             seen[b, m, g] = [mine[j] for j in ids if mine[j] is not None]

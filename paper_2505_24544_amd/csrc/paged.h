@@ -101,5 +101,14 @@ __device__ __forceinline__ int sum_upto(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
+// Inclusive maximum over the lanes, of numbers from 0 on.
+__device__ __forceinline__ int max_upto(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+}
 
 }  // namespace beagle

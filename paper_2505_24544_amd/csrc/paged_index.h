@@ -62,18 +62,24 @@ PAGED_HD PagedRows paged_picked_rows(const PagedPick& p, int n, int nt, int shif
   const int hidden = p.gap << shift;
   return paged_rows(n - hidden, paged_max(paged_min(paged_max(nt, 0), n) - hidden, 0), 0, 0);
 }
-// page number at place i of the pages seen; -1 where the list names no page that stands between the others and behind the one before it
-PAGED_HD int paged_picked_page(const PagedPick& p, const int32_t* list, const int32_t* table, int i, int n_pages) {
+// number `at` of the list of n_list; -1 where there is none, or none that stands between the others and behind the one before it
+PAGED_HD int paged_listed(const PagedPick& p, const int32_t* list, int at, int n_list) {
+  const int in = paged_max(paged_min(at, n_list - 1), 0);              // (no branch: a lane without a place reads one for nothing)
+  const int col = list[in], before = list[paged_max(in - 1, 0)];
+  return in == at && at < p.listed && (at == 0 || col > before) && col >= p.lead && col < p.lead + p.listed + p.gap ? col : -1;
+}
+// a number as what the ones behind it have to be above, to list a page that is not listed yet
+PAGED_HD int paged_at_least(const PagedPick& p, int col) { return col >= p.lead && col < p.lead + p.listed + p.gap ? col : -1; }
+// page number at place i of the pages seen, whose number in the list is `col` (not read elsewhere); -1 where the list names no page
+PAGED_HD int paged_picked_page(const PagedPick& p, int col, const int32_t* table, int i, int n_pages) {
   const int at = i - p.lead;
-  const bool from_list = at >= 0 && at < p.listed;
-  int col = i + (at >= p.listed ? p.gap : 0);
-  if (from_list) {
-    col = list[at];
-    const int before = at > 0 ? list[at - 1] : -1;
-    if (col <= before || col < p.lead || col >= p.lead + p.listed + p.gap) return -1;
-  }
-  const int number = table[col];
-  return (unsigned)number < (unsigned)n_pages ? number : -1;
+  if (at < 0 || at >= p.listed) col = i + (at >= p.listed ? p.gap : 0);
+  const int number = table[paged_max(col, 0)];
+  return col >= 0 && (unsigned)number < (unsigned)n_pages ? number : -1;
+}
+// (both, for a place by itself)
+PAGED_HD int paged_picked_page(const PagedPick& p, const int32_t* list, const int32_t* table, int i, int n_pages) {
+  return paged_picked_page(p, p.listed > 0 ? paged_listed(p, list, i - p.lead, p.listed) : -1, table, i, n_pages);
 }
 
 // The rows of an entry from row `from` of its true ones on

@@ -221,14 +221,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void paged_shared_plan_kernel(Shares 
 
 // The same by one wave, where everything is counted in 32 bits: lane b has entry b, lane g group g.
 constexpr int WAVE_ENTRIES = 64, WAVE_ROWS = 1 << 15, WAVE_BOUND = 1 << 20;      // entries (and groups: one less), query rows of all, rows of a sequence
-__device__ __forceinline__ int max_upto(int v) {             // (of numbers from 0 on)
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
-  return max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
-}
 // the last of the 64 numbers, in ascending order, that is not above v
 __device__ __forceinline__ int last_upto(const int* at, int v) {
   int i = 0;
