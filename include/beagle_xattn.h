@@ -740,6 +740,11 @@ beagle_status beagle_xattn_kv_append_paged(const beagle_xattn_desc* desc, const 
  *   in : as beagle_xattn_paged_attend; group_first [n_groups + 1], n_shared
  *        [n_groups], DEVICE; 1 <= n_groups <= B
  *   out: o [B,M,H,d], lse [B,H,M] float
+ * It pays where many entries have many rows in common.  Of little work it is slower than
+ * beagle_xattn_paged_attend on the same cache, which reads common rows for each entry: with 8 kv heads of
+ * 128 bf16 and a query each, 4 entries up to 14000 common rows, 16 up to 1200, 64 up to 500 (340 rows
+ * 8 us, here 16; 16 entries of 4000 rows 33 and 22).  desc->seq_kv is a matter of speed, too: with a bound
+ * far above the longest sequence groups of more than 128 query rows can take up to 9 us more.
  * B * M * H / G at most 2^28.
  * Workspace: BEAGLE_WS_PAGED_SHARED.
  */

@@ -5,8 +5,10 @@
 //
 // Bound: the rows' bytes where groups have few query rows, their products where many (see attend_wide); of little work the three launches and their trips to
 // memory, some 14 us.  Measured (MI355X, bf16, a graph's replays): 12 entries of 10 queries under a tree, 40 heads, 3 groups of up to 6000 common rows, up to
-// 500 own (340 MB) 94 us, its second launch 81 at 4.2 TB/s; 32 entries of a query, 32 / 8 heads, 4000 common, up to 700 own (69 MB) 31.5 us, its second launch 21.
-// Each entry by itself they would read 1.0 and 0.6 GB.
+// 500 own (340 MB) 95 us, its second launch 78 at 4.4 TB/s; 32 entries of a query, 32 / 8 heads, 4000 common, up to 700 own (69 MB) 31 us, its second launch 20.
+// Each entry by itself they would read 1.0 and 0.6 GB.  Of few common rows paged_attend, one launch or two, takes less though it reads them for every entry: 4 entries
+// of a query 340 rows 8.3 us and here 15.8, 4000 16.5 / 20.4, 16000 32.1 / 30.5; 16 entries of 1000 17.6 / 18.5, 2000 23.9 / 20.2; 64 of 300 and 200 own 25.4 / 27.1,
+// 1000 39.3 / 28.5.
 //
 // Three launches.  The first, one workgroup, divides the work into units: some blocks of 32 rows for a few tiles of 16 query rows, of a
 // group's common rows or of an entry's own.  In the second as many workgroups as fit take units, those that are done take more; each unit
@@ -678,7 +680,8 @@ void launch_paged_shared(bool bf16, PagedSharedArgs p, void* ws, hipStream_t s) 
   // Eight waves where a group has on average more query rows than one of their wide units, and those times the rows that a sequence can have pass 3 * 2^20 (8 kv
   // heads, us with 8 / 4 waves): 1024 query rows over 16000 rows 150 / 179, over 4000 65 / 74, 256 over 16000 74 / 78; 512 over 4000 58 / 49, 1024 over
   // 2000 52 / 45, 128 over 4000 44 / 37: there the entries' own rows are as much, whose units are better small and many.  Wide units already from 33
-  // query rows on: groups of 40 over 6000 rows, 32 or 40 kv heads: 92 and 81 us, in units of 32 query rows, 113 and 86 (48: as fast).
+  // query rows on: groups of 40 over 6000 rows, 32 or 40 kv heads: 92 and 81 us, in units of 32 query rows, 113 and 86 (48: as fast).  (The rows are the caller's
+  // bound: where it is far above the sequences there are, eight waves come too early, by the figures above up to 9 us.)
   auto work = [&](auto w_) {
     using W = Work<decltype(w_)::value>;
     x.waves = decltype(w_)::value;
