@@ -55,7 +55,8 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 
 struct PickShared {
-  uint32_t count[256], state[2];
+  alignas(16) uint32_t count[256];         // (four are read at a time)
+  uint32_t state[2];
   int sure, listed, here, list[SELECT_LISTED];
   uint32_t best[SELECT_LISTED];
   int found[SELECT_WAVES];

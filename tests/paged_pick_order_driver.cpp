@@ -6,6 +6,7 @@
 #include <ucontext.h>
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -82,6 +83,7 @@ static void hand_over() { host_barrier(__LINE__); }
 
 namespace {
 using namespace beagle;
+static_assert(alignof(PickShared) >= 16 && offsetof(PickShared, count) % 16 == 0, "four counts are read at a time");
 constexpr int EDGE = 64;
 struct Case {
   int n, n_select, lead, R, memory, order;
